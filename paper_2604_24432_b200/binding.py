@@ -29,6 +29,8 @@ KSA_FLAG_SINGLE_CTA_KERNEL = 0x4
 KSA_FLAG_CTA_PAIR_KERNEL = 0x8
 KSA_FLAG_BWD_MMA_SYNC_KERNELS = 0x10
 KSA_STREAM_TEXT, KSA_STREAM_SUMMARY = 0, 1
+KSA_KV_BF16, KSA_KV_E4M3 = 0, 1
+KSA_PAGED_STATUS_BAD_PAGE, KSA_PAGED_STATUS_BAD_ROWS = 103, 104
 
 EXPORTS = [
     "ksa_create", "ksa_destroy", "ksa_aug_len", "ksa_total_aug_len", "ksa_workspace_bytes",
@@ -42,6 +44,7 @@ EXPORTS = [
     "ksa_anneal_lambda", "ksa_position_ids", "ksa_total_summary_rows", "ksa_qkv_prepare",
     "ksa_prepared_workspace_bytes", "ksa_attn_fwd_prepared",
     "ksa_part_rows", "ksa_attn_fwd_part",
+    "ksa_paged_append", "ksa_paged_gather", "ksa_paged_attn",
 ]
 
 
@@ -71,6 +74,19 @@ class ksa_cache_params(ctypes.Structure):
         ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
         ("softmax_scale", ctypes.c_float), ("flags", ctypes.c_uint32),
     ]
+
+
+class ksa_paged_params(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("struct_size", "batch", "num_rows", "chunk_len", "summaries_per_chunk", "window_chunks",
+                                              "num_q_heads", "num_kv_heads", "head_dim")] + [
+        ("softmax_scale", ctypes.c_float), ("flags", ctypes.c_uint32), ("kv_format", ctypes.c_int32), ("page_rows", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32), ("text_cols", ctypes.c_int32), ("summ_cols", ctypes.c_int32)] + [
+        (n, ctypes.c_int64) for n in ("page_stride", "head_stride", "row_stride", "q_stride_tok", "q_stride_head", "k_stride_tok",
+                                      "k_stride_head", "v_stride_tok", "v_stride_head", "o_stride_tok", "o_stride_head")]
+
+
+class ksa_paged_kv(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("kpages", "vpages", "kscale", "vscale", "text_table", "summ_table", "cached", "cu_rows")]
 
 
 class ksa_tile_rec(ctypes.Structure):
@@ -143,6 +159,10 @@ def lib():
     L.ksa_cache_fill_from_prefill.argtypes = [vp, vp, vp, vp, vp, vp, pp, cp, vp]
     L.ksa_decode_text.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, cp, vp]
     L.ksa_decode_summary.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, cp, vp]
+    gp, gk = ctypes.POINTER(ksa_paged_params), ctypes.POINTER(ksa_paged_kv)
+    L.ksa_paged_append.argtypes = [vp, gk, vp, vp, gp, vp]
+    L.ksa_paged_gather.argtypes = [vp, gk, vp, vp, gp, vp]
+    L.ksa_paged_attn.argtypes = [vp, gk, vp, vp, vp, gp, vp]
     L.ksa_strerror.restype = ctypes.c_char_p
     L.ksa_strerror.argtypes = [ctypes.c_int]
     _lib = L
@@ -530,3 +550,125 @@ class DecodeCache:
 
     def decode_summary(self, q, k_new, v_new, out, lse, stream=None):
         self._step(lib().ksa_decode_summary, "ksa_decode_summary", q, k_new, v_new, out, lse, stream)
+
+
+@dataclass
+class PagedSpec:
+    """Python-side holder of what a ``ksa_paged_params`` says of the cache (fmt: "bf16" or "e4m3")."""
+    k: int
+    m: int
+    C: int
+    Hq: int
+    Hkv: int
+    D: int
+    scale: float
+    page_rows: int
+    num_pages: int
+    fmt: str = "bf16"
+    flags: int = 0
+
+
+@dataclass
+class PagedBatch:
+    """The sequences of a call (int32 CUDA tensors, see include/ksa_paged.h): rows cached before it [B], the calls' packed
+    rows [B + 1], and the page tables [B, columns] of text and summaries (summ_table may be None where m == 0).  The tensors
+    are read on the device at every call (and every replay of a captured one)."""
+    cached: "torch.Tensor"
+    cu_rows: "torch.Tensor"
+    text_table: "torch.Tensor"
+    summ_table: Optional["torch.Tensor"] = None
+
+    def __post_init__(self):
+        import torch
+        B = self.cached.numel()
+        _expect(self.cached.dim() == 1 and B >= 1 and tuple(self.cu_rows.shape) == (B + 1,), "cached must be [B], cu_rows [B + 1]")
+        for name in ("cached", "cu_rows", "text_table", "summ_table"):
+            t = getattr(self, name)
+            if name == "summ_table" and t is None:
+                continue
+            _expect(t.dtype == torch.int32 and t.is_contiguous() and t.device == self.cached.device, name + " must be contiguous int32, all on one device")
+            if name.endswith("table"):
+                _expect(t.dim() == 2 and t.shape[0] == B, name + " must be [B, columns]")
+
+
+def _expect(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+class PagedCache:
+    """The page pools of a paged KV cache plus the calls on it (argument marshalling only).
+
+    kpages, vpages [num_pages, Hkv, page_rows, D] (any strides, head_dim contiguous; bf16, or float8_e4m3fn with the scale
+    bytes kscale, vscale uint8 [num_pages, Hkv, page_rows]) are allocated here unless they are given."""
+
+    def __init__(self, ctx: "Context", spec: PagedSpec, kpages=None, vpages=None, kscale=None, vscale=None):
+        import torch
+        self.ctx, self.spec = ctx, spec
+        self.device = torch.device("cuda", ctx.device)
+        _expect(spec.fmt in ("bf16", "e4m3"), "fmt must be \"bf16\" or \"e4m3\"")
+        quantised = spec.fmt == "e4m3"
+        dtype = torch.float8_e4m3fn if quantised else torch.bfloat16
+        shape = (spec.num_pages, spec.Hkv, spec.page_rows, spec.D)
+        _expect((kpages is None) == (vpages is None) and (kscale is None) == (vscale is None), "K and V pools come together")
+        if kpages is None:
+            kpages, vpages = (torch.zeros(shape, dtype=dtype, device=self.device) for _ in range(2))
+        if quantised and kscale is None:
+            kscale, vscale = (torch.zeros(shape[:3], dtype=torch.uint8, device=self.device) for _ in range(2))
+        _expect(quantised or kscale is None, "a bf16 cache has no scales")
+        for t in (kpages, vpages):
+            _expect(tuple(t.shape) == shape and t.dtype == dtype and t.device == self.device, "pools must be %s %s on %s" % (shape, dtype, self.device))
+            _expect(t.stride() == kpages.stride() and t.stride(3) == 1, "K and V pools must have the same strides, head_dim contiguous")
+        for t in (kscale, vscale) if quantised else ():
+            _expect(tuple(t.shape) == shape[:3] and t.dtype == torch.uint8 and t.device == self.device and t.is_contiguous(), "scales must be contiguous uint8 %s on %s" % (shape[:3], self.device))
+        self.kpages, self.vpages, self.kscale, self.vscale = kpages, vpages, kscale, vscale
+
+    def _args(self, batch: PagedBatch, rows: int, q, k, v, o):
+        s = self.spec
+        _expect(batch.cached.device == self.device, "the batch must be on " + str(self.device))
+        _expect(batch.summ_table is not None or s.m == 0, "summ_table is missing")
+
+        def strides(t, H):
+            if t is None:
+                return H * s.D, s.D
+            _expect(tuple(t.shape) == (rows, H, s.D) and t.dtype == self._bf16() and t.device == self.device and t.stride(2) == 1,
+                    "rows must be bf16 [num_rows, heads, head_dim] on %s, head_dim contiguous" % self.device)
+            return t.stride(0) if rows > 1 else H * s.D, t.stride(1) if H > 1 else s.D
+        p = ksa_paged_params(_PAGED_SIZE, batch.cached.numel(), rows, s.k, s.m, s.C, s.Hq, s.Hkv, s.D, s.scale, s.flags,
+                             KSA_KV_E4M3 if s.fmt == "e4m3" else KSA_KV_BF16, s.page_rows, s.num_pages, batch.text_table.shape[1],
+                             0 if batch.summ_table is None else batch.summ_table.shape[1], *self.kpages.stride()[:3],
+                             *strides(q, s.Hq), *strides(k, s.Hkv), *strides(v, s.Hkv), *strides(o, s.Hq))
+        ptr = lambda t: None if t is None else t.data_ptr()
+        return ksa_paged_kv(self.kpages.data_ptr(), self.vpages.data_ptr(), ptr(self.kscale), ptr(self.vscale), batch.text_table.data_ptr(),
+                            ptr(batch.summ_table), batch.cached.data_ptr(), batch.cu_rows.data_ptr()), p
+
+    @staticmethod
+    def _bf16():
+        import torch
+        return torch.bfloat16
+
+    def _stream(self, stream):
+        return _current_stream(self.device) if stream is None else stream
+
+    def append(self, batch: PagedBatch, k, v, stream: Optional[int] = None):
+        """ksa_paged_append: k, v [num_rows, Hkv, D] of the batch's new rows into their pages (quantised on the way)."""
+        kv, p = self._args(batch, k.shape[0], None, k, v, None)
+        _check(lib().ksa_paged_append(self.ctx.handle, ctypes.byref(kv), k.data_ptr(), v.data_ptr(), ctypes.byref(p), self._stream(stream)),
+               "ksa_paged_append")
+
+    def gather(self, batch: PagedBatch, k, v, stream: Optional[int] = None):
+        """ksa_paged_gather: the rows cached[b] .. of every sequence back into k, v [num_rows, Hkv, D]."""
+        kv, p = self._args(batch, k.shape[0], None, k, v, None)
+        _check(lib().ksa_paged_gather(self.ctx.handle, ctypes.byref(kv), k.data_ptr(), v.data_ptr(), ctypes.byref(p), self._stream(stream)),
+               "ksa_paged_gather")
+
+    def attn(self, batch: PagedBatch, q, out, lse, stream: Optional[int] = None):
+        """ksa_paged_attn: q, out [num_rows, Hq, D], lse fp32 [Hq, num_rows]; the rows' own K and V have been appended."""
+        kv, p = self._args(batch, q.shape[0], q, None, None, out)
+        _expect(tuple(lse.shape) == (self.spec.Hq, q.shape[0]) and lse.is_contiguous() and lse.element_size() == 4 and lse.is_floating_point() and lse.device == self.device,
+                "lse must be contiguous fp32 [heads, num_rows]")
+        _check(lib().ksa_paged_attn(self.ctx.handle, ctypes.byref(kv), q.data_ptr(), out.data_ptr(), lse.data_ptr(), ctypes.byref(p),
+                                    self._stream(stream)), "ksa_paged_attn")
+
+
+_PAGED_SIZE = ctypes.sizeof(ksa_paged_params)

@@ -55,7 +55,7 @@ struct ksa_ctx {
     bool tc_ready = false;
     bool pair_ready = false;          // CTA-pair text kernel set up on this device
     int max_pairs = 0;                // clusters of two CTAs the device runs at once
-    bool bwd_ready = false, bwd_tc_ready = false, decode_ready = false;
+    bool bwd_ready = false, bwd_tc_ready = false, decode_ready = false, paged_ready = false;
     // host entry point: copy streams and per-chunk events of its upload / compute / download pipeline
     cudaStream_t s_in = nullptr, s_out = nullptr;
     std::vector<cudaEvent_t> ev_in, ev_done;
@@ -101,6 +101,8 @@ int ksa_ctx_num_sms(const ksa_ctx* ctx) { return ctx->num_sms; }
 void ksa_ctx_add_launches(ksa_ctx* ctx, int n) { ctx->launches += n; }
 int ksa_ctx_cuda_fail(ksa_ctx* ctx, int cuda_error) { return cuda_fail(ctx, (cudaError_t)cuda_error); }
 bool* ksa_ctx_decode_ready(ksa_ctx* ctx) { return &ctx->decode_ready; }
+bool* ksa_ctx_paged_ready(ksa_ctx* ctx) { return &ctx->paged_ready; }
+int ksa_ctx_device(const ksa_ctx* ctx) { return ctx->device; }
 
 // ---------------------------------------------------------------------------------------
 // validation and layout

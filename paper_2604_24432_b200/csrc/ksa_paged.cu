@@ -1,0 +1,306 @@
+// The paged KV cache: rows written into their pages (quantised on the way) and read back, and the C ABI of the paged calls.
+//
+// Both passes are bound by HBM: an element is read and written once.  D / 8 lanes take one row of one head, 16 bytes of
+// bf16 each, K and V of it at once; the row's sequence, page and place in the page are worked out by every lane for itself.
+#include <cuda_bf16.h>
+
+#include "ksa_host.h"
+#include "ksa_launch.h"
+#include "ksa_paged.h"
+#include "ksa_ptx.cuh"
+
+namespace ksa {
+
+constexpr int kRowThreads = 256;
+
+// Where packed row i of the call lies: its page (or -1, -2) and the place in it; false if it is no row of a sequence.
+// Executed by whole warps.  Up to 32 sequences are searched in registers (one load instead of one after another).
+__device__ __forceinline__ bool paged_find(const PagedArgs& a, int i, int& page, int& slot)
+{
+    int lo = 0, hi = a.B - 1, row0, r1;                        // the last sequence that starts at or before row i
+    if (a.B <= 32) {
+        const int lane = threadIdx.x & 31, mine = __ldcg(a.cu + min(lane, a.B));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            const int at = __shfl_sync(0xffffffffu, mine, (lo + o) & 31);
+            if (lo + o <= hi && at <= i) lo += o;
+        }
+        row0 = __shfl_sync(0xffffffffu, mine, lo);
+        r1 = __shfl_sync(0xffffffffu, mine, (lo + 1) & 31);
+        if (lo == 31) r1 = __ldcg(a.cu + 32);
+    } else {
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (__ldcg(a.cu + mid) <= i) lo = mid; else hi = mid - 1;
+        }
+        row0 = __ldcg(a.cu + lo);
+        r1 = __ldcg(a.cu + lo + 1);
+    }
+    int n, first;
+    if (i >= a.rows || !paged_seq(a, row0, r1, lo, n, first) || i < row0 || i >= r1) return false;
+    bool summ;
+    const int x = paged_place(a, first + (i - row0), summ);
+    page = paged_page(a, lo, summ, x);
+    slot = x & ((1 << a.page_shift) - 1);
+    return true;
+}
+
+// Every sequence's lengths, looked at by the first block: a row's search meets only those of the sequences that it lands in.
+__device__ __forceinline__ void paged_check_all(const PagedArgs& a)
+{
+    if (blockIdx.x != 0) return;
+    for (int b = threadIdx.x; b < a.B; b += kRowThreads) {
+        int n, first;
+        paged_seq(a, __ldcg(a.cu + b), __ldcg(a.cu + b + 1), b, n, first);
+    }
+}
+
+// 8 bf16 values times a power of two -> 8 e4m3
+__device__ __forceinline__ uint32_t e4m3x2_from_f32(float lo, float hi)
+{
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint2 quantise8(const uint4& x, float f)
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint32_t y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = e4m3x2_from_f32(__uint_as_float(w[i] << 16) * f, __uint_as_float(w[i] & 0xffff0000u) * f);
+    return make_uint2(y[0] | (y[1] << 16), y[2] | (y[3] << 16));
+}
+// The largest scale, 2^120: 256 times it is more than bf16 holds, the value below it is 240 (0x77)
+__device__ __forceinline__ uint2 keep_finite(const uint2& y)
+{
+    auto cut = [](uint32_t w) { return __vminu4(w & 0x7f7f7f7fu, 0x77777777u) | (w & 0x80808080u); };
+    return make_uint2(cut(y.x), cut(y.y));
+}
+// largest magnitude of 8 bf16 values, as bits (in both halves' order: an infinity or a NaN comes out at 0x7f80 or above)
+__device__ __forceinline__ uint32_t top8(const uint4& x)
+{
+    const uint32_t m = 0x7fff7fffu;
+    const uint32_t t = __vmaxu2(__vmaxu2(x.x & m, x.y & m), __vmaxu2(x.z & m, x.w & m));
+    return max(t >> 16, t & 0xffffu);
+}
+
+template <int D, bool E4M3>
+__global__ void __launch_bounds__(kRowThreads) ksa_paged_append_kernel(PagedArgs a)
+{
+    constexpr int kLanes = D / 8, kUnits = kRowThreads / kLanes;
+    ptx::pdl_launch_dependents();
+    ptx::pdl_wait();
+    paged_check_all(a);
+    const int lane = threadIdx.x % kLanes;
+    const int64_t unit = (int64_t)blockIdx.x * kUnits + threadIdx.x / kLanes;      // (row, head)
+    const int i = (int)(unit / a.Hkv), h = (int)(unit - (int64_t)i * a.Hkv);
+    int page = -1, slot = 0;
+    bool put = paged_find(a, i, page, slot);
+    if (put && page < 0) {
+        atomicCAS(a.status, 0, KSA_PAGED_STATUS_BAD_PAGE);
+        put = false;
+    }
+    uint4 xk{}, xv{};
+    if (put) {
+        xk = __ldcg(reinterpret_cast<const uint4*>(a.k + i * a.k_st + h * a.k_sh + lane * 8));
+        xv = __ldcg(reinterpret_cast<const uint4*>(a.v + i * a.v_st + h * a.v_sh + lane * 8));
+    }
+    const int64_t at = page * a.page_st + h * a.head_st + slot * a.row_st;
+    if constexpr (!E4M3) {
+        if (!put) return;
+        *reinterpret_cast<uint4*>(a.kp + at + lane * 16) = xk;
+        *reinterpret_cast<uint4*>(a.vp + at + lane * 16) = xv;
+    } else {
+        uint32_t top = top8(xk) | (top8(xv) << 16);            // K's in the low half, V's in the high half
+#pragma unroll
+        for (int o = kLanes / 2; o > 0; o >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (!put) return;
+        // the row's largest magnitude is (1 + mant / 128) 2^(e - 127): within 448 = 1.75 * 2^8 at 2^(e - 135), or at twice that
+        auto scale_of = [](uint32_t t) { return t >= 0x7f80u ? 255 : max(17, (int)(t >> 7) - 8 + ((t & 0x7fu) > 0x60u)); };
+        const int ek = scale_of(top & 0xffffu), ev = scale_of(top >> 16);
+        // (two to the minus that is a normal number for every byte from 17 to 247)
+        uint2 yk = quantise8(xk, __uint_as_float((uint32_t)(254 - ek) << 23)), yv = quantise8(xv, __uint_as_float((uint32_t)(254 - ev) << 23));
+        if (ek == 247) yk = keep_finite(yk);
+        if (ev == 247) yv = keep_finite(yv);
+        *reinterpret_cast<uint2*>(a.kp + at + lane * 8) = ek == 255 ? make_uint2(0, 0) : yk;
+        *reinterpret_cast<uint2*>(a.vp + at + lane * 8) = ev == 255 ? make_uint2(0, 0) : yv;
+        if (lane == 0) {
+            const int64_t se = (((int64_t)page * a.Hkv + h) << a.page_shift) + slot;
+            a.ke[se] = (uint8_t)ek;
+            a.ve[se] = (uint8_t)ev;
+        }
+    }
+}
+
+template <int D, bool E4M3>
+__global__ void __launch_bounds__(kRowThreads) ksa_paged_gather_kernel(PagedArgs a)
+{
+    constexpr int kLanes = D / 8, kUnits = kRowThreads / kLanes;
+    ptx::pdl_launch_dependents();
+    ptx::pdl_wait();
+    paged_check_all(a);
+    const int lane = threadIdx.x % kLanes;
+    const int64_t unit = (int64_t)blockIdx.x * kUnits + threadIdx.x / kLanes;
+    const int i = (int)(unit / a.Hkv), h = (int)(unit - (int64_t)i * a.Hkv);
+    int page = -1, slot = 0;
+    if (!paged_find(a, i, page, slot)) return;
+    if (page == -2) atomicCAS(a.status, 0, KSA_PAGED_STATUS_BAD_PAGE);
+    uint4 xk{}, xv{};
+    if (page >= 0) {
+        const int64_t at = page * a.page_st + h * a.head_st + slot * a.row_st;
+        if constexpr (!E4M3) {
+            xk = __ldcg(reinterpret_cast<const uint4*>(a.kp + at + lane * 16));
+            xv = __ldcg(reinterpret_cast<const uint4*>(a.vp + at + lane * 16));
+        } else {
+            const uint2 yk = __ldcg(reinterpret_cast<const uint2*>(a.kp + at + lane * 8)), yv = __ldcg(reinterpret_cast<const uint2*>(a.vp + at + lane * 8));
+            const int64_t se = (((int64_t)page * a.Hkv + h) << a.page_shift) + slot;
+            const float fk = e8m0_scale(__ldcg(a.ke + se)), fv = e8m0_scale(__ldcg(a.ve + se));
+            auto two = [](uint32_t y, float f) { const float2 v = e4m3x2_to_f32(y & 0xffffu); return ptx::pack_bf16x2(v.x * f, v.y * f); };
+            xk = make_uint4(two(yk.x, fk), two(yk.x >> 16, fk), two(yk.y, fk), two(yk.y >> 16, fk));
+            xv = make_uint4(two(yv.x, fv), two(yv.x >> 16, fv), two(yv.y, fv), two(yv.y >> 16, fv));
+        }
+    }
+    *reinterpret_cast<uint4*>(a.k + i * a.k_st + h * a.k_sh + lane * 8) = xk;
+    *reinterpret_cast<uint4*>(a.v + i * a.v_st + h * a.v_sh + lane * 8) = xv;
+}
+
+template <class K>
+static cudaError_t launch_rows(K kernel, const PagedArgs& a, cudaStream_t stream)
+{
+    const int64_t units = (int64_t)a.rows * a.Hkv, per = kRowThreads / (a.D / 8);
+    return launch_dependent(kernel, dim3((unsigned)((units + per - 1) / per)), kRowThreads, 0, stream, a);
+}
+cudaError_t launch_paged_append(const PagedArgs& a, bool e4m3, cudaStream_t stream)
+{
+    if (a.D == 128) return launch_rows(e4m3 ? ksa_paged_append_kernel<128, true> : ksa_paged_append_kernel<128, false>, a, stream);
+    return launch_rows(e4m3 ? ksa_paged_append_kernel<64, true> : ksa_paged_append_kernel<64, false>, a, stream);
+}
+cudaError_t launch_paged_gather(const PagedArgs& a, bool e4m3, cudaStream_t stream)
+{
+    if (a.D == 128) return launch_rows(e4m3 ? ksa_paged_gather_kernel<128, true> : ksa_paged_gather_kernel<128, false>, a, stream);
+    return launch_rows(e4m3 ? ksa_paged_gather_kernel<64, true> : ksa_paged_gather_kernel<64, false>, a, stream);
+}
+
+}  // namespace ksa
+
+// =================================================================================================
+// C ABI
+// =================================================================================================
+using namespace ksa;
+
+#define KSA_API extern "C" __attribute__((visibility("default")))
+
+static int validate_paged(const ksa_paged_params* p, const ksa_paged_kv* kv)
+{
+    if (!p || p->struct_size != (int32_t)sizeof(ksa_paged_params) || !kv) return KSA_ERR_INVALID_ARG;
+    if (p->batch < 1 || p->num_rows < 0 || p->chunk_len < 1 || p->summaries_per_chunk < 0 || p->window_chunks < 0) return KSA_ERR_INVALID_ARG;
+    if (p->num_q_heads < 1 || p->num_kv_heads < 1 || p->num_q_heads % p->num_kv_heads != 0) return KSA_ERR_INVALID_ARG;
+    if (!(p->softmax_scale > 0.f) || p->softmax_scale > 1e30f) return KSA_ERR_INVALID_ARG;
+    if (p->flags & ~KSA_FLAG_SUMMARY_TEXT_ONLY) return KSA_ERR_INVALID_ARG;
+    if (p->kv_format != KSA_KV_BF16 && p->kv_format != KSA_KV_E4M3) return KSA_ERR_INVALID_ARG;
+    if (p->num_pages < 1 || p->text_cols < 1 || p->summ_cols < (p->summaries_per_chunk > 0 ? 1 : 0)) return KSA_ERR_INVALID_ARG;
+    if (p->head_dim != 64 && p->head_dim != 128) return KSA_ERR_UNSUPPORTED;
+    if (p->page_rows != 16 && p->page_rows != 32 && p->page_rows != 64 && p->page_rows != 128) return KSA_ERR_UNSUPPORTED;
+    if (p->num_q_heads / p->num_kv_heads > 64 || p->num_q_heads > 1024 || p->batch > 65535 || p->num_rows > (1 << 24)) return KSA_ERR_UNSUPPORTED;
+    if ((int64_t)p->chunk_len + p->summaries_per_chunk > (1 << 30)) return KSA_ERR_UNSUPPORTED;
+    const int64_t unit = p->kv_format == KSA_KV_BF16 ? 8 : 16;              // 16 bytes
+    for (int64_t st : {p->page_stride, p->head_stride, p->row_stride}) {
+        if (st < 0 || st % unit != 0) return KSA_ERR_INVALID_ARG;
+        if (st >= (1ll << 38)) return KSA_ERR_UNSUPPORTED;
+    }
+    if (p->row_stride < p->head_dim) return KSA_ERR_INVALID_ARG;
+    auto misaligned = [](const void* q) { return ((uintptr_t)q & 15) != 0; };
+    if (!kv->kpages || !kv->vpages || misaligned(kv->kpages) || misaligned(kv->vpages)) return KSA_ERR_INVALID_ARG;
+    if (p->kv_format == KSA_KV_E4M3 && (!kv->kscale || !kv->vscale || misaligned(kv->kscale) || misaligned(kv->vscale))) return KSA_ERR_INVALID_ARG;
+    if (!kv->text_table || (!kv->summ_table && p->summaries_per_chunk > 0) || !kv->cached || !kv->cu_rows) return KSA_ERR_INVALID_ARG;
+    return KSA_OK;
+}
+
+// A packed tensor of the call
+static bool tensor_ok(const void* t, int64_t st, int64_t sh)
+{
+    return t && ((uintptr_t)t & 15) == 0 && st >= 0 && sh >= 0 && st % 8 == 0 && sh % 8 == 0 && st < (1ll << 38) && sh < (1ll << 38);
+}
+
+static PagedArgs paged_args(ksa_ctx* ctx, const ksa_paged_kv* kv, const ksa_paged_params* p)
+{
+    PagedArgs a{};
+    a.kp = (uint8_t*)kv->kpages; a.vp = (uint8_t*)kv->vpages; a.ke = kv->kscale; a.ve = kv->vscale;
+    a.text_table = kv->text_table; a.summ_table = kv->summ_table; a.cached = kv->cached; a.cu = kv->cu_rows;
+    const int64_t width = p->kv_format == KSA_KV_BF16 ? 2 : 1;
+    a.page_st = p->page_stride * width; a.head_st = p->head_stride * width; a.row_st = p->row_stride * width;
+    a.q_st = p->q_stride_tok; a.q_sh = p->q_stride_head; a.k_st = p->k_stride_tok; a.k_sh = p->k_stride_head;
+    a.v_st = p->v_stride_tok; a.v_sh = p->v_stride_head; a.o_st = p->o_stride_tok; a.o_sh = p->o_stride_head;
+    a.B = p->batch; a.rows = p->num_rows; a.kk = p->chunk_len; a.m = p->summaries_per_chunk; a.C = p->window_chunks;
+    a.Hq = p->num_q_heads; a.Hkv = p->num_kv_heads; a.G = a.Hq / a.Hkv; a.D = p->head_dim;
+    a.page_shift = p->page_rows == 16 ? 4 : p->page_rows == 32 ? 5 : p->page_rows == 64 ? 6 : 7;
+    a.num_pages = p->num_pages; a.text_cols = p->text_cols; a.summ_cols = p->summ_cols;
+    a.flags = p->flags;
+    a.scale_log2 = p->softmax_scale * 1.4426950408889634f;
+    a.status = ksa_ctx_status_word(ctx);
+    return a;
+}
+
+namespace {
+// The context's device for the length of a call
+struct OnDevice {
+    int before = -1;
+    cudaError_t err;
+    explicit OnDevice(int device)
+    {
+        err = cudaGetDevice(&before);
+        if (err == cudaSuccess && before != device) err = cudaSetDevice(device); else before = -1;
+    }
+    ~OnDevice() { if (before >= 0) cudaSetDevice(before); }
+};
+}  // namespace
+
+template <class F>
+static int paged_call(ksa_ctx* ctx, const ksa_paged_params* p, F launch)
+{
+    if (p->num_rows == 0) return KSA_OK;
+    OnDevice on(ksa_ctx_device(ctx));
+    cudaError_t e = on.err;
+    if (e == cudaSuccess) e = launch();
+    if (e != cudaSuccess) return ksa_ctx_cuda_fail(ctx, (int)e);
+    ksa_ctx_add_launches(ctx, 1);
+    return KSA_OK;
+}
+
+KSA_API int ksa_paged_append(ksa_ctx* ctx, const ksa_paged_kv* kv, const void* k, const void* v, const ksa_paged_params* p, void* cuda_stream)
+{
+    const int rc = validate_paged(p, kv);
+    if (rc != KSA_OK) return rc;
+    if (!ctx || !tensor_ok(k, p->k_stride_tok, p->k_stride_head) || !tensor_ok(v, p->v_stride_tok, p->v_stride_head)) return KSA_ERR_INVALID_ARG;
+    PagedArgs a = paged_args(ctx, kv, p);
+    a.k = (uint16_t*)k; a.v = (uint16_t*)v;
+    return paged_call(ctx, p, [&] { return launch_paged_append(a, p->kv_format == KSA_KV_E4M3, (cudaStream_t)cuda_stream); });
+}
+
+KSA_API int ksa_paged_gather(ksa_ctx* ctx, const ksa_paged_kv* kv, void* k, void* v, const ksa_paged_params* p, void* cuda_stream)
+{
+    const int rc = validate_paged(p, kv);
+    if (rc != KSA_OK) return rc;
+    if (!ctx || !tensor_ok(k, p->k_stride_tok, p->k_stride_head) || !tensor_ok(v, p->v_stride_tok, p->v_stride_head)) return KSA_ERR_INVALID_ARG;
+    PagedArgs a = paged_args(ctx, kv, p);
+    a.k = (uint16_t*)k; a.v = (uint16_t*)v;
+    return paged_call(ctx, p, [&] { return launch_paged_gather(a, p->kv_format == KSA_KV_E4M3, (cudaStream_t)cuda_stream); });
+}
+
+KSA_API int ksa_paged_attn(ksa_ctx* ctx, const ksa_paged_kv* kv, const void* q, void* out, float* lse, const ksa_paged_params* p, void* cuda_stream)
+{
+    const int rc = validate_paged(p, kv);
+    if (rc != KSA_OK) return rc;
+    if (!ctx || !tensor_ok(q, p->q_stride_tok, p->q_stride_head) || !tensor_ok(out, p->o_stride_tok, p->o_stride_head) || !lse || ((uintptr_t)lse & 3)) return KSA_ERR_INVALID_ARG;
+    PagedArgs a = paged_args(ctx, kv, p);
+    a.q = (const uint16_t*)q; a.out = (uint16_t*)out; a.lse = lse;
+    return paged_call(ctx, p, [&]() -> cudaError_t {
+        bool& ready = *ksa_ctx_paged_ready(ctx);                // shared-memory opt-in: a per-device setting
+        if (!ready) {
+            const cudaError_t e = setup_paged_attn();
+            if (e != cudaSuccess) return e;
+            ready = true;
+        }
+        return launch_paged_attn(a, p->kv_format == KSA_KV_E4M3, ksa_ctx_num_sms(ctx), (cudaStream_t)cuda_stream);
+    });
+}

@@ -1,0 +1,123 @@
+// Internal declarations of the paged KV cache: arguments of its kernels, where a row lies, which rows a query tile sees.
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include "../../include/ksa_paged.h"
+#include "ksa_common.h"
+#include "ksa_paged_index.h"
+
+namespace ksa {
+
+struct PagedArgs {
+    uint8_t* kp; uint8_t* vp; uint8_t* ke; uint8_t* ve;              // pages (bytes), scale bytes
+    const int32_t* text_table; const int32_t* summ_table; const int32_t* cached; const int32_t* cu;
+    uint16_t* k; uint16_t* v;                                        // rows written or read back
+    const uint16_t* q; uint16_t* out; float* lse;
+    int64_t page_st, head_st, row_st;                                // of the pages, in bytes
+    int64_t q_st, q_sh, k_st, k_sh, v_st, v_sh, o_st, o_sh;          // in elements
+    int32_t B, rows, kk, m, C, Hq, Hkv, G, D;
+    int32_t page_shift, num_pages, text_cols, summ_cols;             // page_rows = 1 << page_shift
+    int32_t tokens_per_tile, head_blocks, nsplit;                    // attention: see the kernels
+    uint32_t flags;
+    float scale_log2;
+    int32_t* status;
+};
+
+cudaError_t launch_paged_append(const PagedArgs& a, bool e4m3, cudaStream_t stream);
+cudaError_t launch_paged_gather(const PagedArgs& a, bool e4m3, cudaStream_t stream);
+cudaError_t launch_paged_attn(const PagedArgs& a, bool e4m3, int num_sms, cudaStream_t stream);
+cudaError_t setup_paged_attn();
+
+#if defined(__CUDACC__)
+// ---- rows and pages -------------------------------------------------------------------------------------------------
+// (Lengths, tables and rows are read past L1: a kernel here may start while the one before the one in front of it still reads,
+// after which L1 may keep a line that the one in front rewrites.)
+// Lengths of sequence b, checked: false for what are no lengths (nothing of such a sequence is touched).
+__device__ __forceinline__ bool paged_seq(const PagedArgs& a, int row0, int r1, int b, int& n, int& first)
+{
+    first = __ldcg(a.cached + b);
+    n = r1 - row0;
+    if (!paged_lengths_ok(a, row0, r1, first)) {
+        atomicCAS(a.status, 0, KSA_PAGED_STATUS_BAD_ROWS);
+        n = 0;
+        return false;
+    }
+    return true;
+}
+
+// The page of row x of a sequence's text (summaries), or -1 (entry -1: given back) or -2 (no page of the pool).
+__device__ __forceinline__ int paged_page(const PagedArgs& a, int b, bool summ, int x)
+{
+    const int col = x >> a.page_shift, cols = summ ? a.summ_cols : a.text_cols;
+    if (col >= cols) return -2;
+    return paged_entry(a, __ldcg((summ ? a.summ_table : a.text_table) + (int64_t)b * cols + col));
+}
+
+// ---- query tiles ------------------------------------------------------------------------------------------------------
+// Tile `item` of the call, counted through the sequences (text tiles of a sequence before its summary tiles).  Executed by a
+// whole warp: 32 sequences at a time.
+__device__ __forceinline__ PagedTile paged_tile(const PagedArgs& a, int item)
+{
+    const int lane = threadIdx.x & 31, per = a.tokens_per_tile;
+    PagedTile t{-1, false, 0, 0, 0, 0};
+    for (int base = 0; base < a.B; base += 32) {
+        int row0 = 0, n = 0, first = 0, t0 = 0, nt = 0, tt = 0, ts = 0;
+        if (base + lane < a.B) {
+            row0 = __ldcg(a.cu + base + lane);
+            paged_seq(a, row0, __ldcg(a.cu + base + lane + 1), base + lane, n, first);
+        }
+        if (n > 0) {
+            t0 = paged_texts(a, first);
+            nt = paged_texts(a, first + n) - t0;
+            tt = (nt + per - 1) / per;
+            ts = (n - nt + per - 1) / per;
+        }
+        int sum = tt + ts;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += up;
+        }
+        const int total = __shfl_sync(0xffffffffu, sum, 31);
+        if (item < total) {
+            const int src = __ffs(__ballot_sync(0xffffffffu, sum > item)) - 1;
+            int i = item - __shfl_sync(0xffffffffu, sum - tt - ts, src);
+            tt = __shfl_sync(0xffffffffu, tt, src); nt = __shfl_sync(0xffffffffu, nt, src); t0 = __shfl_sync(0xffffffffu, t0, src);
+            n = __shfl_sync(0xffffffffu, n, src);
+            t.b = base + src;
+            t.row0 = __shfl_sync(0xffffffffu, row0, src);
+            t.first = __shfl_sync(0xffffffffu, first, src);
+            t.summ = i >= tt;
+            if (t.summ) i -= tt;
+            const int have = t.summ ? n - nt : nt;
+            t.x0 = (t.summ ? t.first - t0 : t0) + i * per;
+            t.n = min(per, have - i * per);
+            return t;
+        }
+        item -= total;
+    }
+    return t;
+}
+
+// ---- e4m3 rows ------------------------------------------------------------------------------------------------------------
+// 2^(e - 127); 255: NaN
+__device__ __forceinline__ float e8m0_scale(uint32_t e)
+{
+    return __uint_as_float(e == 255u ? 0x7fc00000u : e == 0u ? 0x00400000u : e << 23);
+}
+// Two e4m3 values (low byte first) as fp32
+__device__ __forceinline__ float2 e4m3x2_to_f32(uint32_t two)
+{
+    float2 f;
+    asm("{\n\t.reg .b32 h;\n\t.reg .b16 w, lo, hi;\n\t"
+        "cvt.u16.u32 w, %2;\n\t"
+        "cvt.rn.f16x2.e4m3x2 h, w;\n\t"
+        "mov.b32 {lo, hi}, h;\n\t"
+        "cvt.f32.f16 %0, lo;\n\tcvt.f32.f16 %1, hi;\n\t}"
+        : "=f"(f.x), "=f"(f.y) : "r"(two));
+    return f;
+}
+#endif
+
+}  // namespace ksa

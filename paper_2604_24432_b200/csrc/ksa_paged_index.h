@@ -1,0 +1,83 @@
+// Index arithmetic of the paged KV cache: which row is which token, where it lies, what it sees.  Plain C++ for both sides: the
+// kernels use it, and the tests compile it for the host and compare it with Eqs. 1 and 3 row by row.
+// `A` holds kk, m, C (chunk length, summaries, window), flags, rows and num_pages.
+#pragma once
+#include <stdint.h>
+
+#ifdef __CUDACC__
+#define KSA_HD __host__ __device__ __forceinline__
+#else
+#define KSA_HD inline
+#endif
+#ifndef KSA_FLAG_SUMMARY_TEXT_ONLY
+#define KSA_FLAG_SUMMARY_TEXT_ONLY 0x1u
+#endif
+
+namespace ksa {
+
+// Whether a sequence can have the packed rows [row0, r1), the first of them its row `first` (at most 2^30 rows a sequence).
+template <class A> KSA_HD bool paged_lengths_ok(const A& a, int row0, int r1, int first)
+{
+    return row0 >= 0 && r1 >= row0 && r1 <= a.rows && first >= 0 && r1 - row0 <= (1 << 30) && first <= (1 << 30) - (r1 - row0);
+}
+// A page-table entry: the page, -1 (given back) or -2 (no page of the pool).
+template <class A> KSA_HD int paged_entry(const A& a, int entry) { return entry >= -1 && entry < a.num_pages ? entry : -2; }
+
+// A row of Eq. 1: text or summary, and its number among those.
+template <class A> KSA_HD int paged_place(const A& a, int row, bool& summ)
+{
+    const int s = a.kk + a.m, c = row / s, r = row - c * s;
+    summ = r >= a.kk;
+    return summ ? c * a.m + (r - a.kk) : c * a.kk + r;
+}
+// Text tokens (summaries) among the first `row` rows of a sequence.
+template <class A> KSA_HD int paged_texts(const A& a, int row)
+{
+    const int s = a.kk + a.m, c = row / s, r = row - c * s;
+    return c * a.kk + (r < a.kk ? r : a.kk);
+}
+
+// A query tile: tokens_per_tile (or fewer) consecutive text tokens, or consecutive summaries, of one sequence.  Its rows
+// are (token, query head of the group), and what they see is one range of text and one of summaries each.
+struct PagedTile {
+    int b;                   // sequence; -1: no such tile
+    bool summ;
+    int x0, n;               // first text token (summary) and how many
+    int64_t row0;            // packed row of the sequence's row `first`
+    int first;
+};
+
+// The packed row of a tile's text token (summary) x.
+template <class A> KSA_HD int64_t paged_row(const A& a, const PagedTile& t, int x)
+{
+    const int64_t s = a.kk + a.m;
+    const int64_t row = t.summ ? (int64_t)(x / a.m) * s + a.kk + x % a.m : (int64_t)(x / a.kk) * s + x % a.kk;
+    return t.row0 + (row - t.first);
+}
+
+// What text token (summary) x sees: text [t_lo, t_hi), summaries [s_lo, s_hi).
+struct PagedView { int t_lo, t_hi, s_lo, s_hi; };
+template <class A> KSA_HD PagedView paged_view(const A& a, bool summ, int x)
+{
+    PagedView w;
+    if (!summ) {                                       // Eq. 3
+        const int c = x / a.kk, far = c > a.C ? c - a.C : 0;
+        w.t_lo = far * a.kk; w.t_hi = x + 1;
+        w.s_lo = 0; w.s_hi = far * a.m;
+    } else {                                           // own chunk (Sec. 2.2.1)
+        const int c = x / a.m;
+        w.t_lo = c * a.kk; w.t_hi = w.t_lo + a.kk;
+        w.s_lo = c * a.m;
+        w.s_hi = (a.flags & KSA_FLAG_SUMMARY_TEXT_ONLY) ? w.s_lo : x + 1;
+    }
+    return w;
+}
+// What anything in the tile sees: both ranges start with those of its first row and end with those of its last.
+template <class A> KSA_HD PagedView paged_tile_view(const A& a, const PagedTile& t)
+{
+    const PagedView lo = paged_view(a, t.summ, t.x0), hi = paged_view(a, t.summ, t.x0 + t.n - 1);
+    const bool none = t.summ && (a.flags & KSA_FLAG_SUMMARY_TEXT_ONLY);
+    return PagedView{lo.t_lo, hi.t_hi, lo.s_lo, hi.s_hi > lo.s_lo && !none ? hi.s_hi : lo.s_lo};
+}
+
+}  // namespace ksa

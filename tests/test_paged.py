@@ -1,0 +1,167 @@
+"""Paged KV cache without a GPU: the index arithmetic of its kernels (compiled for the host) against Eqs. 1 and 3 row by row,
+and what the calls refuse."""
+import ctypes
+import dataclasses
+import os
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_24432_b200 import binding as ksa
+from paper_2604_24432_b200 import build as ksa_build
+from tests import paged_ref as ref
+
+HOST = r"""
+#include "ksa_paged_index.h"
+struct Shape { int kk, m, C, rows, num_pages; unsigned flags; };
+extern "C" {
+int place(const Shape* a, int row, int* summ) { bool s; int x = ksa::paged_place(*a, row, s); *summ = s; return x; }
+int texts(const Shape* a, int row) { return ksa::paged_texts(*a, row); }
+int entry(const Shape* a, int e) { return ksa::paged_entry(*a, e); }
+int lengths_ok(const Shape* a, int row0, int r1, int first) { return ksa::paged_lengths_ok(*a, row0, r1, first); }
+void view(const Shape* a, int summ, int x, int* v) { auto w = ksa::paged_view(*a, summ, x); v[0] = w.t_lo; v[1] = w.t_hi; v[2] = w.s_lo; v[3] = w.s_hi; }
+void tile_view(const Shape* a, int summ, int x0, int n, int* v) { ksa::PagedTile t{0, summ != 0, x0, n, 0, 0}; auto w = ksa::paged_tile_view(*a, t); v[0] = w.t_lo; v[1] = w.t_hi; v[2] = w.s_lo; v[3] = w.s_hi; }
+long long row(const Shape* a, int summ, int x, int row0, int first) { ksa::PagedTile t{0, summ != 0, 0, 0, row0, first}; return ksa::paged_row(*a, t, x); }
+}
+"""
+
+
+class Shape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("kk", "m", "C", "rows", "num_pages")] + [("flags", ctypes.c_uint)]
+
+
+@pytest.fixture(scope="module")
+def index(tmp_path_factory):
+    d = tmp_path_factory.mktemp("paged")
+    src, so = d / "index.cpp", d / "index.so"
+    src.write_text(HOST)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-I", ksa_build.CSRC, str(src), "-o", str(so)], check=True)
+    L = ctypes.CDLL(str(so))
+    L.row.restype = ctypes.c_longlong
+    return L
+
+
+@pytest.mark.parametrize("k,m,C,flags", [(8, 1, 3, 0), (8, 1, 0, 0), (64, 8, 1, 0), (1, 1, 5, 0), (3, 2, 2, 1), (8, 0, 1 << 20, 0), (4, 0, 2, 0), (200, 3, 1, 1)])
+def test_rows_places_and_views(index, k, m, C, flags):
+    a = Shape(k, m, C, 1 << 20, 10, flags)
+    rows = 4 * (k + m) * max(1, min(C, 4)) + 5
+    where = ref.places(k, m, rows)
+    out4 = (ctypes.c_int * 4)()
+    for row, (is_summ, x) in enumerate(where):
+        s = ctypes.c_int()
+        assert (index.place(ctypes.byref(a), row, ctypes.byref(s)), bool(s.value)) == (x, is_summ)
+        assert index.texts(ctypes.byref(a), row) == sum(not w[0] for w in where[:row])
+        assert index.row(ctypes.byref(a), int(is_summ), x, 70, 3) == 70 + row - 3
+        index.view(ctypes.byref(a), int(is_summ), x, out4)
+        see = ref.visible(k, m, C, row, rows, bool(flags & 1))
+        text = [w[1] for i, w in enumerate(where) if see[i] and not w[0]]
+        summ = [w[1] for i, w in enumerate(where) if see[i] and w[0]]
+        assert list(range(out4[0], out4[1])) == text and list(range(out4[2], max(out4[2], out4[3]))) == summ, row
+    # a tile's view covers what its rows see, and is no wider than from its first to its last
+    for kind in (False, True):
+        have = [i for i, w in enumerate(where) if w[0] == kind]
+        for lo in range(0, len(have), max(1, len(have) // 7)):
+            for n in (1, 5, 16):
+                part = have[lo:lo + n]
+                if not part:
+                    continue
+                index.tile_view(ctypes.byref(a), int(kind), where[part[0]][1], len(part), out4)
+                see = np.any([ref.visible(k, m, C, i, rows, bool(flags & 1)) for i in part], axis=0)
+                text = [w[1] for i, w in enumerate(where) if see[i] and not w[0]]
+                summ = [w[1] for i, w in enumerate(where) if see[i] and w[0]]
+                assert (min(text), max(text) + 1) == (out4[0], out4[1])
+                assert (summ == [] and out4[2] >= out4[3]) or (min(summ), max(summ) + 1) == (out4[2], out4[3])
+
+
+def test_entries_and_lengths(index):
+    a = Shape(8, 1, 3, 100, 10, 0)
+    assert [index.entry(ctypes.byref(a), e) for e in (-1, 0, 9, 10, -2, 2**31 - 1, -2**31)] == [-1, 0, 9, -2, -2, -2, -2]
+    ok = lambda *v: bool(index.lengths_ok(ctypes.byref(a), *v))
+    assert ok(0, 0, 0) and ok(0, 100, 0) and ok(99, 100, 2**30 - 1) and ok(100, 100, 2**30)
+    assert not ok(-1, 5, 0) and not ok(5, 4, 0) and not ok(0, 101, 0) and not ok(0, 1, -1) and not ok(0, 1, 2**30)
+    assert not ok(-2**31, 2**31 - 1, 0) and not ok(0, -5, 0) and not ok(0, 1, 2**31 - 1)
+
+
+def test_e4m3_reference_matches_torch():
+    x = np.concatenate([np.linspace(-448, 448, 20001), ref.E4M3, (ref.E4M3[1:] + ref.E4M3[:-1]) / 2])
+    x = torch.from_numpy(x).float().double().numpy()
+    x[0] = 448.0
+    codes, byte = ref.quantise_row(x)
+    assert byte == 127
+    want = torch.from_numpy(x).float().to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    assert (codes == want).all()
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    ksa_build.build()
+
+
+def _call(fn="append", kv_change=None, tensor_change=None, **change):
+    """Status of a call with made-up (never touched) pointers and no context: what is wrong is said before anything else."""
+    D, Hkv, Hq, ps = change.get("head_dim", 128), 2, 8, 64
+    good = dict(struct_size=ctypes.sizeof(ksa.ksa_paged_params), batch=2, num_rows=5, chunk_len=8, summaries_per_chunk=1, window_chunks=4,
+                num_q_heads=Hq, num_kv_heads=Hkv, head_dim=D, softmax_scale=0.1, flags=0, kv_format=ksa.KSA_KV_E4M3, page_rows=ps,
+                num_pages=7, text_cols=3, summ_cols=1, page_stride=Hkv * ps * D, head_stride=ps * D, row_stride=D,
+                q_stride_tok=Hq * D, q_stride_head=D, k_stride_tok=Hkv * D, k_stride_head=D, v_stride_tok=Hkv * D, v_stride_head=D,
+                o_stride_tok=Hq * D, o_stride_head=D)
+    p = ksa.ksa_paged_params(**{**good, **change})
+    kv = ksa.ksa_paged_kv(**{**{n: 0x10000 * (i + 1) for i, (n, _) in enumerate(ksa.ksa_paged_kv._fields_)}, **(kv_change or {})})
+    x, y, z = {**dict(x=0x900000, y=0xA00000, z=0xB00000), **(tensor_change or {})}.values()
+    L = ksa.lib()
+    if fn == "attn":
+        return L.ksa_paged_attn(None, ctypes.byref(kv), x, y, z, ctypes.byref(p), None)
+    return getattr(L, "ksa_paged_" + fn)(None, ctypes.byref(kv), x, y, ctypes.byref(p), None)
+
+
+BAD, UNSUP = ksa.KSA_ERR_INVALID_ARG, ksa.KSA_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("fn", ["append", "gather", "attn"])
+@pytest.mark.parametrize("change,want", [
+    (dict(struct_size=8), BAD), (dict(batch=0), BAD), (dict(num_rows=-1), BAD), (dict(chunk_len=0), BAD), (dict(summaries_per_chunk=-1), BAD),
+    (dict(window_chunks=-1), BAD), (dict(num_q_heads=7), BAD), (dict(num_kv_heads=0), BAD), (dict(head_dim=96), UNSUP),
+    (dict(softmax_scale=0.0), BAD), (dict(softmax_scale=float("nan")), BAD), (dict(flags=2), BAD), (dict(kv_format=2), BAD),
+    (dict(page_rows=48), UNSUP), (dict(page_rows=256), UNSUP), (dict(page_rows=8), UNSUP), (dict(num_pages=0), BAD), (dict(text_cols=0), BAD),
+    (dict(summ_cols=0), BAD), (dict(page_stride=-16), BAD), (dict(row_stride=120), BAD), (dict(row_stride=64), BAD), (dict(head_stride=8), BAD),
+    (dict(num_q_heads=130), UNSUP), (dict(num_rows=1 << 25), UNSUP), (dict(batch=70000), UNSUP), (dict(chunk_len=2**31 - 1), UNSUP),
+    (dict(kv_change=dict(kpages=None)), BAD), (dict(kv_change=dict(vpages=0x10008)), BAD), (dict(kv_change=dict(kscale=None)), BAD),
+    (dict(kv_change=dict(vscale=0x10004)), BAD), (dict(kv_change=dict(text_table=None)), BAD), (dict(kv_change=dict(summ_table=None)), BAD),
+    (dict(kv_change=dict(cached=None)), BAD), (dict(kv_change=dict(cu_rows=None)), BAD), (dict(tensor_change=dict(x=None)), BAD),
+    (dict(tensor_change=dict(y=0xA00008)), BAD), (dict(), BAD),        # all well but for the context
+])
+def test_refusals(fn, change, want):
+    assert _call(fn, **change) == want
+
+
+@pytest.mark.parametrize("fn,change", [("append", dict(k_stride_tok=12)), ("append", dict(v_stride_head=-8)), ("gather", dict(k_stride_tok=1 << 38)),
+                                       ("attn", dict(q_stride_tok=4)), ("attn", dict(o_stride_head=-8)), ("attn", dict(tensor_change=dict(z=None))),
+                                       ("attn", dict(tensor_change=dict(z=0xB00002)))])
+def test_refusals_of_row_tensors(fn, change):
+    assert _call(fn, **change) == BAD
+
+
+def test_null_structures():
+    assert ksa.lib().ksa_paged_append(None, None, None, None, None, None) == BAD
+    assert ksa.lib().ksa_paged_attn(None, None, None, None, None, None, None) == BAD
+
+
+def test_binding_refusals():
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
+    good = dict(cached=i32(2), cu_rows=i32(3), text_table=i32(2, 4), summ_table=i32(2, 1))
+    ksa.PagedBatch(**good)
+    for bad in (dict(cu_rows=i32(2)), dict(cached=i32(2, 1)), dict(text_table=i32(3, 4)), dict(text_table=i32(8)), dict(cached=torch.zeros(2, dtype=torch.int64)),
+                dict(summ_table=i32(4, 2).t()), dict(summ_table=i32(2, 4)[:, ::2])):
+        with pytest.raises(ValueError):
+            ksa.PagedBatch(**{**good, **bad})
+
+    class Ctx:                                       # no device is needed to refuse
+        device, handle = 0, None
+    spec = ksa.PagedSpec(8, 1, 4, 8, 2, 128, 0.1, 64, 3, "bf16")
+    pool = torch.zeros((3, 2, 64, 128), dtype=torch.bfloat16)
+    for s, kw in ((dataclasses.replace(spec, fmt="int8"), {}), (spec, dict(kpages=pool)), (spec, dict(kpages=pool, vpages=pool)),
+                  (spec, dict(kpages=pool, vpages=pool, kscale=pool, vscale=pool))):
+        with pytest.raises(ValueError):
+            ksa.PagedCache(Ctx, s, **kw)
