@@ -103,6 +103,7 @@ int ksa_ctx_cuda_fail(ksa_ctx* ctx, int cuda_error) { return cuda_fail(ctx, (cud
 bool* ksa_ctx_decode_ready(ksa_ctx* ctx) { return &ctx->decode_ready; }
 bool* ksa_ctx_paged_ready(ksa_ctx* ctx) { return &ctx->paged_ready; }
 int ksa_ctx_device(const ksa_ctx* ctx) { return ctx->device; }
+void* ksa_ctx_encode_tiled(const ksa_ctx* ctx) { return (void*)ctx->encode; }
 
 // ---------------------------------------------------------------------------------------
 // validation and layout

@@ -28,6 +28,11 @@ cudaError_t launch_paged_append(const PagedArgs& a, bool e4m3, cudaStream_t stre
 cudaError_t launch_paged_gather(const PagedArgs& a, bool e4m3, cudaStream_t stream);
 cudaError_t launch_paged_attn(const PagedArgs& a, bool e4m3, int num_sms, cudaStream_t stream);
 cudaError_t setup_paged_attn();
+// The same on tcgen05, for tiles of more than 16 query rows.
+typedef CUresult (*PagedEncode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+cudaError_t launch_paged_tc(const PagedArgs& a, bool e4m3, int num_sms, PagedEncode encode, cudaStream_t stream);
+cudaError_t setup_paged_tc();
 
 #if defined(__CUDACC__)
 // ---- rows and pages -------------------------------------------------------------------------------------------------

@@ -1,0 +1,675 @@
+// Attention of a run of new rows over the paged KV cache on the sm_100a tensor cores: pieces of prompts, drafted tokens.
+//
+// A CTA works on up to 256 query rows of one sequence and KV head, (token, query head of the group) each, as two tiles of 128
+// (128 / group tokens), so that a key tile serves the whole group.  What they see is one range of summaries and one of text
+// (Eq. 3; a summary: its own chunk), walked in tiles of 128 keys; where a call has too few query tiles for the device, the
+// key tiles are split over a cluster's CTAs, whose results meet in distributed shared memory.
+//
+// Warp roles:
+//   warps 0-3   query tile 0: load Q, softmax (one row per thread), O rescale, epilogue
+//   warps 4-7   query tile 1
+//   warp  8     TMA of the key tiles, one box a page, the pages looked up a tile ahead by a lane each
+//   warp  9     issues S = Q K^T (tcgen05.mma, smem x smem)
+//   warp 10     issues O += P V (P from TMEM)
+//   warp 11     TMA of the value tiles (bf16 pages)
+//   warps 12-15 (e4m3 pages) turn the tiles that warp 8 brings in 8 bits into bf16 ones, a row per thread, its scale on the way
+// TMEM: one score slot S [0,128) that the two query tiles take in turns, the bf16 probabilities P0 [128,192), P1 [192,256),
+// O0 [256,256+D), O1 [384,384+D).  The pipeline over the key tiles is that of the text-row kernel (ksa_text_tc.cu).
+//
+// Rows of a page that nothing in the tile sees may hold anything.  Scores of such keys are replaced by -inf; their V rows
+// are overwritten with zeros in shared memory (0 * NaN would reach the accumulators): by warp 10 in the tiles that hold an end
+// of a range, or by the converting warps.
+//
+// Every mbarrier wait is bounded, as in the other kernels: on timeout all roles leave their loops, copies in flight are waited
+// for, the cluster's barriers are still passed, TMEM is freed.
+#include <cuda_bf16.h>
+
+#include "ksa_launch.h"
+#include "ksa_paged.h"
+#include "ksa_ptx.cuh"
+#include "ksa_wait.cuh"
+
+namespace ksa {
+
+using namespace ptx;
+
+constexpr int kPtTile = 128;
+constexpr int kPtMaxSplit = 8;                       // the portable cluster size
+// log2 units: P stays below 2^12 (see ksa_text_tc.cu)
+constexpr float kPtRescale = 12.0f;
+
+template <int D, bool E4M3>
+struct PtCfg {
+    static constexpr int kThreads = E4M3 ? 512 : 384;
+    // registers per thread after the hand-over: softmax, TMA / MMA, converting warps
+    static constexpr int kRegsSoftmax = E4M3 ? 208 : 216, kRegsOther = E4M3 ? 40 : 72, kRegsConvert = 56;
+    static_assert(8 * kRegsSoftmax + 4 * kRegsOther + (E4M3 ? 4 * kRegsConvert : 0) <= kThreads / 32 * ((65536 / kThreads) / 8 * 8), "register hand-over exceeds the CTA's allocation");
+    static constexpr int kTileBytes = kPtTile * D * 2;
+    static constexpr int kHalves = D / 64;           // 64-column (128-byte) swizzle panels
+    static constexpr int kRawBytes = kPtTile * D;    // a tile in 8 bits
+    static constexpr int kStagesK = E4M3 ? (D == 128 ? 2 : 3) : (D == 128 ? 3 : 5);
+    static constexpr int kStagesV = E4M3 ? (D == 128 ? 2 : 3) : (D == 128 ? 2 : 5);
+    static constexpr int kStagesRaw = E4M3 ? (D == 128 ? 2 : 6) : 0;
+    static constexpr int kQOff = 0;
+    static constexpr int kKOff = 2 * kTileBytes;
+    static constexpr int kVOff = kKOff + kStagesK * kTileBytes;
+    static constexpr int kRawOff = kVOff + kStagesV * kTileBytes;
+    static constexpr int kBarOff = kRawOff + kStagesRaw * kRawBytes;
+    // barrier slots
+    static constexpr int kQFull = 0, kSFull = 2, kLoaded = 4, kPFull = 6, kPvDone = 8, kDrain = 10;
+    static constexpr int kKFull = 12, kKEmpty = kKFull + kStagesK, kVFull = kKEmpty + kStagesK, kVEmpty = kVFull + kStagesV;
+    static constexpr int kRawFull = kVEmpty + kStagesV, kRawEmpty = kRawFull + kStagesRaw;
+    static constexpr int kNumBars = kRawEmpty + kStagesRaw;
+    static constexpr int kSmemBytes = kBarOff + 8 * kNumBars + 64 + 1024;   // + slack for 1024-byte alignment
+    // partial results, over Q, K and V once these are done with: O fp32 [256][D], then (maximum, sum) [256]
+    static constexpr int kPartMl = 256 * D * 4;
+    static_assert(kPartMl + 256 * 8 <= kBarOff, "partial results fit over the tiles");
+};
+
+struct PagedMaps { CUtensorMap k, v; };
+
+__device__ __forceinline__ void pt_named_barrier(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ void pt_st_shared4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint4 pt_ld_shared4(uint32_t addr)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 pt_ld_cluster4(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float2 pt_ld_cluster2(uint32_t addr)
+{
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+    return v;
+}
+
+// The share of the key tiles that a CTA walks: tiles [j0, j1) of the unit's summary tiles (from s_t0), then its text tiles.
+struct PtWalk {
+    PagedView see;
+    int s_tiles, s_t0, t_t0, j0, j1;
+    // tile j: its first row, its stream, and the rows [lo, hi) of that stream that anything in the unit sees
+    __device__ __forceinline__ bool at(int j, int& x0, int& lo, int& hi) const
+    {
+        const bool summ = j < s_tiles;
+        x0 = (summ ? s_t0 + j : t_t0 + j - s_tiles) * kPtTile;
+        lo = summ ? see.s_lo : see.t_lo;
+        hi = summ ? see.s_hi : see.t_hi;
+        return summ;
+    }
+};
+__device__ __forceinline__ PtWalk pt_walk(const PagedArgs& a, const PagedTile& t, int split)
+{
+    PtWalk w;
+    w.see = paged_tile_view(a, t);
+    w.s_t0 = w.see.s_lo / kPtTile;
+    w.s_tiles = w.see.s_hi > w.see.s_lo ? (w.see.s_hi + kPtTile - 1) / kPtTile - w.s_t0 : 0;
+    w.t_t0 = w.see.t_lo / kPtTile;
+    const int tiles = w.s_tiles + (w.see.t_hi + kPtTile - 1) / kPtTile - w.t_t0;
+    const int per = (tiles + a.nsplit - 1) / a.nsplit;
+    w.j0 = min(tiles, split * per);
+    w.j1 = min(tiles, w.j0 + per);
+    return w;
+}
+
+template <int D, bool E4M3>
+__global__ void __launch_bounds__(PtCfg<D, E4M3>::kThreads, 1)
+ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedMaps maps)
+{
+    using Cfg = PtCfg<D, E4M3>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t sQ = smem_base + Cfg::kQOff, sK = smem_base + Cfg::kKOff, sV = smem_base + Cfg::kVOff, sRaw = smem_base + Cfg::kRawOff;
+    const uint32_t bars = smem_base + Cfg::kBarOff;
+    const uint32_t tmem_slot = bars + 8 * Cfg::kNumBars;
+    const uint32_t abort_addr = tmem_slot + 4;
+    auto bar = [&](int i) -> uint32_t { return bars + 8u * (uint32_t)i; };
+
+    const int tid = threadIdx.x;
+    const int warp = (int)__reduce_or_sync(0xffffffffu, (unsigned)tid >> 5);     // (uniform to the compiler)
+    const int lane = tid & 31;
+
+    if (tid == 0) {
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(bar(Cfg::kQFull + t), 128);       // one arrival per row's thread
+            mbar_init(bar(Cfg::kSFull + t), 1);
+            mbar_init(bar(Cfg::kLoaded + t), 4);        // one arrival per softmax warp
+            mbar_init(bar(Cfg::kPFull + t), 4);
+            mbar_init(bar(Cfg::kPvDone + t), 1);
+            mbar_init(bar(Cfg::kDrain + t), 1);
+        }
+        const int writers = E4M3 ? 4 : 1;               // converting warps, or the TMA's thread
+        for (int st = 0; st < Cfg::kStagesK; ++st) { mbar_init(bar(Cfg::kKFull + st), writers); mbar_init(bar(Cfg::kKEmpty + st), 1); }
+        for (int st = 0; st < Cfg::kStagesV; ++st) { mbar_init(bar(Cfg::kVFull + st), writers); mbar_init(bar(Cfg::kVEmpty + st), 1); }
+        for (int st = 0; st < Cfg::kStagesRaw; ++st) { mbar_init(bar(Cfg::kRawFull + st), 1); mbar_init(bar(Cfg::kRawEmpty + st), 4); }
+        st_shared_u32(abort_addr, 0u);
+        st_shared_u32(abort_addr + 4, 0u);     // never raised: lets the teardown waits run while aborting
+        fence_mbar_init();
+    }
+    if (warp == 8) {                           // one warp allocates all 512 TMEM columns (1 CTA per SM)
+        tmem_alloc(tmem_slot, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = ld_shared_u32(tmem_slot);
+    pdl_wait();
+    pdl_launch_dependents();
+
+    const int split = (int)blockIdx.x % a.nsplit, unit = (int)blockIdx.x / a.nsplit;
+    const int hk = unit % a.Hkv;
+    const PagedTile t = paged_tile(a, unit / a.Hkv);       // up to 2 * per tokens
+    const int per = a.tokens_per_tile / 2;
+    if (t.b >= 0) {                                         // (the same for the whole cluster)
+    const PtWalk w = pt_walk(a, t, split);
+    const int T = w.j1 - w.j0;
+    const int nh = T == 0 ? 0 : t.n > per ? 2 : 1;          // query tiles
+
+    if (warp >= 12) {
+        if constexpr (E4M3) {
+            // ============================ 8-bit tiles to bf16 ============================
+            setmaxnreg_dec<Cfg::kRegsConvert>();
+            const int row = tid & 127;
+            bool alive = true;
+            int k_stage = 0, v_stage = 0, raw = 0;
+            uint32_t k_phase = 0, v_phase = 0, raw_phase = 0;
+            // this thread's row of tile j: whether anyone sees it, and its scales (found a tile ahead)
+            auto scales = [&](int j, float& fk, float& fv) {
+                fk = fv = 0.f;
+                if (j >= w.j1) return;
+                int x0, lo, hi;
+                const bool summ = w.at(j, x0, lo, hi);
+                const int x = x0 + row;
+                if (x < lo || x >= hi) return;
+                const int page = paged_page(a, t.b, summ, x);
+                if (page < 0) return;
+                const int64_t at = (((int64_t)page * a.Hkv + hk) << a.page_shift) + (x & ((1 << a.page_shift) - 1));
+                fk = e8m0_scale(__ldcg(a.ke + at));
+                fv = e8m0_scale(__ldcg(a.ve + at));
+            };
+            auto convert = [&](uint32_t full, uint32_t empty, uint32_t empty_parity, uint32_t dst, float f) {
+                if (alive) alive = __all_sync(0xffffffffu, bounded_wait(bar(Cfg::kRawFull + raw), raw_phase, abort_addr, a.status, kStatusWaitKvFull));
+                if (alive) alive = __all_sync(0xffffffffu, bounded_wait(empty, empty_parity, abort_addr, a.status, kStatusWaitKvEmpty));
+                if (!alive) return;
+                const uint32_t src = sRaw + raw * Cfg::kRawBytes + row * D;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    const int c = (i + row) & (D / 16 - 1);         // neighbouring rows start at different banks
+                    uint4 y = pt_ld_shared4(src + c * 16);
+                    uint32_t z[8];
+                    const uint32_t yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 p = e4m3x2_to_f32(yw[e] & 0xffffu), q = e4m3x2_to_f32(yw[e] >> 16);
+                        z[2 * e] = f == 0.f ? 0u : pack_bf16x2(p.x * f, p.y * f);
+                        z[2 * e + 1] = f == 0.f ? 0u : pack_bf16x2(q.x * f, q.y * f);
+                    }
+                    const uint32_t d = dst + (c >> 2) * 16384 + row * 128;
+                    pt_st_shared4(d + ((((c & 3) * 2) ^ (row & 7)) << 4), z[0], z[1], z[2], z[3]);
+                    pt_st_shared4(d + ((((c & 3) * 2 + 1) ^ (row & 7)) << 4), z[4], z[5], z[6], z[7]);
+                }
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) { mbar_arrive(full); mbar_arrive(bar(Cfg::kRawEmpty + raw)); }
+                if (++raw == Cfg::kStagesRaw) { raw = 0; raw_phase ^= 1u; }
+            };
+            float fk, fv;
+            scales(w.j0, fk, fv);
+            for (int j = w.j0; j < w.j1 && alive; ++j) {
+                float nk, nv;
+                scales(j + 1, nk, nv);
+                convert(bar(Cfg::kKFull + k_stage), bar(Cfg::kKEmpty + k_stage), k_phase ^ 1u, sK + k_stage * Cfg::kTileBytes, fk);
+                if (++k_stage == Cfg::kStagesK) { k_stage = 0; k_phase ^= 1u; }
+                convert(bar(Cfg::kVFull + v_stage), bar(Cfg::kVEmpty + v_stage), v_phase ^ 1u, sV + v_stage * Cfg::kTileBytes, fv);
+                if (++v_stage == Cfg::kStagesV) { v_stage = 0; v_phase ^= 1u; }
+                fk = nk; fv = nv;
+            }
+            if (a.nsplit > 1) { __syncwarp(); cluster_arrive(); cluster_wait(); cluster_arrive(); cluster_wait(); }
+        }
+    } else if (warp >= 8) {
+        setmaxnreg_dec<Cfg::kRegsOther>();
+        if (warp == 8 || (warp == 11 && !E4M3)) {
+            // =============================== TMA producers ===============================
+            // bf16: warp 8 brings the K tiles, warp 11 the V tiles; e4m3: warp 8 brings K and V tiles in turn.  A page is
+            // one box (a panel of 64 columns of it in bf16), each by a lane of its own.
+            const bool is_v = warp == 11;
+            const int stages = E4M3 ? Cfg::kStagesRaw : is_v ? Cfg::kStagesV : Cfg::kStagesK;
+            const uint32_t ring = E4M3 ? sRaw : is_v ? sV : sK;
+            const uint32_t full0 = bar(E4M3 ? Cfg::kRawFull : is_v ? Cfg::kVFull : Cfg::kKFull), empty0 = bar(E4M3 ? Cfg::kRawEmpty : is_v ? Cfg::kVEmpty : Cfg::kKEmpty);
+            constexpr int kBytes = E4M3 ? Cfg::kRawBytes : Cfg::kTileBytes;
+            const int pages = kPtTile >> a.page_shift;       // of a tile
+            if (lane == 0) { prefetch_tensormap(&maps.k); prefetch_tensormap(&maps.v); }
+            // page of lane's rows of tile j; num_pages (a box of zeros) where nobody sees any of them
+            auto find = [&](int j) {
+                int x0, lo, hi;
+                if (j >= w.j1 || lane >= pages) return a.num_pages;
+                const bool summ = w.at(j, x0, lo, hi);
+                const int x = x0 + (lane << a.page_shift);
+                if (x >= hi || x + (1 << a.page_shift) <= lo) return a.num_pages;
+                const int page = paged_page(a, t.b, summ, x);
+                if (page < 0) { atomicCAS(a.status, 0, KSA_PAGED_STATUS_BAD_PAGE); return a.num_pages; }
+                return page;
+            };
+            int stage = 0;
+            uint32_t phase = 0, armed_mask = 0, armed_parity = 0;
+            bool alive = true;
+            int page = find(w.j0);
+            for (int j = w.j0; j < w.j1 && alive; ++j) {
+                const int next = find(j + 1);
+                for (int u = 0; u < (E4M3 ? 2 : 1) && alive; ++u) {
+                    const uint32_t full = full0 + 8u * stage;
+                    alive = __all_sync(0xffffffffu, bounded_wait(empty0 + 8u * stage, phase ^ 1u, abort_addr, a.status, kStatusWaitKvEmpty));
+                    if (!alive) break;
+                    if (lane == 0) mbar_arrive_expect_tx(full, (uint32_t)kBytes);
+                    armed_mask |= 1u << stage;
+                    armed_parity = (armed_parity & ~(1u << stage)) | (phase << stage);
+                    __syncwarp();
+                    if (lane < pages) {
+                        const CUtensorMap* map = is_v || u == 1 ? &maps.v : &maps.k;
+                        const uint32_t rows0 = (uint32_t)lane << a.page_shift;
+                        if constexpr (E4M3) {
+                            tma_load_4d(ring + stage * kBytes + rows0 * D, map, full, 0, 0, hk, page);
+                        } else {
+#pragma unroll
+                            for (int h = 0; h < Cfg::kHalves; ++h) tma_load_4d(ring + stage * kBytes + h * 16384 + rows0 * 128, map, full, h * 64, 0, hk, page);
+                        }
+                    }
+                    if (++stage == stages) { stage = 0; phase ^= 1u; }
+                }
+                page = next;
+            }
+            if (ld_shared_u32(abort_addr) != 0u) {           // leave no copy in flight behind
+                for (int st = 0; st < stages; ++st)
+                    if (armed_mask & (1u << st)) bounded_wait(full0 + 8u * st, (armed_parity >> st) & 1u, abort_addr + 4, a.status, kStatusWaitKvFull);
+            }
+        } else if (warp != 11) {
+            // =============================== MMA issuers =================================
+            constexpr uint32_t hi = smem_desc_hi_sw128(1024);
+            const uint32_t leader = elect_one();
+            const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+            bool alive = true;
+            auto wait = [&](uint32_t b, uint32_t parity, int code) {
+                if (alive) alive = __all_sync(0xffffffffu, bounded_wait(b, parity, abort_addr, a.status, code));
+            };
+            uint32_t stage = 0, ring_phase = 0, phase0 = 0, phase1 = 0;
+            if (warp == 9) {
+                constexpr uint32_t idesc = make_idesc_bf16(128, 128, false);
+                const uint32_t q_lo = smem_desc_lo(sQ, 16), k_lo = smem_desc_lo(sK, 16);
+                int before = -1;                            // query tile whose scores stand in the slot
+                for (int j = 0; j < T && alive; ++j) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        if (u == 1 && nh == 1) break;
+                        if (j == 0) wait(bar(Cfg::kQFull + u), 0, kStatusWaitQFull);
+                        if (u == 0) wait(bar(Cfg::kKFull) + 8u * stage, ring_phase, kStatusWaitKvFull);
+                        // the slot: the scores before are in their group's registers
+                        if (before == 0) { wait(bar(Cfg::kLoaded), phase0, kStatusWaitPFull); phase0 ^= 1u; }
+                        else if (before == 1) { wait(bar(Cfg::kLoaded + 1), phase1, kStatusWaitPFull); phase1 ^= 1u; }
+                        if (!alive) break;
+                        before = u;
+                        tc_fence_after();
+                        const uint32_t qd = q_lo + (uint32_t)(u * (Cfg::kTileBytes >> 4)), kd = k_lo + stage * (uint32_t)(Cfg::kTileBytes >> 4);
+#pragma unroll
+                        for (int kk = 0; kk < D / 16; ++kk) {
+                            const uint32_t off = (uint32_t)((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
+                            mma_ss_warp(leader, tm, qd + off, kd + off, hi, idesc, kk > 0 ? 1u : 0u);
+                        }
+                        tc_commit_warp(leader, bar(Cfg::kSFull + u));
+                    }
+                    if (++stage == (uint32_t)Cfg::kStagesK) { stage = 0; ring_phase ^= 1u; }
+                }
+            } else {
+                constexpr uint32_t idesc = make_idesc_bf16(128, D, true);
+                const uint32_t v_lo = smem_desc_lo(sV, 16384);   // MN-major: 64-column panels 16 KB apart, groups of 8 keys 1 KB
+                for (int j = 0; j < T && alive; ++j) {
+                    wait(bar(Cfg::kVFull) + 8u * stage, ring_phase, kStatusWaitKvFull);
+                    if constexpr (!E4M3) {
+                        int x0, lo, hi_row;
+                        w.at(w.j0 + j, x0, lo, hi_row);
+                        if (alive && (x0 < lo || x0 + kPtTile > hi_row)) {      // rows outside the range: zeros
+                            const uint32_t base = sV + stage * Cfg::kTileBytes + (uint32_t)(lane & 7) * 16u;
+                            for (int r = lane >> 3; r < kPtTile; r += 4)
+                                if (x0 + r < lo || x0 + r >= hi_row)
+#pragma unroll
+                                    for (int h = 0; h < Cfg::kHalves; ++h) pt_st_shared4(base + h * 16384 + r * 128, 0u, 0u, 0u, 0u);
+                            fence_proxy_async();
+                            __syncwarp();
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        if (u == 1 && nh == 1) break;
+                        wait(bar(Cfg::kPFull + u), u ? phase1 : phase0, kStatusWaitPFull);
+                        if (u) phase1 ^= 1u; else phase0 ^= 1u;
+                        if (!alive) break;
+                        tc_fence_after();
+                        const uint32_t vd = v_lo + stage * (uint32_t)(Cfg::kTileBytes >> 4);
+#pragma unroll
+                        for (int kk = 0; kk < kPtTile / 16; ++kk)
+                            mma_ts_warp(leader, tm + 256u + u * 128u, tm + 128u + u * 64u + kk * 8u, vd + (uint32_t)((kk * 2048) >> 4), hi, idesc, (j > 0 || kk > 0) ? 1u : 0u);
+                        tc_commit_warp(leader, bar(Cfg::kPvDone + u));
+                    }
+                    if (++stage == (uint32_t)Cfg::kStagesV) { stage = 0; ring_phase ^= 1u; }
+                }
+            }
+            // drain the tensor pipe before TMEM is released
+            const uint32_t drain = bar(Cfg::kDrain + (warp == 9 ? 0 : 1));
+            tc_commit_warp(leader, drain);
+            bounded_wait(drain, 0, abort_addr + 4, a.status, kStatusWaitOFull);
+        }
+        if (a.nsplit > 1) { __syncwarp(); cluster_arrive(); cluster_wait(); cluster_arrive(); cluster_wait(); }
+    } else {
+        setmaxnreg_inc<Cfg::kRegsSoftmax>();
+        // =============================== softmax warpgroups =========================
+        const int u = warp >> 2;
+        const int row = tid & 127;
+        const uint32_t lane_sel = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t tS = tmem + lane_sel;                                   // the score slot
+        const uint32_t tP = tmem + lane_sel + 128u + (uint32_t)(u * 64);
+        const uint32_t tO = tmem + lane_sel + 256u + (uint32_t)(u * 128);
+        const int tokens = min(per, t.n - u * per);                            // of this query tile (0 or less: none)
+        float m_used = -INFINITY, l_run = 0.f;
+        const int nrow = max(tokens, 0) * a.G;
+        const int r_in = min(row, max(nrow - 1, 0));                           // rows past the last mimic it; never stored
+        const int x = t.x0 + u * per + r_in / a.G;
+        const int head = hk * a.G + r_in % a.G;
+        const bool valid = row < nrow;
+        bool alive = true;
+        if (u < nh) {
+            // ---- Q: this thread's row, K-major with 128-byte swizzle ----
+            {
+                const uint16_t* q = a.q + paged_row(a, t, x) * a.q_st + head * a.q_sh;
+                const uint32_t d = sQ + u * Cfg::kTileBytes + row * 128;
+                uint4 y[D / 8];
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) y[c] = __ldcg(reinterpret_cast<const uint4*>(q + c * 8));
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) pt_st_shared4(d + (c >> 3) * 16384 + (((c & 7) ^ (row & 7)) << 4), y[c].x, y[c].y, y[c].z, y[c].w);
+                fence_proxy_async();
+                mbar_arrive(bar(Cfg::kQFull + u));
+            }
+            const PagedView see = paged_view(a, t.summ, x);
+            const float scale_log2 = a.scale_log2;
+            uint32_t sf_phase = 0, pv_phase = 0;
+            int rel_k = 0, rel_v = 0;                        // the stages handed back next, by the last query tile's first thread
+            const bool releaser = (tid & 127) == 0 && u == nh - 1;
+            auto release_k = [&]() { mbar_arrive_relaxed(bar(Cfg::kKEmpty + rel_k)); if (++rel_k == Cfg::kStagesK) rel_k = 0; };
+            auto release_v = [&]() { mbar_arrive_relaxed(bar(Cfg::kVEmpty + rel_v)); if (++rel_v == Cfg::kStagesV) rel_v = 0; };
+            bool s_ok = false;                               // the scores of this tile are known to be there
+            for (int j = 0; j < T; ++j) {
+                bool ok;
+                if (!__all_sync(0xffffffffu, s_ok)) {
+                    ok = bounded_wait(bar(Cfg::kSFull + u), sf_phase, abort_addr, a.status, kStatusWaitSFull);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) { alive = false; break; }
+                }
+                sf_phase ^= 1u;
+                tc_fence_after();
+                uint32_t s[128];
+                {
+                    uint32_t (&c0)[32] = *reinterpret_cast<uint32_t (*)[32]>(&s[0]);
+                    uint32_t (&c1)[32] = *reinterpret_cast<uint32_t (*)[32]>(&s[32]);
+                    uint32_t (&c2)[32] = *reinterpret_cast<uint32_t (*)[32]>(&s[64]);
+                    uint32_t (&c3)[32] = *reinterpret_cast<uint32_t (*)[32]>(&s[96]);
+                    tmem_ld32(tS + 0, c0); tmem_ld32(tS + 32, c1); tmem_ld32(tS + 64, c2); tmem_ld32(tS + 96, c3);
+                }
+                if (releaser) release_k();                   // both query tiles' products with K(j) are done
+                tc_wait_ld();
+                // the scores are in registers: the slot may take the next ones
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_relaxed(bar(Cfg::kLoaded + u));
+                // the row's own range, where the tile holds an end of some row's
+                int x0, lo, hi;
+                const bool summ = w.at(w.j0 + j, x0, lo, hi);
+                const int ca = (summ ? see.s_lo : see.t_lo) - x0, cb = (summ ? see.s_hi : see.t_hi) - x0;    // visible columns
+                if (__any_sync(0xffffffffu, ca > 0 || cb < kPtTile)) {
+                    const uint32_t width = (uint32_t)max(cb - ca, 0);
+#pragma unroll
+                    for (int c = 0; c < 128; ++c)
+                        if ((uint32_t)(c - ca) >= width) s[c] = 0xff800000u;   // -inf
+                }
+                // row maximum, two new scores per instruction
+                float mx0 = fmax3(__uint_as_float(s[0]), __uint_as_float(s[1]), __uint_as_float(s[2]));
+                float mx1 = fmax3(__uint_as_float(s[3]), __uint_as_float(s[4]), __uint_as_float(s[5]));
+                float mx2 = fmax3(__uint_as_float(s[6]), __uint_as_float(s[7]), __uint_as_float(s[8]));
+                float mx3 = fmax3(__uint_as_float(s[9]), __uint_as_float(s[10]), __uint_as_float(s[11]));
+#pragma unroll
+                for (int c = 12; c < 124; c += 8) {
+                    mx0 = fmax3(mx0, __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
+                    mx1 = fmax3(mx1, __uint_as_float(s[c + 2]), __uint_as_float(s[c + 3]));
+                    mx2 = fmax3(mx2, __uint_as_float(s[c + 4]), __uint_as_float(s[c + 5]));
+                    mx3 = fmax3(mx3, __uint_as_float(s[c + 6]), __uint_as_float(s[c + 7]));
+                }
+                mx0 = fmax3(mx0, __uint_as_float(s[124]), __uint_as_float(s[125]));
+                mx1 = fmax3(mx1, __uint_as_float(s[126]), __uint_as_float(s[127]));
+                const float mx_sc = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * scale_log2;
+                // lazy rescale: the reference max only moves when some row of the warp outgrew it
+                const bool need_any = __any_sync(0xffffffffu, mx_sc > m_used + kPtRescale);
+                float alpha = 1.f;
+                if (need_any) {
+                    const float m_new = fmaxf(m_used, mx_sc);
+                    alpha = (m_new == -INFINITY) ? 1.f : ex2_approx(m_used - m_new);
+                    m_used = m_new;
+                    l_run *= alpha;
+                }
+                const float neg_m = (m_used == -INFINITY) ? 0.f : -m_used;
+                const float2 sc2 = make_float2(scale_log2, scale_log2);
+                const float2 nm2 = make_float2(neg_m, neg_m);
+                bool pv_ok = false;                           // the product before is known to be done
+                float2 la = make_float2(0.f, 0.f), lb = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int q = 0; q < 64; ++q) {
+                    const float2 z = ffma2(make_float2(__uint_as_float(s[2 * q]), __uint_as_float(s[2 * q + 1])), sc2, nm2);
+                    float2 pr;
+                    pr.x = ex2_approx(z.x); pr.y = ex2_approx(z.y);
+                    if (q & 1) lb = fadd2(lb, pr); else la = fadd2(la, pr);
+                    if (q == 48 && j > 0) pv_ok = mbar_test_wait(bar(Cfg::kPvDone + u), pv_phase);
+                    s[q] = pack_bf16x2(pr.x, pr.y);
+                }
+                l_run += (la.x + la.y) + (lb.x + lb.y);
+                if (j > 0) {
+                    // O_u += P_u V(j-1) has read P_u and written O_u
+                    if (!__all_sync(0xffffffffu, pv_ok)) {
+                        ok = bounded_wait(bar(Cfg::kPvDone + u), pv_phase, abort_addr, a.status, kStatusWaitPvDone);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) { alive = false; break; }
+                    }
+                    pv_phase ^= 1u;
+                    if (releaser) release_v();               // V(j-1)
+                    tc_fence_after();
+                }
+                s_ok = j + 1 < T && mbar_test_wait(bar(Cfg::kSFull + u), sf_phase);
+                {
+                    uint32_t (&p0)[32] = *reinterpret_cast<uint32_t (*)[32]>(&s[0]);
+                    uint32_t (&p1)[32] = *reinterpret_cast<uint32_t (*)[32]>(&s[32]);
+                    tmem_st32(tP + 0, p0); tmem_st32(tP + 32, p1);
+                }
+                if (need_any && j > 0) {
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c) {
+                        uint32_t o[32];
+                        tmem_ld32(tO + c * 32, o);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                        tmem_st32(tO + c * 32, o);
+                    }
+                }
+                tc_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_relaxed(bar(Cfg::kPFull + u));
+            }
+            if (alive) {
+                const bool ok = bounded_wait(bar(Cfg::kPvDone + u), pv_phase, abort_addr, a.status, kStatusWaitOFull);
+                alive = __all_sync(0xffffffffu, ok);
+                tc_fence_after();
+            }
+        }
+        if (a.nsplit == 1) {
+            // ---- epilogue: O / l -> bf16 at the row's place, LSE ----
+            if (u < nh && alive) {
+                const float inv_l = 1.f / l_run;
+                const int64_t prow = paged_row(a, t, x);
+                const bool store = valid && ksa_in_bounds(prow >= 0 && prow < a.rows && head < a.Hq, a.status);
+                // a row stands in one lane: four lanes exchange 64 bytes of their rows, so that a store touches 8 lines, not 32
+                const int64_t off = store ? prow * a.o_st + (int64_t)head * a.o_sh : -1;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t o[32];
+                    tmem_ld32(tO + c * 32, o);
+                    tc_wait_ld();
+                    uint4 pk[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        pk[e].x = pack_bf16x2(__uint_as_float(o[8 * e]) * inv_l, __uint_as_float(o[8 * e + 1]) * inv_l);
+                        pk[e].y = pack_bf16x2(__uint_as_float(o[8 * e + 2]) * inv_l, __uint_as_float(o[8 * e + 3]) * inv_l);
+                        pk[e].z = pack_bf16x2(__uint_as_float(o[8 * e + 4]) * inv_l, __uint_as_float(o[8 * e + 5]) * inv_l);
+                        pk[e].w = pack_bf16x2(__uint_as_float(o[8 * e + 6]) * inv_l, __uint_as_float(o[8 * e + 7]) * inv_l);
+                    }
+                    quad_transpose(pk, lane);                             // pk[e]: 16 bytes of the group's row e
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int64_t at = __shfl_sync(0xffffffffu, off, (lane & 28) + e);
+                        if (at >= 0) *reinterpret_cast<uint4*>(a.out + at + c * 32 + (lane & 3) * 8) = pk[e];
+                    }
+                }
+                if (store) a.lse[(int64_t)head * a.rows + prow] = (m_used + log2f(l_run)) * 0.6931471805599453f;
+                tc_fence_before();
+            }
+        } else {
+            // ---- partial results into shared memory, summed up over the cluster, a share of the rows by each CTA ----
+            pt_named_barrier(1, 256);                         // both query tiles' products have read their K, V and Q
+            const uint32_t part_o = smem_base, part_ml = smem_base + Cfg::kPartMl;
+            if (tokens > 0) {
+                const uint32_t d = part_o + (uint32_t)((u * 128 + row) * D * 4);
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t o[32];
+                    if (u < nh) { tmem_ld32(tO + c * 32, o); tc_wait_ld(); }
+                    else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = 0u;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)               // (neighbouring rows on different banks)
+                        pt_st_shared4(d + (uint32_t)((c * 8 + (e ^ (row & 7))) * 16), o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                }
+                asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(part_ml + (u * 128 + row) * 8), "f"(m_used), "f"(l_run) : "memory");
+                tc_fence_before();
+            }
+            __syncwarp();
+            cluster_arrive(); cluster_wait();
+            // D / 4 lanes a row
+            constexpr int kLanes = D / 4, kRowsPass = 256 / kLanes;
+            const int total = t.n * a.G, c4 = tid % kLanes;
+            for (int i = split * kRowsPass + tid / kLanes; i < total; i += kRowsPass * a.nsplit) {
+                const int tok = i / a.G, hh = hk * a.G + i - tok * a.G;
+                const int pr = tok < per ? i : 128 + i - per * a.G;          // row of the partial results
+                const uint32_t at = part_o + (uint32_t)(pr * D * 4 + ((c4 & ~7) + ((c4 & 7) ^ (pr & 7))) * 16);
+                float2 ml[kPtMaxSplit];
+                float4 v[kPtMaxSplit];
+#pragma unroll
+                for (int s = 0; s < kPtMaxSplit; ++s)
+                    if (s < a.nsplit) {
+                        ml[s] = pt_ld_cluster2(mapa_shared(part_ml + pr * 8, s));
+                        v[s] = pt_ld_cluster4(mapa_shared(at, s));
+                    }
+                float M = -INFINITY, L = 0.f;
+#pragma unroll
+                for (int s = 0; s < kPtMaxSplit; ++s) if (s < a.nsplit) M = fmaxf(M, ml[s].x);
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int s = 0; s < kPtMaxSplit; ++s)
+                    if (s < a.nsplit) {
+                        const float f = (ml[s].x == -INFINITY) ? 0.f : ex2_approx(ml[s].x - M);
+                        L += ml[s].y * f;
+                        acc.x += v[s].x * f; acc.y += v[s].y * f; acc.z += v[s].z * f; acc.w += v[s].w * f;
+                    }
+                const float inv = 1.f / L;
+                const int64_t prow = paged_row(a, t, t.x0 + tok);
+                if (!ksa_in_bounds(prow >= 0 && prow < a.rows && hh < a.Hq, a.status)) continue;
+                *reinterpret_cast<uint2*>(a.out + prow * a.o_st + (int64_t)hh * a.o_sh + c4 * 4) =
+                    make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+                if (c4 == 0) a.lse[(int64_t)hh * a.rows + prow] = (M + log2f(L)) * 0.6931471805599453f;
+            }
+            __syncwarp();
+            cluster_arrive(); cluster_wait();                 // no CTA leaves while another reads its results
+        }
+    }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) tmem_dealloc(tmem, 512);
+}
+
+template <int D, bool E4M3>
+static cudaError_t setup_one()
+{
+    return cudaFuncSetAttribute(ksa_paged_tc_kernel<D, E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, PtCfg<D, E4M3>::kSmemBytes);
+}
+cudaError_t setup_paged_tc()
+{
+    for (cudaError_t e : {setup_one<128, false>(), setup_one<128, true>(), setup_one<64, false>(), setup_one<64, true>()})
+        if (e != cudaSuccess) return e;
+    return cudaSuccess;
+}
+
+static bool encode_pages(PagedEncode encode, CUtensorMap* map, void* base, const PagedArgs& a, bool e4m3)
+{
+    const int rows = 1 << a.page_shift;
+    const cuuint64_t dims[4] = {(cuuint64_t)a.D, (cuuint64_t)rows, (cuuint64_t)a.Hkv, (cuuint64_t)a.num_pages};
+    auto stride = [](int64_t st) { return (cuuint64_t)(st > 0 ? st : 16); };            // (0: a dimension of one)
+    const cuuint64_t strides[3] = {stride(a.row_st), stride(a.head_st), stride(a.page_st)};
+    const cuuint32_t box[4] = {(cuuint32_t)(e4m3 ? a.D : 64), (cuuint32_t)rows, 1, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return encode(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base, dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, e4m3 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+cudaError_t launch_paged_tc(const PagedArgs& args, bool e4m3, int num_sms, PagedEncode encode, cudaStream_t stream)
+{
+    PagedArgs a = args;
+    a.tokens_per_tile = 2 * (kPtTile / a.G);                  // of a CTA: two query tiles
+    a.head_blocks = 1;
+    const int64_t most = (int64_t)a.rows / a.tokens_per_tile + (int64_t)a.B * (a.m > 0 ? 2 : 1);
+    const int64_t units = (most < a.rows ? most : a.rows) * a.Hkv;
+    const int64_t key_tiles = (((int64_t)a.text_cols + (a.m > 0 ? a.summ_cols : 0)) << a.page_shift) / kPtTile;    // of a sequence, at most
+    a.nsplit = 1;
+    while (a.nsplit < kPtMaxSplit && units * a.nsplit * 2 <= num_sms && key_tiles >= 4 * a.nsplit) a.nsplit *= 2;
+    PagedMaps maps;
+    if (!encode_pages(encode, &maps.k, a.kp, a, e4m3) || !encode_pages(encode, &maps.v, a.vp, a, e4m3)) return cudaErrorInvalidValue;
+    cudaLaunchAttribute attr[2]{};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)a.nsplit; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(units * a.nsplit)); cfg.stream = stream;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    auto go = [&](auto kernel, int threads, int smem) {
+        cfg.blockDim = dim3((unsigned)threads);
+        cfg.dynamicSmemBytes = (size_t)smem;
+        return cudaLaunchKernelEx(&cfg, kernel, a, maps);
+    };
+    if (a.D == 128) {
+        if (e4m3) return go(ksa_paged_tc_kernel<128, true>, PtCfg<128, true>::kThreads, PtCfg<128, true>::kSmemBytes);
+        return go(ksa_paged_tc_kernel<128, false>, PtCfg<128, false>::kThreads, PtCfg<128, false>::kSmemBytes);
+    }
+    if (e4m3) return go(ksa_paged_tc_kernel<64, true>, PtCfg<64, true>::kThreads, PtCfg<64, true>::kSmemBytes);
+    return go(ksa_paged_tc_kernel<64, false>, PtCfg<64, false>::kThreads, PtCfg<64, false>::kSmemBytes);
+}
+
+}  // namespace ksa
