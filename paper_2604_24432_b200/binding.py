@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from itertools import accumulate
 from typing import Optional, Sequence
@@ -159,10 +160,9 @@ def lib():
     L.ksa_cache_fill_from_prefill.argtypes = [vp, vp, vp, vp, vp, vp, pp, cp, vp]
     L.ksa_decode_text.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, cp, vp]
     L.ksa_decode_summary.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, cp, vp]
-    gp, gk = ctypes.POINTER(ksa_paged_params), ctypes.POINTER(ksa_paged_kv)
-    L.ksa_paged_append.argtypes = [vp, gk, vp, vp, gp, vp]
-    L.ksa_paged_gather.argtypes = [vp, gk, vp, vp, gp, vp]
-    L.ksa_paged_attn.argtypes = [vp, gk, vp, vp, vp, gp, vp]
+    L.ksa_paged_append.argtypes = [vp, vp, vp, vp, vp, vp]      # (structures: by reference, or packed as bytes)
+    L.ksa_paged_gather.argtypes = [vp, vp, vp, vp, vp, vp]
+    L.ksa_paged_attn.argtypes = [vp, vp, vp, vp, vp, vp, vp]
     L.ksa_strerror.restype = ctypes.c_char_p
     L.ksa_strerror.argtypes = [ctypes.c_int]
     _lib = L
@@ -552,7 +552,7 @@ class DecodeCache:
         self._step(lib().ksa_decode_summary, "ksa_decode_summary", q, k_new, v_new, out, lse, stream)
 
 
-@dataclass
+@dataclass(frozen=True)
 class PagedSpec:
     """Python-side holder of what a ``ksa_paged_params`` says of the cache (fmt: "bf16" or "e4m3")."""
     k: int
@@ -568,11 +568,11 @@ class PagedSpec:
     flags: int = 0
 
 
-@dataclass
+@dataclass(frozen=True)
 class PagedBatch:
     """The sequences of a call (int32 CUDA tensors, see include/ksa_paged.h): rows cached before it [B], the calls' packed
     rows [B + 1], and the page tables [B, columns] of text and summaries (summ_table may be None where m == 0).  The tensors
-    are read on the device at every call (and every replay of a captured one)."""
+    are read on the device at every call (and every replay of a captured one); write into them for new lengths."""
     cached: "torch.Tensor"
     cu_rows: "torch.Tensor"
     text_table: "torch.Tensor"
@@ -589,6 +589,11 @@ class PagedBatch:
             _expect(t.dtype == torch.int32 and t.is_contiguous() and t.device == self.cached.device, name + " must be contiguous int32, all on one device")
             if name.endswith("table"):
                 _expect(t.dim() == 2 and t.shape[0] == B, name + " must be [B, columns]")
+        # what every call passes of the batch
+        summ = self.summ_table
+        for name, value in (("_size", B), ("_index", self.cached.get_device()), ("_cols", (self.text_table.shape[1], 0 if summ is None else summ.shape[1])),
+                            ("_ptrs", (self.text_table.data_ptr(), 0 if summ is None else summ.data_ptr(), self.cached.data_ptr(), self.cu_rows.data_ptr()))):
+            object.__setattr__(self, name, value)
 
 
 def _expect(ok: bool, what: str):
@@ -604,7 +609,7 @@ class PagedCache:
 
     def __init__(self, ctx: "Context", spec: PagedSpec, kpages=None, vpages=None, kscale=None, vscale=None):
         import torch
-        self.ctx, self.spec = ctx, spec
+        self.ctx, self._spec = ctx, spec
         self.device = torch.device("cuda", ctx.device)
         _expect(spec.fmt in ("bf16", "e4m3"), "fmt must be \"bf16\" or \"e4m3\"")
         quantised = spec.fmt == "e4m3"
@@ -621,54 +626,58 @@ class PagedCache:
             _expect(t.stride() == kpages.stride() and t.stride(3) == 1, "K and V pools must have the same strides, head_dim contiguous")
         for t in (kscale, vscale) if quantised else ():
             _expect(tuple(t.shape) == shape[:3] and t.dtype == torch.uint8 and t.device == self.device and t.is_contiguous(), "scales must be contiguous uint8 %s on %s" % (shape[:3], self.device))
-        self.kpages, self.vpages, self.kscale, self.vscale = kpages, vpages, kscale, vscale
+        self._tensors = (kpages, vpages, kscale, vscale)
+        self._marshal()
 
-    def _args(self, batch: PagedBatch, rows: int, q, k, v, o):
-        s = self.spec
-        _expect(batch.cached.device == self.device, "the batch must be on " + str(self.device))
-        _expect(batch.summ_table is not None or s.m == 0, "summ_table is missing")
+    # (read-only: what a call passes of them is worked out once)
+    spec = property(lambda self: self._spec)
+    kpages, vpages, kscale, vscale = (property(lambda self, i=i: self._tensors[i]) for i in range(4))
 
-        def strides(t, H):
-            if t is None:
-                return H * s.D, s.D
-            _expect(tuple(t.shape) == (rows, H, s.D) and t.dtype == self._bf16() and t.device == self.device and t.stride(2) == 1,
-                    "rows must be bf16 [num_rows, heads, head_dim] on %s, head_dim contiguous" % self.device)
-            return t.stride(0) if rows > 1 else H * s.D, t.stride(1) if H > 1 else s.D
-        p = ksa_paged_params(_PAGED_SIZE, batch.cached.numel(), rows, s.k, s.m, s.C, s.Hq, s.Hkv, s.D, s.scale, s.flags,
-                             KSA_KV_E4M3 if s.fmt == "e4m3" else KSA_KV_BF16, s.page_rows, s.num_pages, batch.text_table.shape[1],
-                             0 if batch.summ_table is None else batch.summ_table.shape[1], *self.kpages.stride()[:3],
-                             *strides(q, s.Hq), *strides(k, s.Hkv), *strides(v, s.Hkv), *strides(o, s.Hq))
-        ptr = lambda t: None if t is None else t.data_ptr()
-        return ksa_paged_kv(self.kpages.data_ptr(), self.vpages.data_ptr(), ptr(self.kscale), ptr(self.vscale), batch.text_table.data_ptr(),
-                            ptr(batch.summ_table), batch.cached.data_ptr(), batch.cu_rows.data_ptr()), p
-
-    @staticmethod
-    def _bf16():
+    def _marshal(self):
+        """What every call passes of the cache."""
         import torch
-        return torch.bfloat16
+        s = self.spec
+        self._bf16, self._f32, self._index = torch.bfloat16, torch.float32, self.kpages.get_device()
+        self._fixed = (s.k, s.m, s.C, s.Hq, s.Hkv, s.D, s.scale, s.flags, KSA_KV_E4M3 if s.fmt == "e4m3" else KSA_KV_BF16, s.page_rows, s.num_pages)
+        self._strides = self.kpages.stride()[:3]
+        self._pools = tuple(0 if t is None else t.data_ptr() for t in self._tensors)
 
-    def _stream(self, stream):
-        return _current_stream(self.device) if stream is None else stream
+    def _rows(self, t, rows: int, H: int):
+        """Strides of a tensor of rows, checked."""
+        D = self._spec.D
+        st = t.stride()
+        if t.shape != (rows, H, D) or t.dtype is not self._bf16 or t.get_device() != self._index or st[2] != 1:
+            raise ValueError("rows must be bf16 [num_rows, heads, head_dim] = %s on cuda:%d, head_dim contiguous" % ((rows, H, D), self._index))
+        return st[0] if rows > 1 else H * D, st[1] if H > 1 else D
+
+    def _call(self, fn, name: str, batch: PagedBatch, rows: int, q, k, v, o, stream, *tensors):
+        # (Both structures are packed as bytes: this runs in every call, and a call of one token takes the device some 6 us.)
+        if batch._index != self._index or (batch._cols[1] == 0 and self.spec.m > 0):
+            raise ValueError("the batch must be on cuda:%d, with a summ_table" % self._index)
+        p = _PAGED_PARAMS.pack(_PAGED_PARAMS.size, batch._size, rows, *self._fixed, *batch._cols, *self._strides, *q, *k, *v, *o)
+        _check(fn(self.ctx.handle, _PAGED_KV.pack(*self._pools, *batch._ptrs), *tensors, p, _current_stream(self.device) if stream is None else stream), name)
 
     def append(self, batch: PagedBatch, k, v, stream: Optional[int] = None):
         """ksa_paged_append: k, v [num_rows, Hkv, D] of the batch's new rows into their pages (quantised on the way)."""
-        kv, p = self._args(batch, k.shape[0], None, k, v, None)
-        _check(lib().ksa_paged_append(self.ctx.handle, ctypes.byref(kv), k.data_ptr(), v.data_ptr(), ctypes.byref(p), self._stream(stream)),
-               "ksa_paged_append")
+        rows, H = k.shape[0], self.spec.Hkv
+        self._call(lib().ksa_paged_append, "ksa_paged_append", batch, rows, _NO_ROWS, self._rows(k, rows, H), self._rows(v, rows, H), _NO_ROWS, stream,
+                   k.data_ptr(), v.data_ptr())
 
     def gather(self, batch: PagedBatch, k, v, stream: Optional[int] = None):
         """ksa_paged_gather: the rows cached[b] .. of every sequence back into k, v [num_rows, Hkv, D]."""
-        kv, p = self._args(batch, k.shape[0], None, k, v, None)
-        _check(lib().ksa_paged_gather(self.ctx.handle, ctypes.byref(kv), k.data_ptr(), v.data_ptr(), ctypes.byref(p), self._stream(stream)),
-               "ksa_paged_gather")
+        rows, H = k.shape[0], self.spec.Hkv
+        self._call(lib().ksa_paged_gather, "ksa_paged_gather", batch, rows, _NO_ROWS, self._rows(k, rows, H), self._rows(v, rows, H), _NO_ROWS, stream,
+                   k.data_ptr(), v.data_ptr())
 
     def attn(self, batch: PagedBatch, q, out, lse, stream: Optional[int] = None):
         """ksa_paged_attn: q, out [num_rows, Hq, D], lse fp32 [Hq, num_rows]; the rows' own K and V have been appended."""
-        kv, p = self._args(batch, q.shape[0], q, None, None, out)
-        _expect(tuple(lse.shape) == (self.spec.Hq, q.shape[0]) and lse.is_contiguous() and lse.element_size() == 4 and lse.is_floating_point() and lse.device == self.device,
-                "lse must be contiguous fp32 [heads, num_rows]")
-        _check(lib().ksa_paged_attn(self.ctx.handle, ctypes.byref(kv), q.data_ptr(), out.data_ptr(), lse.data_ptr(), ctypes.byref(p),
-                                    self._stream(stream)), "ksa_paged_attn")
+        rows, H = q.shape[0], self.spec.Hq
+        if lse.shape != (H, rows) or lse.dtype is not self._f32 or lse.get_device() != self._index or not lse.is_contiguous():
+            raise ValueError("lse must be contiguous fp32 [heads, num_rows] = %s on cuda:%d" % ((H, rows), self._index))
+        self._call(lib().ksa_paged_attn, "ksa_paged_attn", batch, rows, self._rows(q, rows, H), _NO_ROWS, _NO_ROWS, self._rows(out, rows, H), stream,
+                   q.data_ptr(), out.data_ptr(), lse.data_ptr())
 
 
-_PAGED_SIZE = ctypes.sizeof(ksa_paged_params)
+_PAGED_PARAMS = struct.Struct("@9i f I 5i 11q")      # ksa_paged_params
+_PAGED_KV = struct.Struct("@8N")                     # ksa_paged_kv
+_NO_ROWS = (0, 0)                                    # strides of a tensor that a call does not take

@@ -304,6 +304,6 @@ KSA_API int ksa_paged_attn(ksa_ctx* ctx, const ksa_paged_kv* kv, const void* q, 
         }
         if ((int64_t)a.rows * a.G > 16 * (int64_t)a.B)
             return launch_paged_tc(a, p->kv_format == KSA_KV_E4M3, ksa_ctx_num_sms(ctx), (PagedEncode)ksa_ctx_encode_tiled(ctx), (cudaStream_t)cuda_stream);
-        return launch_paged_attn(a, p->kv_format == KSA_KV_E4M3, ksa_ctx_num_sms(ctx), (cudaStream_t)cuda_stream);
+        return launch_paged_attn(a, p->kv_format == KSA_KV_E4M3, ksa_ctx_num_sms(ctx), (PagedEncode)ksa_ctx_encode_tiled(ctx), (cudaStream_t)cuda_stream);
     });
 }

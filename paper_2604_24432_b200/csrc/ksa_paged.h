@@ -26,11 +26,13 @@ struct PagedArgs {
 
 cudaError_t launch_paged_append(const PagedArgs& a, bool e4m3, cudaStream_t stream);
 cudaError_t launch_paged_gather(const PagedArgs& a, bool e4m3, cudaStream_t stream);
-cudaError_t launch_paged_attn(const PagedArgs& a, bool e4m3, int num_sms, cudaStream_t stream);
-cudaError_t setup_paged_attn();
-// The same on tcgen05, for tiles of more than 16 query rows.
 typedef CUresult (*PagedEncode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+// Map of a page pool, [D, page rows, KV heads, pages] with a box of box_rows rows of box_bytes bytes of one page and head.
+bool encode_pages(PagedEncode encode, CUtensorMap* map, void* base, const PagedArgs& a, bool e4m3, int box_bytes, int box_rows, CUtensorMapSwizzle swizzle);
+// Tiles of up to 16 query rows (mma.sync), and of up to 256 (tcgen05).
+cudaError_t launch_paged_attn(const PagedArgs& a, bool e4m3, int num_sms, PagedEncode encode, cudaStream_t stream);
+cudaError_t setup_paged_attn();
 cudaError_t launch_paged_tc(const PagedArgs& a, bool e4m3, int num_sms, PagedEncode encode, cudaStream_t stream);
 cudaError_t setup_paged_tc();
 
@@ -61,7 +63,8 @@ __device__ __forceinline__ int paged_page(const PagedArgs& a, int b, bool summ, 
 
 // ---- query tiles ------------------------------------------------------------------------------------------------------
 // Tile `item` of the call, counted through the sequences (text tiles of a sequence before its summary tiles).  Executed by a
-// whole warp: 32 sequences at a time.
+// whole warp: 32 sequences at a time.  kLongestFirst: these in descending order of what their last row sees.
+template <bool kLongestFirst = false>
 __device__ __forceinline__ PagedTile paged_tile(const PagedArgs& a, int item)
 {
     const int lane = threadIdx.x & 31, per = a.tokens_per_tile;
@@ -78,6 +81,26 @@ __device__ __forceinline__ PagedTile paged_tile(const PagedArgs& a, int item)
             tt = (nt + per - 1) / per;
             ts = (n - nt + per - 1) / per;
         }
+        int seq = base + lane;
+        if constexpr (kLongestFirst) {
+            if (a.B > 1) {
+                // a lane's place among the 32, by the keys in view (as a number, ties by lane), then everything to its place
+                const PagedView w = paged_view(a, nt == 0, nt > 0 ? t0 + nt - 1 : max(first + n - t0 - 1, 0));
+                const int keys = n > 0 ? w.t_hi - w.t_lo + w.s_hi - w.s_lo : -1;
+                int place = 0;
+#pragma unroll
+                for (int o = 0; o < 32; ++o) {
+                    const int other = __shfl_sync(0xffffffffu, keys, o);
+                    place += other > keys || (other == keys && o < lane);
+                }
+                int from = 0;
+#pragma unroll
+                for (int o = 0; o < 32; ++o) if (__shfl_sync(0xffffffffu, place, o) == lane) from = o;
+                seq = base + from;
+                row0 = __shfl_sync(0xffffffffu, row0, from); n = __shfl_sync(0xffffffffu, n, from); first = __shfl_sync(0xffffffffu, first, from);
+                t0 = __shfl_sync(0xffffffffu, t0, from); nt = __shfl_sync(0xffffffffu, nt, from); tt = __shfl_sync(0xffffffffu, tt, from); ts = __shfl_sync(0xffffffffu, ts, from);
+            }
+        }
         int sum = tt + ts;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -90,7 +113,7 @@ __device__ __forceinline__ PagedTile paged_tile(const PagedArgs& a, int item)
             int i = item - __shfl_sync(0xffffffffu, sum - tt - ts, src);
             tt = __shfl_sync(0xffffffffu, tt, src); nt = __shfl_sync(0xffffffffu, nt, src); t0 = __shfl_sync(0xffffffffu, t0, src);
             n = __shfl_sync(0xffffffffu, n, src);
-            t.b = base + src;
+            t.b = __shfl_sync(0xffffffffu, seq, src);
             t.row0 = __shfl_sync(0xffffffffu, row0, src);
             t.first = __shfl_sync(0xffffffffu, first, src);
             t.summ = i >= tt;
@@ -111,6 +134,26 @@ __device__ __forceinline__ float e8m0_scale(uint32_t e)
 {
     return __uint_as_float(e == 255u ? 0x7fc00000u : e == 0u ? 0x00400000u : e << 23);
 }
+// Four e4m3 values as f16, exact: bytes 0, 1 and bytes 2, 3
+__device__ __forceinline__ void e4m3x4_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi)
+{
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
+}
+// fp32 -> f16x2 (lo in the low half)
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// 2^(e - 127) for the products: 255, whose row is all zeros, as an infinity, which makes NaN of them
+__device__ __forceinline__ float e8m0_factor(uint32_t e) { return __uint_as_float(max(e << 23, 0x00400000u)); }
 // Two e4m3 values (low byte first) as fp32
 __device__ __forceinline__ float2 e4m3x2_to_f32(uint32_t two)
 {

@@ -1,49 +1,73 @@
-// Attention of a run of new rows over the paged KV cache: tiles of up to 16 query rows.
+// Attention of a run of new rows over the paged KV cache: tiles of up to 8 or 16 query rows.
 //
-// A query tile is up to 16 rows of one sequence and KV head, (token, query head of the group) each, so that a token's whole
-// group reads every key once; what the tile sees is one range of summaries and one of text (Eq. 3; a summary: its own chunk).
-// With so few rows the work is bound by the bytes of K and V.  The 64-row key tiles of the two ranges are split over the
-// CTAs of a cluster; a CTA streams its share through a ring of cp.async stages in (swizzled) shared memory, page by page;
-// its four warps take 16 keys of each tile: S = Q K^T and O += P V with mma.sync m16n8k16, running maximum and sum of the
-// softmax in fp32.  Partial results meet in distributed shared memory: each CTA of the cluster sums up its share of the
-// output's elements, so a call is one launch, needs no workspace and adds in a fixed order.
+// A query tile is up to 8 N rows (N = 1 or 2) of one sequence and KV head, (token, query head of the group) each, so that a
+// token's whole group reads every key once; what the tile sees is one range of summaries and one of text (Eq. 3; a summary:
+// its own chunk).  With so few rows the work is bound by the bytes of K and V.  The key tiles of the two ranges are split
+// over the CTAs of a cluster and over each CTA's warps.  A warp has its own ring of stages in shared memory, filled by TMA, a
+// box for each run of 16 rows (the pages' least size) by a lane of its own, and waits for no other warp until the end.
+// Partial results meet in shared memory, those of the CTAs in distributed shared memory, each CTA of the cluster summing up its
+// share of the output's elements: a call is one launch, needs no workspace and adds in a fixed order.
 //
-// e4m3 rows are taken to bf16 in registers on their way into the products: the scale of a key multiplies its
-// scores, that of a value row the probability before it is rounded to bf16.  A key's 16 bytes hold four values for each of four
-// lanes; which of the 16 columns a product calls its k-th does not matter as long as Q agrees, so lane t takes
-// columns 4 t .. 4 t + 3, as they stand, and loads Q the same way.  Of V, ldmatrix.trans hands a lane two neighbouring
-// columns of two keys; they go to two products, one of the even columns and one of the odd ones.
+// The keys are the M rows of the products, S^T = K Q^T and O^T += V^T P^T with mma.sync m16n8k16, so that 8 query rows take
+// half the products, half the registers of O and half of its rescaling that they would as 16 rows of M; P^T gets from the
+// first product's layout to the second's by movmatrix.  Running maximum and sum in fp32.
+//
+// bf16 rows: P rounded to bf16.  e4m3 rows become f16 in registers on their way into the products, one conversion for two
+// values (sm_100 has no mma.sync for e4m3: it is made of conversions to f16 and two f16 products).  So Q becomes f16 too, its
+// row scaled by a power of two, and the scale of a key multiplies its scores.  The scale of a value row goes into the
+// exponent, u = 2^(score + e - 127 - reference) with the reference maximum taken over these sums: u is at most 2^8 and what f16
+// rounds off or loses is relative to the largest that the row has met, whatever the scales are; the softmax's sum takes
+// u 2^(127 - e).  A key's 16 bytes hold four values for each of four lanes; which of the 16 columns a product calls its k-th
+// does not matter as long as Q agrees, so lane t takes columns 4 t .. 4 t + 3 as they stand.  Of V, ldmatrix.trans hands a lane
+// two neighbouring columns of two keys, which become rows r and r + 8 of a product.
 #include <cuda_bf16.h>
 
 #include "ksa_launch.h"
 #include "ksa_paged.h"
 #include "ksa_ptx.cuh"
+#include "ksa_wait.cuh"
 
 namespace ksa {
 
-constexpr int kPgTile = 64;         // cache rows per shared-memory tile
-constexpr int kPgThreads = 128;
-constexpr int kPgMaxSplit = 8;      // the portable cluster size
+constexpr int kPgRun = 16;                      // rows of a box: the pages' least size
+constexpr int kPgMaxSplit = 8;                  // CTAs of a cluster: the portable size
 
-template <int D, bool E4M3>
+struct PgMaps { CUtensorMap k, v; };
+
+template <int D, bool E4M3, int N>
 struct PgCfg {
-    static constexpr int kRowB = E4M3 ? D : D * 2;              // bytes of a row
-    static constexpr int kVec = kRowB / 16;
-    static constexpr int kTileB = kPgTile * kRowB;
-    static constexpr int kScaleB = E4M3 ? 2 * kPgTile : 0;      // scale bytes of K, then V
-    static constexpr int kStageB = 2 * kTileB + kScaleB;
-    static constexpr int kStages = E4M3 ? 4 : 3;
-    static constexpr int kRingB = kStages * kStageB;
-    static constexpr int kMergeB = 4 * 16 * D * 4 + 4 * 16 * 2 * 4 + 16 * D * 4 + 16 * 2 * 4;
-    static constexpr int kSmemBytes = kRingB > kMergeB ? kRingB : kMergeB;
+    static constexpr int kSubs = E4M3 ? 2 : 1;                  // runs in a warp's tile
+    static constexpr int kKeys = kPgRun * kSubs;
+    static constexpr int kWarps = 4, kThreads = 32 * kWarps;
+    static constexpr int kTile = kWarps * kKeys;                // keys of a CTA's tile
+    static constexpr int kRows = 8 * N;                         // of the query tile
+    static constexpr int kRowB = E4M3 ? D : D * 2;              // bytes of a cached row
+    static constexpr int kPanelB = kRowB < 128 ? kRowB : 128;   // a box's width: 128 bytes at most with a swizzle
+    static constexpr int kPanels = kRowB / kPanelB;
+    static constexpr int kRunB = kPgRun * kRowB;                // of K or of V: its panels, 16 rows each
+    static constexpr int kVOff = kSubs * kRunB, kScaleOff = 2 * kVOff;
+    static constexpr int kStageB = kScaleOff + (E4M3 ? 1024 : 0);       // K, V, scale bytes (run by run 16 of K, 16 of V)
+    static constexpr int kTxBytes = 2 * kVOff + (E4M3 ? 2 * kKeys : 0);
+    static constexpr int kStages = 3;
+    static constexpr int kRingB = kStages * kStageB;            // of a warp
+    // log2 units.  The reference maximum moves when a score outgrows it by this
+    static constexpr float kRescale = 8.0f;
+    static constexpr int kLd = D + 4;                           // floats from one row of partial results to the next
+    static constexpr int kMergeB = (kWarps + 1) * kRows * (kLd + 2) * 4;
+    static constexpr int kBarOff = kWarps * kRingB > kMergeB ? kWarps * kRingB : kMergeB;
+    static constexpr int kSmemBytes = kBarOff + 8 * kWarps * kStages + 16 + 1024;       // + slack for 1024-byte alignment
+    // 16-byte vector c of row r of a run, as the boxes' swizzles place them
+    __device__ static __forceinline__ uint32_t at(int r, int c)
+    {
+        return (uint32_t)((c >> 3) * (kPgRun * 128) + r * kPanelB + (((c & 7) ^ (kPanelB == 64 ? (r >> 1) & 3 : r & 7)) << 4));
+    }
 };
 
-__device__ __forceinline__ void pg_cp16(uint32_t dst, const void* src, bool valid)
+// untiled copy of 16 bytes global -> shared, counted on an mbarrier
+__device__ __forceinline__ void pg_bulk16(uint32_t dst, const void* src, uint32_t bar)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 16, [%2];" ::"r"(dst), "l"(src), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void pg_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void pg_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void pg_ldsm(uint32_t (&r)[4], uint32_t addr)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -54,326 +78,412 @@ __device__ __forceinline__ void pg_ldsm_t(uint32_t (&r)[4], uint32_t addr)
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
-__device__ __forceinline__ void pg_mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+__device__ __forceinline__ uint32_t pg_transpose(uint32_t x)
+{
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ void pg_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint32_t (&b)[2])
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
 }
-// two e4m3 values -> bf16x2
-__device__ __forceinline__ uint32_t pg_two(uint32_t y)
+__device__ __forceinline__ void pg_mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint32_t (&b)[2])
 {
-    const float2 f = e4m3x2_to_f32(y & 0xffffu);
-    return ptx::pack_bf16x2(f.x, f.y);
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
 }
-__device__ __forceinline__ uint32_t pg_ld_u32(uint32_t addr)
+__device__ __forceinline__ uint32_t pg_ld_u8(uint32_t addr)
 {
     uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr));
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr));
     return v;
 }
 __device__ __forceinline__ float2 pg_ld_cluster2(uint32_t addr)
 {
     float2 v;
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr));
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
     return v;
 }
 __device__ __forceinline__ float4 pg_ld_cluster4(uint32_t addr)
 {
     float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
     return v;
 }
 
-template <int D, bool E4M3>
-__global__ void __launch_bounds__(kPgThreads) ksa_paged_attn_kernel(const __grid_constant__ PagedArgs a)
+template <int D, bool E4M3, int N>
+__global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PgMaps maps)
 {
-    using Cfg = PgCfg<D, E4M3>;
-    constexpr int kStages = Cfg::kStages;
-    extern __shared__ __align__(128) uint8_t pgsm[];
+    using Cfg = PgCfg<D, E4M3, N>;
+    constexpr int kStages = Cfg::kStages, kSubs = Cfg::kSubs, kKeys = Cfg::kKeys, kTile = Cfg::kTile, kWarps = Cfg::kWarps, kThreads = Cfg::kThreads;
+    extern __shared__ uint8_t pgsm_raw[];
+    uint8_t* pgsm = pgsm_raw + (-ptx::smem_u32(pgsm_raw) & 1023u);
     const uint32_t sbase = ptx::smem_u32(pgsm);
+    const uint32_t bars = sbase + Cfg::kBarOff, abort_addr = bars + 8 * kWarps * kStages;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kWarps * kStages; ++i) ptx::mbar_init(bars + 8 * i, 1);
+        st_shared_u32(abort_addr, 0u);
+        st_shared_u32(abort_addr + 4, 0u);                     // never raised: lets the last waits run while aborting
+        ptx::fence_mbar_init();
+        ptx::prefetch_tensormap(&maps.k);
+        ptx::prefetch_tensormap(&maps.v);
+    }
+    __syncthreads();
     ptx::pdl_launch_dependents();
     ptx::pdl_wait();
     const int split = (int)blockIdx.x % a.nsplit, unit = (int)blockIdx.x / a.nsplit;
     const int hb = unit % a.head_blocks, hk = unit / a.head_blocks % a.Hkv;
-    const PagedTile t = paged_tile(a, unit / a.head_blocks / a.Hkv);
+    const PagedTile t = paged_tile<true>(a, unit / a.head_blocks / a.Hkv);
     if (t.b < 0) return;                                       // (the whole cluster)
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int g0 = lane >> 2, c2 = (lane & 3) * 2;             // fragment row and column pair
+    const int l4 = lane >> 2, c2 = (lane & 3) * 2;             // fragment row and column pair
     // the tile's rows: (token, head), heads `head0 ..` of the group
-    const int head0 = hk * a.G + hb * 16, heads = min(16, a.G - hb * 16), nrow = t.n * heads;
-    const PagedView see = paged_tile_view(a, t);
-    const int s_t0 = see.s_lo / kPgTile, s_tiles = see.s_hi > see.s_lo ? (see.s_hi + kPgTile - 1) / kPgTile - s_t0 : 0;
-    const int t_t0 = see.t_lo / kPgTile, tiles = s_tiles + (see.t_hi + kPgTile - 1) / kPgTile - t_t0;
+    const int head0 = hk * a.G + hb * Cfg::kRows, heads = min(Cfg::kRows, a.G - hb * Cfg::kRows), nrow = t.n * heads;
+    // what anything in the tile sees; rows that all of it sees: a warp's keys within them need no mask
+    const PagedView see = paged_tile_view(a, t), first = paged_view(a, t.summ, t.x0), last = paged_view(a, t.summ, t.x0 + t.n - 1);
+    const int s_t0 = see.s_lo / kTile, s_tiles = see.s_hi > see.s_lo ? (see.s_hi + kTile - 1) / kTile - s_t0 : 0;
+    const int t_t0 = see.t_lo / kTile, tiles = s_tiles + (see.t_hi + kTile - 1) / kTile - t_t0;
     const int per = (tiles + a.nsplit - 1) / a.nsplit;
     const int my0 = min(tiles, split * per), my1 = min(tiles, my0 + per);
 
-    // Q fragments (A operand, 16 x D); rows past the tile's are zero
-    uint32_t qa[D / 16][4];
-    PagedView v0 = see, v1 = see;                              // what fragment rows g0 and g0 + 8 see
-    {
-        const int r0 = min(g0, nrow - 1), r1 = min(g0 + 8, nrow - 1);
-        const int x0 = t.x0 + r0 / heads, x1 = t.x0 + r1 / heads;
-        v0 = paged_view(a, t.summ, x0);
-        v1 = paged_view(a, t.summ, x1);
-        const uint16_t* q0 = a.q + paged_row(a, t, x0) * a.q_st + (head0 + r0 % heads) * a.q_sh;
-        const uint16_t* q1 = a.q + paged_row(a, t, x1) * a.q_st + (head0 + r1 % heads) * a.q_sh;
-        const bool ok0 = g0 < nrow, ok1 = g0 + 8 < nrow;
+    // First row of the warp's tile j in its stream.
+    auto tile_at = [&](int j, bool& summ) { summ = j < s_tiles; return (summ ? s_t0 + j : t_t0 + j - s_tiles) * kTile + warp * kKeys; };
+    // Lane u < kSubs brings the tile's run u.  Its page-table entry is fetched a tile ahead of its use; -3: nobody sees the rows.
+    auto find_entry = [&](int j) {
+        bool summ;
+        const int x = tile_at(j, summ) + kPgRun * lane, col = x >> a.page_shift, cols = summ ? a.summ_cols : a.text_cols;
+        if (lane >= kSubs || j >= my1 || x >= (summ ? see.s_hi : see.t_hi) || x + kPgRun <= (summ ? see.s_lo : see.t_lo)) return -3;
+        return col < cols ? __ldcg((summ ? a.summ_table : a.text_table) + (int64_t)t.b * cols + col) : -2;
+    };
+    const uint32_t ring = sbase + warp * Cfg::kRingB, full = bars + 8 * warp * kStages;
+    auto load_tile = [&](int j, int stage, int entry) {
+        if (lane == 0) ptx::mbar_arrive_expect_tx(full + 8 * stage, Cfg::kTxBytes);
+        __syncwarp();
+        if (lane < kSubs) {
+            bool summ;
+            const int row = tile_at(j, summ) + kPgRun * lane & ((1 << a.page_shift) - 1);
+            int page = paged_entry(a, entry);
+            if (page < 0) {
+                if (entry != -3) atomicCAS(a.status, 0, KSA_PAGED_STATUS_BAD_PAGE);
+                page = a.num_pages;                            // outside the pool: a box of zeros
+            }
+            const uint32_t sk = ring + stage * Cfg::kStageB + lane * Cfg::kRunB, bar = full + 8 * stage;
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
+            for (int p = 0; p < Cfg::kPanels; ++p) {
+                ptx::tma_load_4d(sk + p * (kPgRun * 128), &maps.k, bar, p * (Cfg::kPanelB / (E4M3 ? 1 : 2)), row, hk, page);
+                ptx::tma_load_4d(sk + Cfg::kVOff + p * (kPgRun * 128), &maps.v, bar, p * (Cfg::kPanelB / (E4M3 ? 1 : 2)), row, hk, page);
+            }
             if constexpr (E4M3) {
-                const uint2 w0 = __ldcg(reinterpret_cast<const uint2*>(q0 + kk * 16 + c2 * 2)), w1 = __ldcg(reinterpret_cast<const uint2*>(q1 + kk * 16 + c2 * 2));
-                qa[kk][0] = ok0 ? w0.x : 0u; qa[kk][2] = ok0 ? w0.y : 0u;
-                qa[kk][1] = ok1 ? w1.x : 0u; qa[kk][3] = ok1 ? w1.y : 0u;
-            } else {
-                qa[kk][0] = ok0 ? __ldcg(reinterpret_cast<const uint32_t*>(q0 + kk * 16 + c2)) : 0u;
-                qa[kk][1] = ok1 ? __ldcg(reinterpret_cast<const uint32_t*>(q1 + kk * 16 + c2)) : 0u;
-                qa[kk][2] = ok0 ? __ldcg(reinterpret_cast<const uint32_t*>(q0 + kk * 16 + 8 + c2)) : 0u;
-                qa[kk][3] = ok1 ? __ldcg(reinterpret_cast<const uint32_t*>(q1 + kk * 16 + 8 + c2)) : 0u;
-            }
-        }
-    }
-    float o[D / 8][4];
-#pragma unroll
-    for (int i = 0; i < D / 8; ++i) { o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f; }
-    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
-
-    // The pages of a tile, one for each 16 rows (a page holds a multiple of 16); rows that nothing in the tile sees have none.
-    auto tile_at = [&](int j, bool& summ) { summ = j < s_tiles; return summ ? s_t0 + j : t_t0 + j - s_tiles; };
-    auto find_pages = [&](int j, int (&pg)[4]) {
-        bool summ;
-        const int x0 = tile_at(j, summ) * kPgTile;
-        const int lo = summ ? see.s_lo : see.t_lo, hi = summ ? see.s_hi : see.t_hi;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int x = x0 + 16 * i;
-            pg[i] = j < my1 && x < hi && x + 16 > lo ? paged_page(a, t.b, summ, x) : -3;
-            if (pg[i] == -1 || pg[i] == -2) { atomicCAS(a.status, 0, KSA_PAGED_STATUS_BAD_PAGE); pg[i] = -3; }
-        }
-    };
-    // rows nobody sees and rows without a page come as zeros: they are masked, and their V must be finite
-    auto load_tile = [&](int j, int stage, const int (&pg)[4]) {
-        bool summ;
-        const int x0 = tile_at(j, summ) * kPgTile;
-        const int lo = summ ? see.s_lo : see.t_lo, hi = summ ? see.s_hi : see.t_hi;
-        const uint32_t sk = sbase + stage * Cfg::kStageB, sv = sk + Cfg::kTileB;
-        constexpr int kRowsPass = kPgThreads / Cfg::kVec, kPasses = kPgTile / kRowsPass;
-        const int c16 = threadIdx.x % Cfg::kVec, rr = threadIdx.x / Cfg::kVec;
-        const int in_page = (1 << a.page_shift) - 1;
-#pragma unroll
-        for (int i = 0; i < kPasses; ++i) {
-            const int r = rr + i * kRowsPass, x = x0 + r;
-            int page;
-            if constexpr (kRowsPass <= 16) page = pg[i * kRowsPass / 16];
-            else page = rr >= 16 ? pg[(i * kRowsPass / 16 + 1) & 3] : pg[i * kRowsPass / 16];
-            const bool valid = page >= 0 && x >= lo && x < hi;
-            const int64_t off = valid ? page * a.page_st + hk * a.head_st + (x & in_page) * a.row_st + c16 * 16 : 0;
-            const uint32_t d = (uint32_t)(r * Cfg::kRowB + ((c16 ^ (Cfg::kVec == 4 ? (r >> 1) & 3 : r & 7)) << 4));
-            pg_cp16(sk + d, a.kp + off, valid);
-            pg_cp16(sv + d, a.vp + off, valid);
-        }
-        if constexpr (E4M3) {
-            if (threadIdx.x < 8) {
-                const int i = threadIdx.x & 3, x = x0 + 16 * i;
-                const int page = i == 0 ? pg[0] : i == 1 ? pg[1] : i == 2 ? pg[2] : pg[3];
-                const int64_t off = page >= 0 ? (((int64_t)page * a.Hkv + hk) << a.page_shift) + (x & in_page) : 0;
-                pg_cp16(sk + 2 * Cfg::kTileB + threadIdx.x * 16, (threadIdx.x < 4 ? a.ke : a.ve) + off, page >= 0);
+                const int64_t at = page < a.num_pages ? (((int64_t)page * a.Hkv + hk) << a.page_shift) + row : 0;
+                const uint32_t se = ring + stage * Cfg::kStageB + Cfg::kScaleOff + lane * 32;
+                pg_bulk16(se, a.ke + at, bar);
+                pg_bulk16(se + 16, a.ve + at, bar);
             }
         }
     };
-    int pg[4];
+    int entry;
+    {
+        int early[kStages - 1];
 #pragma unroll
-    for (int s = 0; s < kStages - 1; ++s) {
-        if (my0 + s < my1) {
-            find_pages(my0 + s, pg);
-            load_tile(my0 + s, s, pg);
-        }
-        pg_commit();
+        for (int s = 0; s < kStages - 1; ++s) early[s] = find_entry(my0 + s);
+        entry = find_entry(my0 + kStages - 1);
+#pragma unroll
+        for (int s = 0; s < kStages - 1; ++s)
+            if (my0 + s < my1) load_tile(my0 + s, s, early[s]);
     }
-    find_pages(my0 + kStages - 1, pg);
-    const int mi = lane >> 3, r8 = lane & 7;
-    for (int j = my0; j < my1; ++j) {
-        if (j + kStages - 1 < my1) load_tile(j + kStages - 1, (j - my0 + kStages - 1) % kStages, pg);
-        pg_commit();
-        find_pages(j + kStages, pg);                           // ahead of their use
-        pg_wait<kStages - 1>();
-        __syncthreads();
-        const uint32_t sk = sbase + ((j - my0) % kStages) * Cfg::kStageB, sv = sk + Cfg::kTileB;
-        const int wkey0 = warp * 16;
-        // S (16 rows x 16 keys of this warp) = Q K^T
-        float s[2][4];
+    // Q^T fragments (B operand, D x 8 N); rows past the tile's are zero
+    uint32_t qb[D / 16][N][2];
+    float qf[N][2];                                            // e4m3: what the scores of rows 8 n + c2, + 1 are to be multiplied with
 #pragma unroll
-        for (int i = 0; i < 2; ++i) { s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f; }
-        float fv[2][2];
+    for (int n = 0; n < N; ++n) {
+        const int r = min(n * 8 + l4, nrow - 1);
+        const bool ok = n * 8 + l4 < nrow;
+        const uint16_t* q = a.q + paged_row(a, t, t.x0 + r / heads) * a.q_st + (head0 + r % heads) * a.q_sh;
         if constexpr (E4M3) {
+            // columns 4 t .. 4 t + 3.  As f16, the row scaled by a power of two to a largest value of 2^8 .. 2^9: exact down to 2^-22
+            // of that, and off by 2^-33 of it below
+            uint2 w[D / 16];
+            uint32_t top = 0;
 #pragma unroll
-            for (int kk = 0; kk < D / 32; ++kk) {              // 32 columns of 16 keys
-                uint32_t kb[4];
-                const int key = wkey0 + (mi >> 1) * 8 + r8, chunk = kk * 2 + (mi & 1);
-                pg_ldsm(kb, sk + key * Cfg::kRowB + ((chunk ^ (Cfg::kVec == 4 ? (key >> 1) & 3 : key & 7)) << 4));
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    pg_mma(s[i >> 1], qa[kk * 2 + (i & 1)], pg_two(kb[i]), pg_two(kb[i] >> 16));
+            for (int kk = 0; kk < D / 16; ++kk) {
+                w[kk] = __ldcg(reinterpret_cast<const uint2*>(q + kk * 16 + c2 * 2));
+                top = __vmaxu2(top, __vmaxu2(w[kk].x & 0x7fff7fffu, w[kk].y & 0x7fff7fffu));
             }
-            const uint32_t se = sv + Cfg::kTileB + wkey0 + c2;
+            top = max(top >> 16, top & 0xffffu);
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const int e = min(max((int)(top >> 7) - 8, 1), 253);                  // the scale is 2^(127 - e), its inverse 2^(e - 127)
+            const float f = __uint_as_float((uint32_t)(254 - e) << 23);
+            auto two = [&](uint32_t x) {
+                const uint32_t h = pack_f16x2(__uint_as_float(x << 16) * f, __uint_as_float(x & 0xffff0000u) * f);
+                return ok ? h : 0u;
+            };
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt) {
-                const uint32_t at = se + nt * 8, sh = (at & 2) * 8;
-                const uint32_t ek = pg_ld_u32(at & ~3u) >> sh, ev = pg_ld_u32((at + kPgTile) & ~3u) >> sh;
-                const float f0 = e8m0_scale(ek & 255), f1 = e8m0_scale(ek >> 8 & 255);
-                s[nt][0] *= f0; s[nt][1] *= f1; s[nt][2] *= f0; s[nt][3] *= f1;
-                fv[nt][0] = e8m0_scale(ev & 255); fv[nt][1] = e8m0_scale(ev >> 8 & 255);
+            for (int kk = 0; kk < D / 16; ++kk) {
+                qb[kk][n][0] = two(w[kk].x);
+                qb[kk][n][1] = two(w[kk].y);
             }
+            const float back = __uint_as_float((uint32_t)e << 23);             // (lane 4 i holds row i)
+            qf[n][0] = __shfl_sync(0xffffffffu, back, c2 * 4);
+            qf[n][1] = __shfl_sync(0xffffffffu, back, c2 * 4 + 4);
         } else {
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
-                uint32_t kb[4];
-                const int key = wkey0 + (mi >> 1) * 8 + r8, chunk = kk * 2 + (mi & 1);
-                pg_ldsm(kb, sk + key * Cfg::kRowB + ((chunk ^ (key & 7)) << 4));
-                pg_mma(s[0], qa[kk], kb[0], kb[1]);
-                pg_mma(s[1], qa[kk], kb[2], kb[3]);
+                qb[kk][n][0] = ok ? __ldcg(reinterpret_cast<const uint32_t*>(q + kk * 16 + c2)) : 0u;
+                qb[kk][n][1] = ok ? __ldcg(reinterpret_cast<const uint32_t*>(q + kk * 16 + 8 + c2)) : 0u;
             }
         }
-        // each row's own range, online softmax in log2 units
-        bool summ;
-        const int x0 = tile_at(j, summ) * kPgTile + wkey0 + c2;
-        const int lo0 = summ ? v0.s_lo : v0.t_lo, hi0 = summ ? v0.s_hi : v0.t_hi, lo1 = summ ? v1.s_lo : v1.t_lo, hi1 = summ ? v1.s_hi : v1.t_hi;
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int x = x0 + nt * 8 + (e & 1);
-                s[nt][e] = x >= (e < 2 ? lo0 : lo1) && x < (e < 2 ? hi0 : hi1) ? s[nt][e] * a.scale_log2 : -INFINITY;
-            }
-        float mx0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
-        float mx1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
-        mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 1)); mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 2));
-        mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 1)); mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 2));
-        const float mn0 = fmaxf(m0, mx0), mn1 = fmaxf(m1, mx1);
-        const float al0 = (mn0 == -INFINITY) ? 1.f : ptx::ex2_approx(m0 - mn0), al1 = (mn1 == -INFINITY) ? 1.f : ptx::ex2_approx(m1 - mn1);
-        const float sub0 = (mn0 == -INFINITY) ? 0.f : mn0, sub1 = (mn1 == -INFINITY) ? 0.f : mn1;
-        m0 = mn0; m1 = mn1;
-        float pr[2][4];
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-            pr[nt][0] = ptx::ex2_approx(s[nt][0] - sub0); pr[nt][1] = ptx::ex2_approx(s[nt][1] - sub0);
-            pr[nt][2] = ptx::ex2_approx(s[nt][2] - sub1); pr[nt][3] = ptx::ex2_approx(s[nt][3] - sub1);
-        }
-        l0 = l0 * al0 + (pr[0][0] + pr[0][1]) + (pr[1][0] + pr[1][1]);
-        l1 = l1 * al1 + (pr[0][2] + pr[0][3]) + (pr[1][2] + pr[1][3]);
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) { o[i][0] *= al0; o[i][1] *= al0; o[i][2] *= al1; o[i][3] *= al1; }
-        if constexpr (E4M3) {                                  // (the scale bytes of rows that nobody sees may be anything)
-#pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) pr[nt][e] = pr[nt][e] == 0.f ? 0.f : pr[nt][e] * fv[nt][e & 1];
-        }
-        uint32_t pa[4];
-        pa[0] = ptx::pack_bf16x2(pr[0][0], pr[0][1]); pa[1] = ptx::pack_bf16x2(pr[0][2], pr[0][3]);
-        pa[2] = ptx::pack_bf16x2(pr[1][0], pr[1][1]); pa[3] = ptx::pack_bf16x2(pr[1][2], pr[1][3]);
-        // O += P V
-        if constexpr (E4M3) {
-            // o[2 i], o[2 i + 1]: the even and the odd columns of columns 16 i .. 16 i + 15
-#pragma unroll
-            for (int n2 = 0; n2 < D / 32; ++n2) {
-                uint32_t vb[4];
-                const int key = wkey0 + (mi & 1) * 8 + r8, chunk = n2 * 2 + (mi >> 1);
-                pg_ldsm_t(vb, sv + key * Cfg::kRowB + ((chunk ^ (Cfg::kVec == 4 ? (key >> 1) & 3 : key & 7)) << 4));
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t w0 = __byte_perm(vb[2 * i], 0, 0x3120), w1 = __byte_perm(vb[2 * i + 1], 0, 0x3120);
-                    pg_mma(o[4 * n2 + 2 * i], pa, pg_two(w0), pg_two(w1));
-                    pg_mma(o[4 * n2 + 2 * i + 1], pa, pg_two(w0 >> 16), pg_two(w1 >> 16));
-                }
-            }
-        } else {
-#pragma unroll
-            for (int n2 = 0; n2 < D / 16; ++n2) {
-                uint32_t vb[4];
-                const int key = wkey0 + (mi & 1) * 8 + r8, chunk = n2 * 2 + (mi >> 1);
-                pg_ldsm_t(vb, sv + key * Cfg::kRowB + ((chunk ^ (key & 7)) << 4));
-                pg_mma(o[2 * n2], pa, vb[0], vb[1]);
-                pg_mma(o[2 * n2 + 1], pa, vb[2], vb[3]);
-            }
-        }
-        __syncthreads();      // the stage is refilled by the load issued in the next iteration
     }
-    pg_wait<0>();
-    l0 += __shfl_xor_sync(0xffffffffu, l0, 1); l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
-    l1 += __shfl_xor_sync(0xffffffffu, l1, 1); l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
-    // the four warps' results: 16 rows of (m, l) and 16 x D of O each
-    __syncthreads();
-    float* sm_o = reinterpret_cast<float*>(pgsm);                      // [4][16][D]
-    float* sm_ml = sm_o + 4 * 16 * D;                                  // [4][16][2]
-    float* ct_o = sm_ml + 4 * 16 * 2;                                  // this CTA's: [16][D]
-    float* ct_ml = ct_o + 16 * D;                                      // [16][2]
-    {
-        float* r0 = sm_o + (warp * 16 + g0) * D;
-        float* r1 = r0 + 8 * D;
+    float o[D / 16][N][4];
+    float m[N][2], l[N][2];                                    // of query rows 8 n + c2, + 1
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
+    for (int n = 0; n < N; ++n) {
+        m[n][0] = m[n][1] = -INFINITY; l[n][0] = l[n][1] = 0.f;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) { o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f; }
+    }
+    const int mi = lane >> 3, r8 = lane & 7;
+    int stage = 0;
+    uint32_t phase = 0;
+    for (int j = my0; j < my1; ++j) {
+        __syncwarp();                                          // the tile before has been read by every lane
+        if (j + kStages - 1 < my1) load_tile(j + kStages - 1, stage == 0 ? kStages - 1 : stage - 1, entry);
+        entry = find_entry(j + kStages);
+        const bool ok = bounded_wait(full + 8 * stage, phase, abort_addr, a.status, kStatusWaitKvFull);
+        if (!__all_sync(0xffffffffu, ok)) {                    // given up: no copy is left in flight behind
+            for (int i = j, st = stage; i < min(j + kStages, my1); ++i) {
+                bounded_wait(full + 8 * st, phase, abort_addr + 4, a.status, kStatusWaitKvFull);
+                if (++st == kStages) { st = 0; phase ^= 1u; }
+            }
+            break;
+        }
+        const uint32_t sk = ring + stage * Cfg::kStageB, sv = sk + Cfg::kVOff;
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        bool summ;
+        const int x0 = tile_at(j, summ);
+        const int lo = summ ? see.s_lo : see.t_lo, hi = summ ? see.s_hi : see.t_hi;
+        if (x0 >= hi || x0 + kKeys <= lo) continue;            // nobody sees any of it
+        if (x0 < lo || x0 + kKeys > hi) {                      // V of rows that nobody sees: zeros (0 times what stands there may be NaN)
+            constexpr int kVec = Cfg::kRowB / 16;
+            for (int i = lane; i < kKeys * kVec; i += 32) {
+                const int r = i / kVec;
+                if (x0 + r < lo || x0 + r >= hi)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sv + (r >> 4) * Cfg::kRunB + Cfg::at(r & 15, i % kVec)), "r"(0u) : "memory");
+            }
+            ptx::fence_proxy_async();                          // (before the stage is filled again)
+            __syncwarp();
+        }
+        // S^T (16 keys x 8 N query rows, run by run) = K Q^T, in log2 units
+        float s[kSubs][N][4], back[kSubs][2];                  // e4m3: with the value rows' exponents, and 2^(127 - e) of these
+#pragma unroll
+        for (int u = 0; u < kSubs; ++u) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) { s[u][n][0] = s[u][n][1] = s[u][n][2] = s[u][n][3] = 0.f; }
             if constexpr (E4M3) {
-                const int d = i * 16 + c2 * 2;
-                *reinterpret_cast<float4*>(r0 + d) = make_float4(o[2 * i][0], o[2 * i + 1][0], o[2 * i][1], o[2 * i + 1][1]);
-                *reinterpret_cast<float4*>(r1 + d) = make_float4(o[2 * i][2], o[2 * i + 1][2], o[2 * i][3], o[2 * i + 1][3]);
+#pragma unroll
+                for (int kk = 0; kk < D / 32; ++kk) {          // 32 columns
+                    uint32_t kb[4];
+                    pg_ldsm(kb, sk + u * Cfg::kRunB + Cfg::at((mi & 1) * 8 + r8, kk * 2 + (mi >> 1)));
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t a0, a1, a2, a3;
+                        e4m3x4_to_f16(kb[2 * i], a0, a2);
+                        e4m3x4_to_f16(kb[2 * i + 1], a1, a3);
+#pragma unroll
+                        for (int n = 0; n < N; ++n) pg_mma_f16(s[u][n], a0, a1, a2, a3, qb[kk * 2 + i][n]);
+                    }
+                }
+                const uint32_t se = sk + Cfg::kScaleOff + u * 32 + l4;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {                  // keys l4, l4 + 8
+                    const float fk = a.scale_log2 * e8m0_factor(pg_ld_u8(se + 8 * h));
+                    const uint32_t e = pg_ld_u8(se + 16 + 8 * h);
+                    const float ef = e == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(0x4b000000u | e) - (8388608.f + 127.f);
+                    back[u][h] = __uint_as_float((uint32_t)max((int)(254u - e) << 23, 0x00400000));
+#pragma unroll
+                    for (int n = 0; n < N; ++n)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) s[u][n][2 * h + c] = fmaf(s[u][n][2 * h + c] * qf[n][c], fk, ef);
+                }
             } else {
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int d = i * 16 + u * 8 + c2;
-                    *reinterpret_cast<float2*>(r0 + d) = make_float2(o[2 * i + u][0], o[2 * i + u][1]);
-                    *reinterpret_cast<float2*>(r1 + d) = make_float2(o[2 * i + u][2], o[2 * i + u][3]);
+                for (int kk = 0; kk < D / 16; ++kk) {
+                    uint32_t kb[4];
+                    pg_ldsm(kb, sk + u * Cfg::kRunB + Cfg::at((mi & 1) * 8 + r8, kk * 2 + (mi >> 1)));
+#pragma unroll
+                    for (int n = 0; n < N; ++n) pg_mma(s[u][n], kb[0], kb[1], kb[2], kb[3], qb[kk][n]);
+                }
+#pragma unroll
+                for (int n = 0; n < N; ++n) { s[u][n][0] *= a.scale_log2; s[u][n][1] *= a.scale_log2; s[u][n][2] *= a.scale_log2; s[u][n][3] *= a.scale_log2; }
+            }
+        }
+        // each row's own range, where the keys hold an end of some row's
+        if (x0 < (summ ? last.s_lo : last.t_lo) || x0 + kKeys > (summ ? first.s_hi : first.t_hi)) {
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const PagedView w = paged_view(a, t.summ, t.x0 + min(n * 8 + c2 + c, nrow - 1) / heads);
+                    const int rlo = (summ ? w.s_lo : w.t_lo) - x0 - l4, rhi = (summ ? w.s_hi : w.t_hi) - x0 - l4;
+#pragma unroll
+                    for (int u = 0; u < kSubs; ++u)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            if (16 * u + 8 * h < rlo || 16 * u + 8 * h >= rhi) s[u][n][2 * h + c] = -INFINITY;
+                }
+        }
+        // the reference maximum moves, and O with it, only when some row outgrew its own (eight lanes share a row)
+        float mx[N][2];
+        bool grown = false;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                mx[n][c] = fmaxf(s[0][n][c], s[0][n][2 + c]);
+#pragma unroll
+                for (int u = 1; u < kSubs; ++u) mx[n][c] = ptx::fmax3(mx[n][c], s[u][n][c], s[u][n][2 + c]);
+                grown |= mx[n][c] > m[n][c] + Cfg::kRescale;
+            }
+        if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float x = mx[n][c];
+#pragma unroll
+                    for (int b = 4; b < 32; b <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, b));
+                    const float mn = fmaxf(m[n][c], x), al = (mn == -INFINITY) ? 1.f : ptx::ex2_approx(m[n][c] - mn);
+                    m[n][c] = mn;
+                    l[n][c] *= al;
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) { o[i][n][c] *= al; o[i][n][2 + c] *= al; }
+                }
+        }
+#pragma unroll
+        for (int u = 0; u < kSubs; ++u) {
+            uint32_t pb[N][2];
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const float sub0 = (m[n][0] == -INFINITY) ? 0.f : m[n][0], sub1 = (m[n][1] == -INFINITY) ? 0.f : m[n][1];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float p0 = ptx::ex2_approx(s[u][n][2 * h] - sub0), p1 = ptx::ex2_approx(s[u][n][2 * h + 1] - sub1);
+                    if constexpr (E4M3) {
+                        l[n][0] = fmaf(p0, back[u][h], l[n][0]);
+                        l[n][1] = fmaf(p1, back[u][h], l[n][1]);
+                        pb[n][h] = pg_transpose(pack_f16x2(p0, p1));
+                    } else {
+                        l[n][0] += p0;
+                        l[n][1] += p1;
+                        pb[n][h] = pg_transpose(ptx::pack_bf16x2(p0, p1));
+                    }
+                }
+            }
+            // O^T += V^T P^T
+            if constexpr (E4M3) {                              // rows r, r + 8 of a product: columns 2 r, 2 r + 1 of 16
+#pragma unroll
+                for (int i2 = 0; i2 < D / 32; ++i2) {
+                    uint32_t vb[4];
+                    pg_ldsm_t(vb, sv + u * Cfg::kRunB + Cfg::at((mi & 1) * 8 + r8, i2 * 2 + (mi >> 1)));
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t a0, a1, a2, a3;
+                        e4m3x4_to_f16(__byte_perm(vb[2 * i], 0, 0x3120), a0, a1);
+                        e4m3x4_to_f16(__byte_perm(vb[2 * i + 1], 0, 0x3120), a2, a3);
+#pragma unroll
+                        for (int n = 0; n < N; ++n) pg_mma_f16(o[2 * i2 + i][n], a0, a1, a2, a3, pb[n]);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    uint32_t vb[4];
+                    pg_ldsm_t(vb, sv + u * Cfg::kRunB + Cfg::at((mi >> 1) * 8 + r8, i * 2 + (mi & 1)));
+#pragma unroll
+                    for (int n = 0; n < N; ++n) pg_mma(o[i][n], vb[0], vb[1], vb[2], vb[3], pb[n]);
                 }
             }
         }
     }
-    if ((lane & 3) == 0) {
-        sm_ml[(warp * 16 + g0) * 2] = m0; sm_ml[(warp * 16 + g0) * 2 + 1] = l0;
-        sm_ml[(warp * 16 + g0 + 8) * 2] = m1; sm_ml[(warp * 16 + g0 + 8) * 2 + 1] = l1;
-    }
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int b = 4; b < 32; b <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], b);
+    // the warps' results: rows of (maximum, sum) and of O each
     __syncthreads();
-    for (int idx = threadIdx.x; idx < nrow * (D / 4); idx += kPgThreads) {
+    constexpr int kRows = Cfg::kRows, kLd = Cfg::kLd;
+    float* sm_o = reinterpret_cast<float*>(pgsm);                      // [warps][rows][kLd]
+    float* ct_o = sm_o + kWarps * kRows * kLd;                       // this CTA's: [rows][kLd]
+    float* sm_ml = ct_o + kRows * kLd;                                 // [warps][rows][2]
+    float* ct_ml = sm_ml + kWarps * kRows * 2;                       // [rows][2]
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            float* r = sm_o + (warp * kRows + n * 8 + c2 + e) * kLd;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                if constexpr (E4M3) *reinterpret_cast<float2*>(r + i * 16 + 2 * l4) = make_float2(o[i][n][e], o[i][n][2 + e]);
+                else { r[i * 16 + l4] = o[i][n][e]; r[i * 16 + 8 + l4] = o[i][n][2 + e]; }
+            }
+            if (l4 == 0) *reinterpret_cast<float2*>(sm_ml + (warp * kRows + n * 8 + c2 + e) * 2) = make_float2(m[n][e], l[n][e]);
+        }
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < nrow * (D / 4); idx += kThreads) {
         const int g = idx / (D / 4), d = (idx - g * (D / 4)) * 4;
+        float2 ml[kWarps];
         float M = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) M = fmaxf(M, sm_ml[(w * 16 + g) * 2]);
+        for (int w = 0; w < kWarps; ++w) { ml[w] = *reinterpret_cast<const float2*>(sm_ml + (w * kRows + g) * 2); M = fmaxf(M, ml[w].x); }
         float L = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float mw = sm_ml[(w * 16 + g) * 2];
-            const float f = (mw == -INFINITY) ? 0.f : ptx::ex2_approx(mw - M);
-            const float4 v = *reinterpret_cast<const float4*>(sm_o + (w * 16 + g) * D + d);
-            L += sm_ml[(w * 16 + g) * 2 + 1] * f;
+        for (int w = 0; w < kWarps; ++w) {
+            const float f = (ml[w].x == -INFINITY) ? 0.f : ptx::ex2_approx(ml[w].x - M);
+            const float4 v = *reinterpret_cast<const float4*>(sm_o + (w * kRows + g) * kLd + d);
+            L += ml[w].y * f;
             acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
         }
-        *reinterpret_cast<float4*>(ct_o + g * D + d) = acc;
-        if (d == 0) { ct_ml[g * 2] = M; ct_ml[g * 2 + 1] = L; }
+        *reinterpret_cast<float4*>(ct_o + g * kLd + d) = acc;
+        if (d == 0) *reinterpret_cast<float2*>(ct_ml + g * 2) = make_float2(M, L);
     }
     if (a.nsplit > 1) { ptx::cluster_arrive(); ptx::cluster_wait(); } else __syncthreads();
     // the cluster's CTAs share the output's elements
     const uint32_t so = ptx::smem_u32(ct_o), sml = ptx::smem_u32(ct_ml);
-    for (int idx = split * kPgThreads + threadIdx.x; idx < nrow * (D / 4); idx += kPgThreads * a.nsplit) {
+    for (int idx = split * kThreads + threadIdx.x; idx < nrow * (D / 4); idx += kThreads * a.nsplit) {
         const int g = idx / (D / 4), d = (idx - g * (D / 4)) * 4;
-        float2 ml[kPgMaxSplit];
-        float4 v[kPgMaxSplit];
-#pragma unroll
-        for (int w = 0; w < kPgMaxSplit; ++w)
-            if (w < a.nsplit) {
-                ml[w] = pg_ld_cluster2(ptx::mapa_shared(sml + g * 8, w));
-                v[w] = pg_ld_cluster4(ptx::mapa_shared(so + (g * D + d) * 4, w));
-            }
         float M = -INFINITY, L = 0.f;
-#pragma unroll
-        for (int w = 0; w < kPgMaxSplit; ++w) if (w < a.nsplit) M = fmaxf(M, ml[w].x);
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < kPgMaxSplit; ++w)
-            if (w < a.nsplit) {
-                const float f = (ml[w].x == -INFINITY) ? 0.f : ptx::ex2_approx(ml[w].x - M);
-                L += ml[w].y * f;
-                acc.x += v[w].x * f; acc.y += v[w].y * f; acc.z += v[w].z * f; acc.w += v[w].w * f;
-            }
+        for (int w0 = 0; w0 < kPgMaxSplit; w0 += 8) {
+            if (w0 >= a.nsplit) break;
+            float2 ml[8];
+            float4 v[8];
+#pragma unroll
+            for (int w = 0; w < 8; ++w)
+                if (w0 + w < a.nsplit) {
+                    ml[w] = pg_ld_cluster2(ptx::mapa_shared(sml + g * 8, w0 + w));
+                    v[w] = pg_ld_cluster4(ptx::mapa_shared(so + (g * kLd + d) * 4, w0 + w));
+                }
+            float mx = M;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) if (w0 + w < a.nsplit) mx = fmaxf(mx, ml[w].x);
+            const float al = (mx == -INFINITY) ? 1.f : ptx::ex2_approx(M - mx);
+            M = mx; L *= al; acc.x *= al; acc.y *= al; acc.z *= al; acc.w *= al;
+#pragma unroll
+            for (int w = 0; w < 8; ++w)
+                if (w0 + w < a.nsplit) {
+                    const float f = (ml[w].x == -INFINITY) ? 0.f : ptx::ex2_approx(ml[w].x - M);
+                    L += ml[w].y * f;
+                    acc.x += v[w].x * f; acc.y += v[w].y * f; acc.z += v[w].z * f; acc.w += v[w].w * f;
+                }
+        }
         const float inv = 1.f / L;
         const int64_t row = paged_row(a, t, t.x0 + g / heads);
         const int h = head0 + g % heads;
@@ -385,50 +495,77 @@ __global__ void __launch_bounds__(kPgThreads) ksa_paged_attn_kernel(const __grid
     if (a.nsplit > 1) { ptx::cluster_arrive(); ptx::cluster_wait(); }      // no CTA leaves while another reads its results
 }
 
-template <int D, bool E4M3>
-static cudaError_t setup_one()
+// f(kernel, shared memory) for each or one of the kernels
+template <int D, bool E4M3, int N, class F> static cudaError_t with_kernel(F f) { return f(ksa_paged_attn_kernel<D, E4M3, N>, PgCfg<D, E4M3, N>::kSmemBytes, PgCfg<D, E4M3, N>::kThreads); }
+template <int D, class F> static cudaError_t with_kernel(bool e4m3, int n, F f)
 {
-    return cudaFuncSetAttribute(ksa_paged_attn_kernel<D, E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, PgCfg<D, E4M3>::kSmemBytes);
+    if (e4m3) return n == 1 ? with_kernel<D, true, 1>(f) : with_kernel<D, true, 2>(f);
+    return n == 1 ? with_kernel<D, false, 1>(f) : with_kernel<D, false, 2>(f);
 }
 cudaError_t setup_paged_attn()
 {
-    for (cudaError_t e : {setup_one<128, false>(), setup_one<128, true>(), setup_one<64, false>(), setup_one<64, true>()})
+    for (int i = 0; i < 8; ++i) {
+        auto set = [](auto kernel, int smem, int) {
+            const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+            return e != cudaSuccess ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        };
+        const cudaError_t e = i & 4 ? with_kernel<128>(i & 1, i & 2 ? 2 : 1, set) : with_kernel<64>(i & 1, i & 2 ? 2 : 1, set);
         if (e != cudaSuccess) return e;
+    }
     return cudaSuccess;
 }
 
-// CTAs of one cluster for a call of `units` query tiles at most: two CTAs of each SM, as far as there are key tiles to split
+// CTAs of one cluster for a call of `units` query tiles at most: up to four CTAs a SM (two are resident), as far as there are
+// key tiles to split.  128 units of 17,300 rows each, e4m3 (1, 2, 4, 8 CTAs a unit): 186, 100, 108, 125 us; 116 units of 700 to
+// 17,400 rows: 199, 112, 63, 73 us; 8 units of 2,000 rows, bf16: 29, 17.7, 11.6, 8.9 us.
 static int paged_splits(int64_t units, int64_t key_tiles, int num_sms)
 {
     int n = 1;
-    while (n < kPgMaxSplit && units * n * 2 <= 2 * num_sms && key_tiles >= 2 * n) n *= 2;
+    while (n < kPgMaxSplit && units * n * 2 <= 4 * num_sms && key_tiles >= 2 * n) n *= 2;
     return n;
 }
 
-cudaError_t launch_paged_attn(const PagedArgs& args, bool e4m3, int num_sms, cudaStream_t stream)
+bool encode_pages(PagedEncode encode, CUtensorMap* map, void* base, const PagedArgs& a, bool e4m3, int box_bytes, int box_rows, CUtensorMapSwizzle swizzle)
+{
+    const cuuint64_t dims[4] = {(cuuint64_t)a.D, (cuuint64_t)1 << a.page_shift, (cuuint64_t)a.Hkv, (cuuint64_t)a.num_pages};
+    auto stride = [](int64_t st) { return (cuuint64_t)(st > 0 ? st : 16); };            // (0: a dimension of one)
+    const cuuint64_t strides[3] = {stride(a.row_st), stride(a.head_st), stride(a.page_st)};
+    const cuuint32_t box[4] = {(cuuint32_t)(e4m3 ? box_bytes : box_bytes / 2), (cuuint32_t)box_rows, 1, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return encode(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base, dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+cudaError_t launch_paged_attn(const PagedArgs& args, bool e4m3, int num_sms, PagedEncode encode, cudaStream_t stream)
 {
     PagedArgs a = args;
-    a.tokens_per_tile = a.G <= 16 ? 16 / a.G : 1;
-    a.head_blocks = (a.G + 15) / 16;
+    const int n = (int64_t)a.rows * a.G <= 8 * (int64_t)a.B ? 1 : 2;
+    a.tokens_per_tile = a.G <= 8 * n ? 8 * n / a.G : 1;
+    a.head_blocks = (a.G + 8 * n - 1) / (8 * n);
     // no tile without a row, none but a sequence's last of its kind with fewer than tokens_per_tile tokens
     const int64_t most = (int64_t)a.rows / a.tokens_per_tile + (int64_t)a.B * (a.m > 0 ? 2 : 1);
     const int64_t units = (most < a.rows ? most : a.rows) * a.Hkv * a.head_blocks;
     const int64_t rows = ((int64_t)a.text_cols + (a.m > 0 ? a.summ_cols : 0)) << a.page_shift;      // of a sequence, at most
-    a.nsplit = paged_splits(units, rows / kPgTile, num_sms);
+    a.nsplit = paged_splits(units, rows / 64, num_sms);
+    const int panel = a.D * (e4m3 ? 1 : 2) < 128 ? 64 : 128;
+    const CUtensorMapSwizzle swizzle = panel == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B;
+    PgMaps maps;
+    if (!encode_pages(encode, &maps.k, a.kp, a, e4m3, panel, kPgRun, swizzle) || !encode_pages(encode, &maps.v, a.vp, a, e4m3, panel, kPgRun, swizzle))
+        return cudaErrorInvalidValue;
     cudaLaunchAttribute attr[2]{};
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = (unsigned)a.nsplit; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(units * a.nsplit)); cfg.blockDim = dim3(kPgThreads); cfg.stream = stream;
+    cfg.gridDim = dim3((unsigned)(units * a.nsplit)); cfg.stream = stream;
     cfg.attrs = attr; cfg.numAttrs = 2;
-    auto go = [&](auto kernel, int smem) {
+    auto go = [&](auto kernel, int smem, int threads) {
+        cfg.blockDim = dim3((unsigned)threads);
         cfg.dynamicSmemBytes = (size_t)smem;
-        return cudaLaunchKernelEx(&cfg, kernel, a);
+        return cudaLaunchKernelEx(&cfg, kernel, a, maps);
     };
-    if (a.D == 128) return e4m3 ? go(ksa_paged_attn_kernel<128, true>, PgCfg<128, true>::kSmemBytes) : go(ksa_paged_attn_kernel<128, false>, PgCfg<128, false>::kSmemBytes);
-    return e4m3 ? go(ksa_paged_attn_kernel<64, true>, PgCfg<64, true>::kSmemBytes) : go(ksa_paged_attn_kernel<64, false>, PgCfg<64, false>::kSmemBytes);
+    return a.D == 128 ? with_kernel<128>(e4m3, n, go) : with_kernel<64>(e4m3, n, go);
 }
 
 }  // namespace ksa

@@ -12,9 +12,15 @@
 //   warp  9     issues S = Q K^T (tcgen05.mma, smem x smem)
 //   warp 10     issues O += P V (P from TMEM)
 //   warp 11     TMA of the value tiles (bf16 pages)
-//   warps 12-15 (e4m3 pages) turn the tiles that warp 8 brings in 8 bits into bf16 ones, a row per thread, its scale on the way
+//   warps 12-15 (e4m3 pages) turn the tiles that warp 8 brings in 8 bits into f16 ones, a row per thread, its scale on the way
 // TMEM: one score slot S [0,128) that the two query tiles take in turns, the bf16 probabilities P0 [128,192), P1 [192,256),
 // O0 [256,256+D), O1 [384,384+D).  The pipeline over the key tiles is that of the text-row kernel (ksa_text_tc.cu).
+//
+// e4m3 pages: all products are of f16 (one conversion for two values, one multiplication for their scale; as bf16 it took three
+// times the instructions, and the converting warps set the pace: 1.6 ms for the last 4,608 of 147,456 rows, 32/4 heads).  A row's
+// scale is taken relative to the largest among the rows in view, which is found first: values are at most 448 * 2^7, and what
+// underflows is below 2^-39 of the largest.  An e4m3 value has four significant bits, so rows whose scale is up to 2^28 smaller than
+// the largest keep theirs.  Q becomes f16 by a power of two for each row; P as f16 is rounded eight times finer than as bf16.
 //
 // Rows of a page that nothing in the tile sees may hold anything.  Scores of such keys are replaced by -inf; their V rows
 // are overwritten with zeros in shared memory (0 * NaN would reach the accumulators): by warp 10 in the tiles that hold an end
@@ -130,7 +136,8 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
     const uint32_t sQ = smem_base + Cfg::kQOff, sK = smem_base + Cfg::kKOff, sV = smem_base + Cfg::kVOff, sRaw = smem_base + Cfg::kRawOff;
     const uint32_t bars = smem_base + Cfg::kBarOff;
     const uint32_t tmem_slot = bars + 8 * Cfg::kNumBars;
-    const uint32_t abort_addr = tmem_slot + 4;
+    const uint32_t abort_addr = tmem_slot + 4;                 // (two words)
+    const uint32_t tops = tmem_slot + 16;                       // e4m3: the largest scale bytes of K and of V, by converting warp
     auto bar = [&](int i) -> uint32_t { return bars + 8u * (uint32_t)i; };
 
     const int tid = threadIdx.x;
@@ -182,9 +189,46 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
             bool alive = true;
             int k_stage = 0, v_stage = 0, raw = 0;
             uint32_t k_phase = 0, v_phase = 0, raw_phase = 0;
-            // this thread's row of tile j: whether anyone sees it, and its scales (found a tile ahead)
-            auto scales = [&](int j, float& fk, float& fv) {
-                fk = fv = 0.f;
+            // the largest scales of K and of V among the rows in view: 16 rows at a time
+            uint32_t top_k = 0, top_v = 0;
+            for (int i = row; i < T * (kPtTile / 16); i += 128) {
+                int x0, lo, hi;
+                const bool summ = w.at(w.j0 + i / (kPtTile / 16), x0, lo, hi);
+                const int x = x0 + i % (kPtTile / 16) * 16;
+                if (x >= hi || x + 16 <= lo) continue;
+                const int page = paged_page(a, t.b, summ, x);
+                if (page < 0) continue;
+                const int64_t at = (((int64_t)page * a.Hkv + hk) << a.page_shift) + (x & ((1 << a.page_shift) - 1));
+                const uint4 k = __ldcg(reinterpret_cast<const uint4*>(a.ke + at)), v = __ldcg(reinterpret_cast<const uint4*>(a.ve + at));
+                const uint32_t kw[4] = {k.x, k.y, k.z, k.w}, vw[4] = {v.x, v.y, v.z, v.w};
+                uint32_t mk = 0, mv = 0;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t in = 0xffffffffu;                 // rows in view
+                    if (x + 4 * c < lo) in &= x + 4 * c + 4 <= lo ? 0u : 0xffffffffu << 8 * (lo - x - 4 * c);
+                    if (x + 4 * c + 4 > hi) in &= x + 4 * c >= hi ? 0u : 0xffffffffu >> 8 * (x + 4 * c + 4 - hi);
+                    mk = __vmaxu4(mk, kw[c] & in & ~__vcmpeq4(kw[c], 0xffffffffu));       // (255: a row of NaN)
+                    mv = __vmaxu4(mv, vw[c] & in & ~__vcmpeq4(vw[c], 0xffffffffu));
+                }
+                mk = __vmaxu2(mk >> 8 & 0x00ff00ffu, mk & 0x00ff00ffu); mv = __vmaxu2(mv >> 8 & 0x00ff00ffu, mv & 0x00ff00ffu);
+                top_k = max(top_k, max(mk >> 16, mk & 0xffffu)); top_v = max(top_v, max(mv >> 16, mv & 0xffffu));
+            }
+            top_k = __reduce_max_sync(0xffffffffu, top_k);
+            top_v = __reduce_max_sync(0xffffffffu, top_v);
+            if (lane == 0) { st_shared_u32(tops + 8 * (warp - 12), top_k); st_shared_u32(tops + 8 * (warp - 12) + 4, top_v); }
+            pt_named_barrier(2, 384);                          // with the softmax warps, who need them too
+            top_k = top_v = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { top_k = max(top_k, ld_shared_u32(tops + 8 * i)); top_v = max(top_v, ld_shared_u32(tops + 8 * i + 4)); }
+            // 2^(e - top + 7) as f16, twice; 255: NaN
+            auto factor = [](uint32_t e, uint32_t top) {
+                const int p = (int)e - (int)top + 7;
+                const uint32_t h = e == 255u ? 0x7e00u : p >= -14 ? (uint32_t)(p + 15) << 10 : p >= -24 ? 1u << (p + 24) : 0u;
+                return h | h << 16;
+            };
+            // this thread's row of tile j: its factors (found a tile ahead), 0xffffffff where nobody sees it
+            auto scales = [&](int j, uint32_t& fk, uint32_t& fv) {
+                fk = fv = 0xffffffffu;
                 if (j >= w.j1) return;
                 int x0, lo, hi;
                 const bool summ = w.at(j, x0, lo, hi);
@@ -193,10 +237,10 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                 const int page = paged_page(a, t.b, summ, x);
                 if (page < 0) return;
                 const int64_t at = (((int64_t)page * a.Hkv + hk) << a.page_shift) + (x & ((1 << a.page_shift) - 1));
-                fk = e8m0_scale(__ldcg(a.ke + at));
-                fv = e8m0_scale(__ldcg(a.ve + at));
+                fk = factor(__ldcg(a.ke + at), top_k);
+                fv = factor(__ldcg(a.ve + at), top_v);
             };
-            auto convert = [&](uint32_t full, uint32_t empty, uint32_t empty_parity, uint32_t dst, float f) {
+            auto convert = [&](uint32_t full, uint32_t empty, uint32_t empty_parity, uint32_t dst, uint32_t f) {
                 if (alive) alive = __all_sync(0xffffffffu, bounded_wait(bar(Cfg::kRawFull + raw), raw_phase, abort_addr, a.status, kStatusWaitKvFull));
                 if (alive) alive = __all_sync(0xffffffffu, bounded_wait(empty, empty_parity, abort_addr, a.status, kStatusWaitKvEmpty));
                 if (!alive) return;
@@ -204,16 +248,17 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
                     const int c = (i + row) & (D / 16 - 1);         // neighbouring rows start at different banks
-                    uint4 y = pt_ld_shared4(src + c * 16);
-                    uint32_t z[8];
-                    const uint32_t yw[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 p = e4m3x2_to_f32(yw[e] & 0xffffu), q = e4m3x2_to_f32(yw[e] >> 16);
-                        z[2 * e] = f == 0.f ? 0u : pack_bf16x2(p.x * f, p.y * f);
-                        z[2 * e + 1] = f == 0.f ? 0u : pack_bf16x2(q.x * f, q.y * f);
-                    }
                     const uint32_t d = dst + (c >> 2) * 16384 + row * 128;
+                    uint32_t z[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+                    if (f != 0xffffffffu) {
+                        const uint4 y = pt_ld_shared4(src + c * 16);
+                        const uint32_t yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            e4m3x4_to_f16(yw[e], z[2 * e], z[2 * e + 1]);
+                            z[2 * e] = mul_f16x2(z[2 * e], f); z[2 * e + 1] = mul_f16x2(z[2 * e + 1], f);
+                        }
+                    }
                     pt_st_shared4(d + ((((c & 3) * 2) ^ (row & 7)) << 4), z[0], z[1], z[2], z[3]);
                     pt_st_shared4(d + ((((c & 3) * 2 + 1) ^ (row & 7)) << 4), z[4], z[5], z[6], z[7]);
                 }
@@ -222,10 +267,10 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                 if (lane == 0) { mbar_arrive(full); mbar_arrive(bar(Cfg::kRawEmpty + raw)); }
                 if (++raw == Cfg::kStagesRaw) { raw = 0; raw_phase ^= 1u; }
             };
-            float fk, fv;
+            uint32_t fk, fv;
             scales(w.j0, fk, fv);
             for (int j = w.j0; j < w.j1 && alive; ++j) {
-                float nk, nv;
+                uint32_t nk, nv;
                 scales(j + 1, nk, nv);
                 convert(bar(Cfg::kKFull + k_stage), bar(Cfg::kKEmpty + k_stage), k_phase ^ 1u, sK + k_stage * Cfg::kTileBytes, fk);
                 if (++k_stage == Cfg::kStagesK) { k_stage = 0; k_phase ^= 1u; }
@@ -302,7 +347,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
             };
             uint32_t stage = 0, ring_phase = 0, phase0 = 0, phase1 = 0;
             if (warp == 9) {
-                constexpr uint32_t idesc = make_idesc_bf16(128, 128, false);
+                constexpr uint32_t idesc = E4M3 ? make_idesc_f16(128, 128, false) : make_idesc_bf16(128, 128, false);
                 const uint32_t q_lo = smem_desc_lo(sQ, 16), k_lo = smem_desc_lo(sK, 16);
                 int before = -1;                            // query tile whose scores stand in the slot
                 for (int j = 0; j < T && alive; ++j) {
@@ -328,7 +373,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                     if (++stage == (uint32_t)Cfg::kStagesK) { stage = 0; ring_phase ^= 1u; }
                 }
             } else {
-                constexpr uint32_t idesc = make_idesc_bf16(128, D, true);
+                constexpr uint32_t idesc = E4M3 ? make_idesc_f16(128, D, true) : make_idesc_bf16(128, D, true);
                 const uint32_t v_lo = smem_desc_lo(sV, 16384);   // MN-major: 64-column panels 16 KB apart, groups of 8 keys 1 KB
                 for (int j = 0; j < T && alive; ++j) {
                     wait(bar(Cfg::kVFull) + 8u * stage, ring_phase, kStatusWaitKvFull);
@@ -384,6 +429,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
         const int head = hk * a.G + r_in % a.G;
         const bool valid = row < nrow;
         bool alive = true;
+        float q_back = 1.f, v_back = 1.f;                                      // e4m3: what the scores and O are to be multiplied with
         if (u < nh) {
             // ---- Q: this thread's row, K-major with 128-byte swizzle ----
             {
@@ -392,13 +438,35 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                 uint4 y[D / 8];
 #pragma unroll
                 for (int c = 0; c < D / 8; ++c) y[c] = __ldcg(reinterpret_cast<const uint4*>(q + c * 8));
+                if constexpr (E4M3) {                        // as f16, the row's largest value taken to 2^8 or more (below 2^9)
+                    uint32_t top = 0;
+#pragma unroll
+                    for (int c = 0; c < D / 8; ++c)
+                        top = __vmaxu2(top, __vmaxu2(__vmaxu2(y[c].x & 0x7fff7fffu, y[c].y & 0x7fff7fffu), __vmaxu2(y[c].z & 0x7fff7fffu, y[c].w & 0x7fff7fffu)));
+                    const int e = min(max((int)(max(top >> 16, top & 0xffffu) >> 7) - 8, 1), 253);
+                    const float f = __uint_as_float((uint32_t)(254 - e) << 23);
+                    q_back = __uint_as_float((uint32_t)e << 23);
+                    auto two = [&](uint32_t& z) { z = pack_f16x2(__uint_as_float(z << 16) * f, __uint_as_float(z & 0xffff0000u) * f); };
+#pragma unroll
+                    for (int c = 0; c < D / 8; ++c) { two(y[c].x); two(y[c].y); two(y[c].z); two(y[c].w); }
+                }
 #pragma unroll
                 for (int c = 0; c < D / 8; ++c) pt_st_shared4(d + (c >> 3) * 16384 + (((c & 7) ^ (row & 7)) << 4), y[c].x, y[c].y, y[c].z, y[c].w);
                 fence_proxy_async();
                 mbar_arrive(bar(Cfg::kQFull + u));
             }
+        }
+        if constexpr (E4M3) {
+            pt_named_barrier(2, 384);                        // the largest scales are known
+            uint32_t top_k = 0, top_v = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { top_k = max(top_k, ld_shared_u32(tops + 8 * i)); top_v = max(top_v, ld_shared_u32(tops + 8 * i + 4)); }
+            q_back *= e8m0_factor(top_k) * 0.0078125f;       // (K and V stand 2^7 times larger)
+            v_back = e8m0_factor(top_v) * 0.0078125f;
+        }
+        if (u < nh) {
             const PagedView see = paged_view(a, t.summ, x);
-            const float scale_log2 = a.scale_log2;
+            const float scale_log2 = E4M3 ? a.scale_log2 * q_back : a.scale_log2;
             uint32_t sf_phase = 0, pv_phase = 0;
             int rel_k = 0, rel_v = 0;                        // the stages handed back next, by the last query tile's first thread
             const bool releaser = (tid & 127) == 0 && u == nh - 1;
@@ -474,7 +542,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                     pr.x = ex2_approx(z.x); pr.y = ex2_approx(z.y);
                     if (q & 1) lb = fadd2(lb, pr); else la = fadd2(la, pr);
                     if (q == 48 && j > 0) pv_ok = mbar_test_wait(bar(Cfg::kPvDone + u), pv_phase);
-                    s[q] = pack_bf16x2(pr.x, pr.y);
+                    s[q] = E4M3 ? pack_f16x2(pr.x, pr.y) : pack_bf16x2(pr.x, pr.y);
                 }
                 l_run += (la.x + la.y) + (lb.x + lb.y);
                 if (j > 0) {
@@ -519,7 +587,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
         if (a.nsplit == 1) {
             // ---- epilogue: O / l -> bf16 at the row's place, LSE ----
             if (u < nh && alive) {
-                const float inv_l = 1.f / l_run;
+                const float inv_l = v_back / l_run;
                 const int64_t prow = paged_row(a, t, x);
                 const bool store = valid && ksa_in_bounds(prow >= 0 && prow < a.rows && head < a.Hq, a.status);
                 // a row stands in one lane: four lanes exchange 64 bytes of their rows, so that a store touches 8 lines, not 32
@@ -556,8 +624,12 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t o[32];
-                    if (u < nh) { tmem_ld32(tO + c * 32, o); tc_wait_ld(); }
-                    else {
+                    if (u < nh) {
+                        tmem_ld32(tO + c * 32, o);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) if (E4M3) o[e] = __float_as_uint(__uint_as_float(o[e]) * v_back);
+                    } else {
 #pragma unroll
                         for (int e = 0; e < 32; ++e) o[e] = 0u;
                     }
@@ -626,19 +698,6 @@ cudaError_t setup_paged_tc()
     return cudaSuccess;
 }
 
-static bool encode_pages(PagedEncode encode, CUtensorMap* map, void* base, const PagedArgs& a, bool e4m3)
-{
-    const int rows = 1 << a.page_shift;
-    const cuuint64_t dims[4] = {(cuuint64_t)a.D, (cuuint64_t)rows, (cuuint64_t)a.Hkv, (cuuint64_t)a.num_pages};
-    auto stride = [](int64_t st) { return (cuuint64_t)(st > 0 ? st : 16); };            // (0: a dimension of one)
-    const cuuint64_t strides[3] = {stride(a.row_st), stride(a.head_st), stride(a.page_st)};
-    const cuuint32_t box[4] = {(cuuint32_t)(e4m3 ? a.D : 64), (cuuint32_t)rows, 1, 1};
-    const cuuint32_t estr[4] = {1, 1, 1, 1};
-    return encode(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base, dims, strides, box, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, e4m3 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 cudaError_t launch_paged_tc(const PagedArgs& args, bool e4m3, int num_sms, PagedEncode encode, cudaStream_t stream)
 {
     PagedArgs a = args;
@@ -650,7 +709,10 @@ cudaError_t launch_paged_tc(const PagedArgs& args, bool e4m3, int num_sms, Paged
     a.nsplit = 1;
     while (a.nsplit < kPtMaxSplit && units * a.nsplit * 2 <= num_sms && key_tiles >= 4 * a.nsplit) a.nsplit *= 2;
     PagedMaps maps;
-    if (!encode_pages(encode, &maps.k, a.kp, a, e4m3) || !encode_pages(encode, &maps.v, a.vp, a, e4m3)) return cudaErrorInvalidValue;
+    const int box_bytes = e4m3 ? a.D : 128;
+    const CUtensorMapSwizzle swizzle = e4m3 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B;
+    if (!encode_pages(encode, &maps.k, a.kp, a, e4m3, box_bytes, 1 << a.page_shift, swizzle) || !encode_pages(encode, &maps.v, a.vp, a, e4m3, box_bytes, 1 << a.page_shift, swizzle))
+        return cudaErrorInvalidValue;
     cudaLaunchAttribute attr[2]{};
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;

@@ -217,6 +217,9 @@ __host__ __device__ constexpr uint32_t make_idesc_bf16(int M, int N, bool b_mn_m
            ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
+// The same for f16 A and B (formats 0)
+__host__ __device__ constexpr uint32_t make_idesc_f16(int M, int N, bool b_mn_major) { return make_idesc_bf16(M, N, b_mn_major) & ~((1u << 7) | (1u << 10)); }
+
 // Shared-memory matrix descriptor, 128-byte swizzle.  Fields: [0,14) start address >> 4;
 // [16,30) leading-dimension byte offset >> 4; [32,46) stride-dimension byte offset >> 4;
 // [46,48) descriptor version (1 on sm_100); [61,64) layout type (2 = 128-byte swizzle).
