@@ -244,39 +244,55 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                 if (alive) alive = __all_sync(0xffffffffu, bounded_wait(bar(Cfg::kRawFull + raw), raw_phase, abort_addr, a.status, kStatusWaitKvFull));
                 if (alive) alive = __all_sync(0xffffffffu, bounded_wait(empty, empty_parity, abort_addr, a.status, kStatusWaitKvEmpty));
                 if (!alive) return;
-                const uint32_t src = sRaw + raw * Cfg::kRawBytes + row * D;
+                // A warp takes its 32 rows four (D = 64: eight) at a time, 16 bytes a lane.  Lanes 0-3 of eight have a row's one half and
+                // lanes 4-7 the next row's other half: neither the reads nor the writes, whose 16-byte places are permuted by the
+                // row's last bits, meet in a bank.
+                const uint32_t src = sRaw + raw * Cfg::kRawBytes + (row & 96) * D;
+                constexpr int kStep = 512 / D;                      // rows of a step
+                const int r0 = D == 128 ? (lane >> 4) * 2 + (lane >> 2 & 1) : lane >> 2;
+                const int half = D == 128 ? (lane >> 3 & 1) ^ (lane >> 2 & 1) : 0, c = lane & 3;
+                const uint32_t at = src + r0 * D + half * 64 + c * 16, to = dst + half * 16384 + ((row & 96) + r0) * 128;
+                const bool all = __all_sync(0xffffffffu, f != 0xffffffffu);
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    const int c = (i + row) & (D / 16 - 1);         // neighbouring rows start at different banks
-                    const uint32_t d = dst + (c >> 2) * 16384 + row * 128;
-                    uint32_t z[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
-                    if (f != 0xffffffffu) {
-                        const uint4 y = pt_ld_shared4(src + c * 16);
-                        const uint32_t yw[4] = {y.x, y.y, y.z, y.w};
+                for (int i = 0; i < 32 / kStep; ++i) {
+                    const uint4 y = pt_ld_shared4(at + i * kStep * D);
+                    const uint32_t g = __shfl_sync(0xffffffffu, f, r0 + i * kStep);
+                    const uint32_t yw[4] = {y.x, y.y, y.z, y.w};
+                    uint32_t z[8];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            e4m3x4_to_f16(yw[e], z[2 * e], z[2 * e + 1]);
-                            z[2 * e] = mul_f16x2(z[2 * e], f); z[2 * e + 1] = mul_f16x2(z[2 * e + 1], f);
-                        }
+                    for (int e = 0; e < 4; ++e) {
+                        e4m3x4_to_f16(yw[e], z[2 * e], z[2 * e + 1]);
+                        z[2 * e] = mul_f16x2(z[2 * e], g); z[2 * e + 1] = mul_f16x2(z[2 * e + 1], g);
                     }
-                    pt_st_shared4(d + ((((c & 3) * 2) ^ (row & 7)) << 4), z[0], z[1], z[2], z[3]);
-                    pt_st_shared4(d + ((((c & 3) * 2 + 1) ^ (row & 7)) << 4), z[4], z[5], z[6], z[7]);
+                    if (!all && g == 0xffffffffu) {                 // nobody sees the row: it may hold anything
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) z[e] = 0u;
+                    }
+                    const int x = (r0 + i * kStep) & 7;
+                    pt_st_shared4(to + i * kStep * 128 + (((c * 2) ^ x) << 4), z[0], z[1], z[2], z[3]);
+                    pt_st_shared4(to + i * kStep * 128 + (((c * 2 + 1) ^ x) << 4), z[4], z[5], z[6], z[7]);
                 }
                 fence_proxy_async();
                 __syncwarp();
                 if (lane == 0) { mbar_arrive(full); mbar_arrive(bar(Cfg::kRawEmpty + raw)); }
                 if (++raw == Cfg::kStagesRaw) { raw = 0; raw_phase ^= 1u; }
             };
-            uint32_t fk, fv;
+            // K a tile ahead of V: a K stage is free as soon as its scores are loaded, a V stage only after the product behind the
+            // softmax, and the next scores must not wait for that
+            uint32_t fk, fv, fv_before = 0;
             scales(w.j0, fk, fv);
-            for (int j = w.j0; j < w.j1 && alive; ++j) {
+            for (int j = w.j0; j <= w.j1 && T > 0 && alive; ++j) {
                 uint32_t nk, nv;
                 scales(j + 1, nk, nv);
-                convert(bar(Cfg::kKFull + k_stage), bar(Cfg::kKEmpty + k_stage), k_phase ^ 1u, sK + k_stage * Cfg::kTileBytes, fk);
-                if (++k_stage == Cfg::kStagesK) { k_stage = 0; k_phase ^= 1u; }
-                convert(bar(Cfg::kVFull + v_stage), bar(Cfg::kVEmpty + v_stage), v_phase ^ 1u, sV + v_stage * Cfg::kTileBytes, fv);
-                if (++v_stage == Cfg::kStagesV) { v_stage = 0; v_phase ^= 1u; }
-                fk = nk; fv = nv;
+                if (j < w.j1) {
+                    convert(bar(Cfg::kKFull + k_stage), bar(Cfg::kKEmpty + k_stage), k_phase ^ 1u, sK + k_stage * Cfg::kTileBytes, fk);
+                    if (++k_stage == Cfg::kStagesK) { k_stage = 0; k_phase ^= 1u; }
+                }
+                if (j > w.j0) {
+                    convert(bar(Cfg::kVFull + v_stage), bar(Cfg::kVEmpty + v_stage), v_phase ^ 1u, sV + v_stage * Cfg::kTileBytes, fv_before);
+                    if (++v_stage == Cfg::kStagesV) { v_stage = 0; v_phase ^= 1u; }
+                }
+                fv_before = fv; fk = nk; fv = nv;
             }
             if (a.nsplit > 1) { __syncwarp(); cluster_arrive(); cluster_wait(); cluster_arrive(); cluster_wait(); }
         }
@@ -307,10 +323,12 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
             int stage = 0;
             uint32_t phase = 0, armed_mask = 0, armed_parity = 0;
             bool alive = true;
-            int page = find(w.j0);
-            for (int j = w.j0; j < w.j1 && alive; ++j) {
+            int page = find(w.j0), page_before = 0;
+            // (e4m3: K a tile ahead of V, as the converting warps take them)
+            for (int j = w.j0; j < w.j1 + (E4M3 && T > 0 ? 1 : 0) && alive; ++j) {
                 const int next = find(j + 1);
                 for (int u = 0; u < (E4M3 ? 2 : 1) && alive; ++u) {
+                    if (E4M3 && (u == 0 ? j == w.j1 : j == w.j0)) continue;
                     const uint32_t full = full0 + 8u * stage;
                     alive = __all_sync(0xffffffffu, bounded_wait(empty0 + 8u * stage, phase ^ 1u, abort_addr, a.status, kStatusWaitKvEmpty));
                     if (!alive) break;
@@ -322,7 +340,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                         const CUtensorMap* map = is_v || u == 1 ? &maps.v : &maps.k;
                         const uint32_t rows0 = (uint32_t)lane << a.page_shift;
                         if constexpr (E4M3) {
-                            tma_load_4d(ring + stage * kBytes + rows0 * D, map, full, 0, 0, hk, page);
+                            tma_load_4d(ring + stage * kBytes + rows0 * D, map, full, 0, 0, hk, u == 1 ? page_before : page);
                         } else {
 #pragma unroll
                             for (int h = 0; h < Cfg::kHalves; ++h) tma_load_4d(ring + stage * kBytes + h * 16384 + rows0 * 128, map, full, h * 64, 0, hk, page);
@@ -330,6 +348,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                     }
                     if (++stage == stages) { stage = 0; phase ^= 1u; }
                 }
+                page_before = page;
                 page = next;
             }
             if (ld_shared_u32(abort_addr) != 0u) {           // leave no copy in flight behind
