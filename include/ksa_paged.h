@@ -32,8 +32,8 @@
  *   lse    : fp32 [num_q_heads, num_rows], natural log of the softmax denominator
  *   text_table : int32 [batch, text_cols]   summ_table : int32 [batch, summ_cols]   cached : int32 [batch]
  *   cu_rows : int32 [batch + 1], ascending, from 0 to at most num_rows; a sequence has at most 2^30 rows
- * Nothing is allocated, no workspace is needed, nothing synchronises the host; calls on different streams are independent
- * as far as their tensors are.
+ * Nothing is allocated, nothing synchronises the host; calls on different streams are independent as far as their tensors
+ * and workspaces are.
  *
  * What only the device can see is reported through ksa_last_device_status: a row that the call needs lies in no page
  * (an entry outside 0 .. num_pages - 1, or a column past the table): KSA_PAGED_STATUS_BAD_PAGE; cu_rows or cached that
@@ -94,7 +94,13 @@ int ksa_paged_gather(ksa_ctx* ctx, const ksa_paged_kv* kv, void* k, void* v, con
  * does not matter; rows that one of the call's rows sees must be finite (or NaN reaches rows of the same sequence that do
  * not see them).
  */
-int ksa_paged_attn(ksa_ctx* ctx, const ksa_paged_kv* kv, const void* q, void* out, float* lse, const ksa_paged_params* p, void* cuda_stream);
+int ksa_paged_attn(ksa_ctx* ctx, const ksa_paged_kv* kv, const void* q, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                   const ksa_paged_params* p, void* cuda_stream);
+/* Bytes of DEVICE workspace, 256-byte aligned, with which ksa_paged_attn is faster for p: 0 but for calls of many rows a sequence
+ * over an e4m3 cache (then room for the rows in view as bf16; of p the strides do not matter).  The workspace is scratch
+ * for the length of the call, and other work must not use it meanwhile; without one (NULL, or smaller) the call works all the
+ * same, and its results differ in the order of roundings only. */
+int ksa_paged_workspace_bytes(const ksa_paged_params* p, size_t* bytes);
 
 #define KSA_PAGED_STATUS_BAD_PAGE  103   /* a row that a call needs lies in no page of the pool */
 #define KSA_PAGED_STATUS_BAD_ROWS  104   /* cu_rows or cached are no lengths */

@@ -45,7 +45,7 @@ EXPORTS = [
     "ksa_anneal_lambda", "ksa_position_ids", "ksa_total_summary_rows", "ksa_qkv_prepare",
     "ksa_prepared_workspace_bytes", "ksa_attn_fwd_prepared",
     "ksa_part_rows", "ksa_attn_fwd_part",
-    "ksa_paged_append", "ksa_paged_gather", "ksa_paged_attn",
+    "ksa_paged_append", "ksa_paged_gather", "ksa_paged_attn", "ksa_paged_workspace_bytes",
 ]
 
 
@@ -162,7 +162,8 @@ def lib():
     L.ksa_decode_summary.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, cp, vp]
     L.ksa_paged_append.argtypes = [vp, vp, vp, vp, vp, vp]      # (structures: by reference, or packed as bytes)
     L.ksa_paged_gather.argtypes = [vp, vp, vp, vp, vp, vp]
-    L.ksa_paged_attn.argtypes = [vp, vp, vp, vp, vp, vp, vp]
+    L.ksa_paged_attn.argtypes = [vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp, vp]
+    L.ksa_paged_workspace_bytes.argtypes = [vp, ctypes.POINTER(ctypes.c_size_t)]
     L.ksa_strerror.restype = ctypes.c_char_p
     L.ksa_strerror.argtypes = [ctypes.c_int]
     _lib = L
@@ -640,6 +641,7 @@ class PagedCache:
         self._bf16, self._f32, self._index = torch.bfloat16, torch.float32, self.kpages.get_device()
         self._fixed = (s.k, s.m, s.C, s.Hq, s.Hkv, s.D, s.scale, s.flags, KSA_KV_E4M3 if s.fmt == "e4m3" else KSA_KV_BF16, s.page_rows, s.num_pages)
         self._strides = self.kpages.stride()[:3]
+        self._quantised = s.fmt == "e4m3"
         self._pools = tuple(0 if t is None else t.data_ptr() for t in self._tensors)
 
     def _rows(self, t, rows: int, H: int):
@@ -650,32 +652,53 @@ class PagedCache:
             raise ValueError("rows must be bf16 [num_rows, heads, head_dim] = %s on cuda:%d, head_dim contiguous" % ((rows, H, D), self._index))
         return st[0] if rows > 1 else H * D, st[1] if H > 1 else D
 
-    def _call(self, fn, name: str, batch: PagedBatch, rows: int, q, k, v, o, stream, *tensors):
-        # (Both structures are packed as bytes: this runs in every call, and a call of one token takes the device some 6 us.)
-        if batch._index != self._index or (batch._cols[1] == 0 and self.spec.m > 0):
+    def _params(self, batch: PagedBatch, rows: int, q, k, v, o) -> bytes:
+        # (The structures are packed as bytes: this runs in every call, and a call of one token takes the device some 6 us.)
+        if batch._index != self._index or (batch._cols[1] == 0 and self._spec.m > 0):
             raise ValueError("the batch must be on cuda:%d, with a summ_table" % self._index)
-        p = _PAGED_PARAMS.pack(_PAGED_PARAMS.size, batch._size, rows, *self._fixed, *batch._cols, *self._strides, *q, *k, *v, *o)
-        _check(fn(self.ctx.handle, _PAGED_KV.pack(*self._pools, *batch._ptrs), *tensors, p, _current_stream(self.device) if stream is None else stream), name)
+        return _PAGED_PARAMS.pack(_PAGED_PARAMS.size, batch._size, rows, *self._fixed, *batch._cols, *self._strides, *q, *k, *v, *o)
+
+    def _kv(self, batch: PagedBatch) -> bytes:
+        return _PAGED_KV.pack(*self._pools, *batch._ptrs)
+
+    def _move(self, fn, name: str, batch: PagedBatch, k, v, stream):
+        rows, H = k.shape[0], self._spec.Hkv
+        p = self._params(batch, rows, _NO_ROWS, self._rows(k, rows, H), self._rows(v, rows, H), _NO_ROWS)
+        _check(fn(self.ctx.handle, self._kv(batch), k.data_ptr(), v.data_ptr(), p, _current_stream(self.device) if stream is None else stream), name)
+
+    def _workspace(self, p: bytes, stream):
+        """The workspace that makes the call faster, from torch's allocator (which keeps it until the work before its next use
+        on the stream is done, in a captured call as long as the graph lives), or None."""
+        import torch
+        n = ctypes.c_size_t()
+        _check(lib().ksa_paged_workspace_bytes(p, ctypes.byref(n)), "ksa_paged_workspace_bytes")
+        if n.value == 0:
+            return None
+        ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        if stream is not None and stream != _current_stream(self.device):
+            ws.record_stream(torch.cuda.ExternalStream(stream, device=self.device))
+        return ws
 
     def append(self, batch: PagedBatch, k, v, stream: Optional[int] = None):
         """ksa_paged_append: k, v [num_rows, Hkv, D] of the batch's new rows into their pages (quantised on the way)."""
-        rows, H = k.shape[0], self.spec.Hkv
-        self._call(lib().ksa_paged_append, "ksa_paged_append", batch, rows, _NO_ROWS, self._rows(k, rows, H), self._rows(v, rows, H), _NO_ROWS, stream,
-                   k.data_ptr(), v.data_ptr())
+        self._move(lib().ksa_paged_append, "ksa_paged_append", batch, k, v, stream)
 
     def gather(self, batch: PagedBatch, k, v, stream: Optional[int] = None):
         """ksa_paged_gather: the rows cached[b] .. of every sequence back into k, v [num_rows, Hkv, D]."""
-        rows, H = k.shape[0], self.spec.Hkv
-        self._call(lib().ksa_paged_gather, "ksa_paged_gather", batch, rows, _NO_ROWS, self._rows(k, rows, H), self._rows(v, rows, H), _NO_ROWS, stream,
-                   k.data_ptr(), v.data_ptr())
+        self._move(lib().ksa_paged_gather, "ksa_paged_gather", batch, k, v, stream)
 
-    def attn(self, batch: PagedBatch, q, out, lse, stream: Optional[int] = None):
-        """ksa_paged_attn: q, out [num_rows, Hq, D], lse fp32 [Hq, num_rows]; the rows' own K and V have been appended."""
-        rows, H = q.shape[0], self.spec.Hq
+    def attn(self, batch: PagedBatch, q, out, lse, stream: Optional[int] = None, workspace=None):
+        """ksa_paged_attn: q, out [num_rows, Hq, D], lse fp32 [Hq, num_rows]; the rows' own K and V have been appended.
+        workspace: a uint8 CUDA tensor of ksa_paged_workspace_bytes; None: allocated here where it makes the call faster."""
+        rows, H = q.shape[0], self._spec.Hq
         if lse.shape != (H, rows) or lse.dtype is not self._f32 or lse.get_device() != self._index or not lse.is_contiguous():
             raise ValueError("lse must be contiguous fp32 [heads, num_rows] = %s on cuda:%d" % ((H, rows), self._index))
-        self._call(lib().ksa_paged_attn, "ksa_paged_attn", batch, rows, self._rows(q, rows, H), _NO_ROWS, _NO_ROWS, self._rows(out, rows, H), stream,
-                   q.data_ptr(), out.data_ptr(), lse.data_ptr())
+        p = self._params(batch, rows, self._rows(q, rows, H), _NO_ROWS, _NO_ROWS, self._rows(out, rows, H))
+        if workspace is None and self._quantised and rows > batch._size:
+            workspace = self._workspace(p, stream)
+        ws, nbytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+        _check(lib().ksa_paged_attn(self.ctx.handle, self._kv(batch), q.data_ptr(), out.data_ptr(), lse.data_ptr(), ws, nbytes, p,
+                                    _current_stream(self.device) if stream is None else stream), "ksa_paged_attn")
 
 
 _PAGED_PARAMS = struct.Struct("@9i f I 5i 11q")      # ksa_paged_params

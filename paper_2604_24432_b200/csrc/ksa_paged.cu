@@ -4,6 +4,8 @@
 // bf16 each, K and V of it at once; the row's sequence, page and place in the page are worked out by every lane for itself.
 #include <cuda_bf16.h>
 
+#include <algorithm>
+
 #include "ksa_host.h"
 #include "ksa_launch.h"
 #include "ksa_paged.h"
@@ -164,6 +166,84 @@ __global__ void __launch_bounds__(kRowThreads) ksa_paged_gather_kernel(PagedArgs
     *reinterpret_cast<uint4*>(a.v + i * a.v_st + h * a.v_sh + lane * 8) = xv;
 }
 
+// ---- e4m3 rows in view as bf16 pages of 128 rows ----------------------------------------------------------------------------
+// For calls with many query rows a sequence: the attention kernel on bf16 pages converts nothing, while the one on e4m3
+// pages converts a key tile again for every 256 query rows.  One block per page of the copy (128 text tokens or summaries from a
+// multiple of 128) and KV head; the copy's page tables are written on the way.  Only rows that some row of the call sees are
+// read (and their pages looked up); the others' places stay as they are, as in any page.
+struct UnpackArgs {
+    uint16_t* k; uint16_t* v;                        // [batch * seq_pages][Hkv][128][D]
+    int32_t* text_table; int32_t* summ_table;        // [batch][text_cols], [batch][summ_cols]
+    int32_t text_cols, summ_cols, text_pages, seq_pages;     // text_pages: of a sequence, before its pages of summaries
+};
+
+template <int D>
+__global__ void __launch_bounds__(kRowThreads) ksa_paged_unpack_kernel(PagedArgs a, UnpackArgs u)
+{
+    constexpr int kLanes = D / 16, kRowsPass = kRowThreads / kLanes;
+    ptx::pdl_launch_dependents();
+    ptx::pdl_wait();
+    const int b = blockIdx.z, h = blockIdx.y, slot = blockIdx.x;
+    int n, first;
+    if (!paged_seq(a, __ldcg(a.cu + b), __ldcg(a.cu + b + 1), b, n, first) || n == 0) return;
+    const bool summ = slot >= u.text_pages;
+    const PagedRange see = paged_range(a, first, n, summ);
+    const int tile = summ ? slot - u.text_pages : see.lo / 128 + slot, x0 = tile * 128;
+    if (x0 >= see.hi || x0 + 128 <= see.lo || tile >= (summ ? u.summ_cols : u.text_cols)) return;
+    const int page = b * u.seq_pages + slot;
+    if (h == 0 && threadIdx.x == 0) (summ ? u.summ_table : u.text_table)[(int64_t)b * (summ ? u.summ_cols : u.text_cols) + tile] = page;
+    const int lane = threadIdx.x % kLanes;
+#pragma unroll 4
+    for (int r = threadIdx.x / kLanes; r < 128; r += kRowsPass) {
+        const int x = x0 + r;
+        if (x < see.lo || x >= see.hi || (x >= see.gap_lo && x < see.gap_hi)) continue;
+        const int from = paged_page(a, b, summ, x);
+        if (from < 0) {
+            atomicCAS(a.status, 0, KSA_PAGED_STATUS_BAD_PAGE);
+            continue;
+        }
+        const int in = x & ((1 << a.page_shift) - 1);
+        const int64_t at = from * a.page_st + h * a.head_st + in * a.row_st + lane * 16, se = (((int64_t)from * a.Hkv + h) << a.page_shift) + in;
+        const uint4 yk = __ldcg(reinterpret_cast<const uint4*>(a.kp + at)), yv = __ldcg(reinterpret_cast<const uint4*>(a.vp + at));
+        const float fk = e8m0_scale(__ldcg(a.ke + se)), fv = e8m0_scale(__ldcg(a.ve + se));
+        const int64_t to = (((int64_t)page * a.Hkv + h) * 128 + r) * D + lane * 16;
+        auto put = [](uint16_t* dst, const uint4& y, float f) {
+            uint4 z[2];
+            uint32_t* w = reinterpret_cast<uint32_t*>(z);
+            const uint32_t yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 p = e4m3x2_to_f32(yw[i] & 0xffffu), q = e4m3x2_to_f32(yw[i] >> 16);
+                w[2 * i] = ptx::pack_bf16x2(p.x * f, p.y * f); w[2 * i + 1] = ptx::pack_bf16x2(q.x * f, q.y * f);
+            }
+            reinterpret_cast<uint4*>(dst)[0] = z[0]; reinterpret_cast<uint4*>(dst)[1] = z[1];
+        };
+        put(u.k + to, yk, fk);
+        put(u.v + to, yv, fv);
+    }
+}
+
+// Where things stand in the workspace of a call, and its size; 0 bytes where the call makes no copy.
+struct UnpackLayout { int64_t text_cols, summ_cols, text_pages, seq_pages, kv_bytes, tables, bytes; };
+static UnpackLayout unpack_layout(const ksa_paged_params* p)
+{
+    UnpackLayout l{};
+    const int64_t G = p->num_q_heads / p->num_kv_heads;
+    // From 2,048 query rows (eight tiles of 256) a sequence on: converting a key tile once costs as much as converting it in three to
+    // four query tiles, and a launch
+    if (p->kv_format != KSA_KV_E4M3 || p->num_rows * G < 2048 * (int64_t)p->batch) return l;
+    const int64_t text = (int64_t)p->text_cols * p->page_rows, summ = p->summaries_per_chunk > 0 ? (int64_t)p->summ_cols * p->page_rows : 0;
+    l.text_cols = (text + 127) / 128; l.summ_cols = (summ + 127) / 128;
+    const int64_t seen = ((int64_t)p->window_chunks + 2) * p->chunk_len + p->num_rows;        // text tokens in view, at most
+    l.text_pages = std::min(l.text_cols, seen / 128 + 2);
+    l.seq_pages = l.text_pages + l.summ_cols;
+    l.kv_bytes = p->batch * l.seq_pages * p->num_kv_heads * 128 * p->head_dim * 2;
+    l.tables = 2 * l.kv_bytes;
+    l.bytes = l.tables + (l.text_cols + l.summ_cols) * p->batch * 4;
+    if (l.bytes > (2ll << 30) || p->batch * l.seq_pages > (1 << 30)) return UnpackLayout{};
+    return l;
+}
+
 template <class K>
 static cudaError_t launch_rows(K kernel, const PagedArgs& a, cudaStream_t stream)
 {
@@ -190,9 +270,9 @@ using namespace ksa;
 
 #define KSA_API extern "C" __attribute__((visibility("default")))
 
-static int validate_paged(const ksa_paged_params* p, const ksa_paged_kv* kv)
+static int validate_shape(const ksa_paged_params* p)
 {
-    if (!p || p->struct_size != (int32_t)sizeof(ksa_paged_params) || !kv) return KSA_ERR_INVALID_ARG;
+    if (!p || p->struct_size != (int32_t)sizeof(ksa_paged_params)) return KSA_ERR_INVALID_ARG;
     if (p->batch < 1 || p->num_rows < 0 || p->chunk_len < 1 || p->summaries_per_chunk < 0 || p->window_chunks < 0) return KSA_ERR_INVALID_ARG;
     if (p->num_q_heads < 1 || p->num_kv_heads < 1 || p->num_q_heads % p->num_kv_heads != 0) return KSA_ERR_INVALID_ARG;
     if (!(p->softmax_scale > 0.f) || p->softmax_scale > 1e30f) return KSA_ERR_INVALID_ARG;
@@ -209,6 +289,14 @@ static int validate_paged(const ksa_paged_params* p, const ksa_paged_kv* kv)
         if (st >= (1ll << 38)) return KSA_ERR_UNSUPPORTED;
     }
     if (p->row_stride < p->head_dim) return KSA_ERR_INVALID_ARG;
+    return KSA_OK;
+}
+
+static int validate_paged(const ksa_paged_params* p, const ksa_paged_kv* kv)
+{
+    const int rc = validate_shape(p);
+    if (rc != KSA_OK) return rc;
+    if (!kv) return KSA_ERR_INVALID_ARG;
     auto misaligned = [](const void* q) { return ((uintptr_t)q & 15) != 0; };
     if (!kv->kpages || !kv->vpages || misaligned(kv->kpages) || misaligned(kv->vpages)) return KSA_ERR_INVALID_ARG;
     if (p->kv_format == KSA_KV_E4M3 && (!kv->kscale || !kv->vscale || misaligned(kv->kscale) || misaligned(kv->vscale))) return KSA_ERR_INVALID_ARG;
@@ -287,23 +375,55 @@ KSA_API int ksa_paged_gather(ksa_ctx* ctx, const ksa_paged_kv* kv, void* k, void
     return paged_call(ctx, p, [&] { return launch_paged_gather(a, p->kv_format == KSA_KV_E4M3, (cudaStream_t)cuda_stream); });
 }
 
-KSA_API int ksa_paged_attn(ksa_ctx* ctx, const ksa_paged_kv* kv, const void* q, void* out, float* lse, const ksa_paged_params* p, void* cuda_stream)
+KSA_API int ksa_paged_workspace_bytes(const ksa_paged_params* p, size_t* bytes)
+{
+    if (!bytes) return KSA_ERR_INVALID_ARG;
+    const int rc = validate_shape(p);
+    if (rc != KSA_OK) return rc;
+    *bytes = (size_t)unpack_layout(p).bytes;
+    return KSA_OK;
+}
+
+KSA_API int ksa_paged_attn(ksa_ctx* ctx, const ksa_paged_kv* kv, const void* q, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                           const ksa_paged_params* p, void* cuda_stream)
 {
     const int rc = validate_paged(p, kv);
     if (rc != KSA_OK) return rc;
     if (!ctx || !tensor_ok(q, p->q_stride_tok, p->q_stride_head) || !tensor_ok(out, p->o_stride_tok, p->o_stride_head) || !lse || ((uintptr_t)lse & 3)) return KSA_ERR_INVALID_ARG;
+    if (workspace && ((uintptr_t)workspace & 255)) return KSA_ERR_INVALID_ARG;
     PagedArgs a = paged_args(ctx, kv, p);
     a.q = (const uint16_t*)q; a.out = (uint16_t*)out; a.lse = lse;
+    bool e4m3 = p->kv_format == KSA_KV_E4M3;
     return paged_call(ctx, p, [&]() -> cudaError_t {
         bool& ready = *ksa_ctx_paged_ready(ctx);                // shared-memory opt-in: a per-device setting
+        const PagedEncode encode = (PagedEncode)ksa_ctx_encode_tiled(ctx);
+        const cudaStream_t stream = (cudaStream_t)cuda_stream;
+        cudaError_t e = cudaSuccess;
         if (!ready) {
-            cudaError_t e = setup_paged_attn();
+            e = setup_paged_attn();
             if (e == cudaSuccess) e = setup_paged_tc();
             if (e != cudaSuccess) return e;
             ready = true;
         }
-        if ((int64_t)a.rows * a.G > 16 * (int64_t)a.B)
-            return launch_paged_tc(a, p->kv_format == KSA_KV_E4M3, ksa_ctx_num_sms(ctx), (PagedEncode)ksa_ctx_encode_tiled(ctx), (cudaStream_t)cuda_stream);
-        return launch_paged_attn(a, p->kv_format == KSA_KV_E4M3, ksa_ctx_num_sms(ctx), (PagedEncode)ksa_ctx_encode_tiled(ctx), (cudaStream_t)cuda_stream);
+        // up to 16 query rows a sequence: as many as the mma.sync kernel's tiles hold
+        if ((int64_t)a.rows * a.G <= 16 * (int64_t)a.B) return launch_paged_attn(a, e4m3, ksa_ctx_num_sms(ctx), encode, stream);
+        const UnpackLayout l = unpack_layout(p);
+        if (l.bytes > 0 && workspace && workspace_bytes >= (size_t)l.bytes) {
+            UnpackArgs u{};
+            u.k = (uint16_t*)workspace; u.v = u.k + l.kv_bytes / 2;
+            u.text_table = (int32_t*)((char*)workspace + l.tables); u.summ_table = u.text_table + l.text_cols * a.B;
+            u.text_cols = (int32_t)l.text_cols; u.summ_cols = (int32_t)l.summ_cols; u.text_pages = (int32_t)l.text_pages; u.seq_pages = (int32_t)l.seq_pages;
+            e = launch_dependent(a.D == 128 ? ksa_paged_unpack_kernel<128> : ksa_paged_unpack_kernel<64>,
+                                 dim3((unsigned)l.seq_pages, (unsigned)a.Hkv, (unsigned)a.B), kRowThreads, 0, stream, a, u);
+            if (e != cudaSuccess) return e;
+            ksa_ctx_add_launches(ctx, 1);
+            // from here on the cache is the copy
+            a.kp = (uint8_t*)u.k; a.vp = (uint8_t*)u.v; a.ke = a.ve = nullptr;
+            a.text_table = u.text_table; a.summ_table = u.summ_table; a.text_cols = u.text_cols; a.summ_cols = u.summ_cols;
+            a.page_shift = 7; a.num_pages = (int32_t)(a.B * l.seq_pages);
+            a.row_st = a.D * 2; a.head_st = 128 * a.row_st; a.page_st = a.Hkv * a.head_st;
+            e4m3 = false;
+        }
+        return launch_paged_tc(a, e4m3, ksa_ctx_num_sms(ctx), encode, stream);
     });
 }

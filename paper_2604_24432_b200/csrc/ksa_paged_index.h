@@ -80,4 +80,31 @@ template <class A> KSA_HD PagedView paged_tile_view(const A& a, const PagedTile&
     return PagedView{lo.t_lo, hi.t_hi, lo.s_lo, hi.s_hi > lo.s_lo && !none ? hi.s_hi : lo.s_lo};
 }
 
+// What the rows [first, first + n) of a sequence, n >= 1, see of its text (summaries): [lo, hi) but for [gap_lo, gap_hi).
+struct PagedRange { int lo, hi, gap_lo, gap_hi; };
+template <class A> KSA_HD PagedRange paged_range(const A& a, int first, int n, bool summ)
+{
+    const int t0 = paged_texts(a, first), t1 = paged_texts(a, first + n), s0 = first - t0, s1 = first + n - t1;
+    const bool texts = t1 > t0, summs = s1 > s0;
+    PagedRange r{0, 0, 0, 0};
+    if (!summ) {
+        const PagedView x = paged_view(a, !texts, texts ? t0 : s0);
+        r.lo = x.t_lo;
+        if (texts && summs) {                          // a first summary's chunk may start before the first text token's window
+            const int lo = paged_view(a, true, s0).t_lo;
+            if (lo < r.lo) r.lo = lo;
+        }
+        r.hi = t1;                                     // (the chunk of the last summary has ended before)
+    } else {
+        if (texts) r.hi = paged_view(a, false, t1 - 1).s_hi;
+        if (summs && !(a.flags & KSA_FLAG_SUMMARY_TEXT_ONLY)) {
+            const int lo = paged_view(a, true, s0).s_lo;
+            if (!texts || r.hi == 0) r.lo = lo;
+            else if (lo > r.hi) { r.gap_lo = r.hi; r.gap_hi = lo; }
+            if (s1 > r.hi) r.hi = s1;
+        }
+    }
+    return r;
+}
+
 }  // namespace ksa

@@ -72,12 +72,12 @@ class Server:
         """Everything before the spans' rows, and those, in one call."""
         self.append([(0, a + n) for a, n in spans])
 
-    def attn(self, spans, pad=0, batch=None, q=None):
+    def attn(self, spans, pad=0, batch=None, q=None, **how):
         q = self.rows(self.q, spans, pad) if q is None else q
         out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV)
         lse = torch.full((self.Hq, q.shape[0]), -1.0, device=DEV)
         self.ctx.clear_device_status()
-        self.cache.attn(batch or self.batch(spans), q, out, lse)
+        self.cache.attn(batch or self.batch(spans), q, out, lse, **how)
         torch.cuda.synchronize()
         assert self.ctx.device_status() == 0
         return out, lse
@@ -256,6 +256,34 @@ def test_peaked_and_spread_scores(ctx, fmt, n):
     s.fill(spans)
     out, lse = s.attn(spans)
     s.check(out, lse, spans, sample=25)
+
+
+@pytest.mark.parametrize("k,m,C,Hq,Hkv,D,ps,flags,spans,pad", [
+    (8, 1, 9, 16, 4, 128, 64, 0, [(2003, 700)], 0),
+    (8, 1, 9, 8, 1, 64, 16, 0, [(77, 800), (0, 0), (1500, 300)], 3),
+    (64, 8, 1, 16, 4, 128, 32, ksa.KSA_FLAG_SUMMARY_TEXT_ONLY, [(500, 530)], 0),
+    (64, 8, 2, 16, 2, 64, 128, 0, [(66, 330), (70, 300)], 0),
+    (8, 0, 1 << 20, 16, 4, 128, 64, 0, [(300, 520)], 0),
+    (8, 1, 0, 32, 4, 128, 16, 0, [(9, 300)], 0),
+])
+def test_long_runs_over_e4m3(ctx, k, m, C, Hq, Hkv, D, ps, flags, spans, pad):
+    """With the workspace (the rows in view as bf16 pages) and without: each against the reference.  Pages before every window are
+    given back, and whatever nobody sees is NaN; so is the workspace."""
+    s = Server(ctx, k, m, C, Hq, Hkv, D, ps, "e4m3", [a + n + 7 for a, n in spans], flags, seed=19)
+    s.fill(spans)
+    for b, (a, n) in enumerate(spans):
+        s.text[b, :max(0, a // (k + m) - C) * k // ps] = -1
+    batch = s.batch(spans)
+    p = s.cache._params(batch, sum(n for _, n in spans) + pad, (0, 0), (0, 0), (0, 0), (0, 0))
+    ws = s.cache._workspace(p, None)
+    assert ws is not None
+    ws.fill_(255)                                             # (as bf16: NaN)
+    before = ctx.launch_count()
+    for how, launches in ((dict(workspace=ws), 2), (dict(workspace=ws[:256]), 1), (dict(), 2)):
+        out, lse = s.attn(spans, pad, **how)
+        assert ctx.launch_count() == before + launches
+        before += launches
+        s.check(out, lse, spans, sample=24)
 
 
 def test_strided_pools_and_rows(ctx):

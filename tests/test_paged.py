@@ -23,6 +23,7 @@ int entry(const Shape* a, int e) { return ksa::paged_entry(*a, e); }
 int lengths_ok(const Shape* a, int row0, int r1, int first) { return ksa::paged_lengths_ok(*a, row0, r1, first); }
 void view(const Shape* a, int summ, int x, int* v) { auto w = ksa::paged_view(*a, summ, x); v[0] = w.t_lo; v[1] = w.t_hi; v[2] = w.s_lo; v[3] = w.s_hi; }
 void tile_view(const Shape* a, int summ, int x0, int n, int* v) { ksa::PagedTile t{0, summ != 0, x0, n, 0, 0}; auto w = ksa::paged_tile_view(*a, t); v[0] = w.t_lo; v[1] = w.t_hi; v[2] = w.s_lo; v[3] = w.s_hi; }
+void range(const Shape* a, int first, int n, int summ, int* v) { auto r = ksa::paged_range(*a, first, n, summ != 0); v[0] = r.lo; v[1] = r.hi; v[2] = r.gap_lo; v[3] = r.gap_hi; }
 long long row(const Shape* a, int summ, int x, int row0, int first) { ksa::PagedTile t{0, summ != 0, 0, 0, row0, first}; return ksa::paged_row(*a, t, x); }
 }
 """
@@ -75,6 +76,42 @@ def test_rows_places_and_views(index, k, m, C, flags):
                 assert (summ == [] and out4[2] >= out4[3]) or (min(summ), max(summ) + 1) == (out4[2], out4[3])
 
 
+@pytest.mark.parametrize("k,m,C,flags", [(8, 1, 3, 0), (8, 1, 0, 0), (64, 8, 1, 0), (1, 1, 5, 0), (3, 2, 2, 1), (8, 0, 1 << 20, 0), (4, 0, 2, 0), (5, 3, 1, 0)])
+def test_what_a_run_of_rows_sees(index, k, m, C, flags):
+    a = Shape(k, m, C, 1 << 20, 10, flags)
+    rows = 5 * (k + m) * max(1, min(C, 3)) + 4
+    where = ref.places(k, m, rows)
+    sees = [ref.visible(k, m, C, i, rows, bool(flags & 1)) for i in range(rows)]
+    out4 = (ctypes.c_int * 4)()
+    for first in range(0, rows, max(1, rows // 60)):
+        for n in (1, 2, k, k + m, 3 * (k + m) + 1):
+            if first + n > rows:
+                continue
+            see = np.any(sees[first:first + n], axis=0)
+            for kind in (False, True):
+                index.range(ctypes.byref(a), first, n, int(kind), out4)
+                got = [x for x in range(out4[0], out4[1]) if not out4[2] <= x < out4[3]]
+                want = [w[1] for i, w in enumerate(where) if see[i] and w[0] == kind]
+                # (text between the windows of two rows that are far apart is no case: a run's windows overlap or touch)
+                assert got == want, (first, n, kind)
+
+
+def test_workspace_of_long_runs_over_e4m3():
+    def need(**change):
+        good = dict(struct_size=ctypes.sizeof(ksa.ksa_paged_params), batch=1, num_rows=1152, chunk_len=8, summaries_per_chunk=1, window_chunks=128,
+                    num_q_heads=32, num_kv_heads=8, head_dim=128, softmax_scale=0.1, flags=0, kv_format=ksa.KSA_KV_E4M3, page_rows=64,
+                    num_pages=7, text_cols=600, summ_cols=70, page_stride=65536, head_stride=8192, row_stride=128)
+        n = ctypes.c_size_t()
+        rc = ksa.lib().ksa_paged_workspace_bytes(ctypes.byref(ksa.ksa_paged_params(**{**good, **change})), ctypes.byref(n))
+        return n.value if rc == 0 else rc
+    pages = (130 * 8 + 1152) // 128 + 2 + 35
+    assert need() == 2 * pages * 8 * 128 * 128 * 2 + (300 + 35) * 4
+    assert need(num_rows=511) == need(batch=3) == need(kv_format=ksa.KSA_KV_BF16, page_stride=65536) == 0
+    assert need(text_cols=5, num_rows=512) == 2 * (3 + 35) * 8 * 128 * 128 * 2 + (3 + 35) * 4
+    assert need(window_chunks=1 << 30, chunk_len=8, summaries_per_chunk=0, summ_cols=0, text_cols=1 << 24) == 0       # over 2 GB: the cache itself
+    assert need(head_dim=96) == ksa.KSA_ERR_UNSUPPORTED
+
+
 def test_entries_and_lengths(index):
     a = Shape(8, 1, 3, 100, 10, 0)
     assert [index.entry(ctypes.byref(a), e) for e in (-1, 0, 9, 10, -2, 2**31 - 1, -2**31)] == [-1, 0, 9, -2, -2, -2, -2]
@@ -99,7 +136,7 @@ def _built():
     ksa_build.build()
 
 
-def _call(fn="append", kv_change=None, tensor_change=None, **change):
+def _call(fn="append", kv_change=None, tensor_change=None, ws=None, **change):
     """Status of a call with made-up (never touched) pointers and no context: what is wrong is said before anything else."""
     D, Hkv, Hq, ps = change.get("head_dim", 128), 2, 8, 64
     good = dict(struct_size=ctypes.sizeof(ksa.ksa_paged_params), batch=2, num_rows=5, chunk_len=8, summaries_per_chunk=1, window_chunks=4,
@@ -112,7 +149,7 @@ def _call(fn="append", kv_change=None, tensor_change=None, **change):
     x, y, z = {**dict(x=0x900000, y=0xA00000, z=0xB00000), **(tensor_change or {})}.values()
     L = ksa.lib()
     if fn == "attn":
-        return L.ksa_paged_attn(None, ctypes.byref(kv), x, y, z, ctypes.byref(p), None)
+        return L.ksa_paged_attn(None, ctypes.byref(kv), x, y, z, ws, 1 << 20, ctypes.byref(p), None)
     return getattr(L, "ksa_paged_" + fn)(None, ctypes.byref(kv), x, y, ctypes.byref(p), None)
 
 
@@ -138,14 +175,16 @@ def test_refusals(fn, change, want):
 
 @pytest.mark.parametrize("fn,change", [("append", dict(k_stride_tok=12)), ("append", dict(v_stride_head=-8)), ("gather", dict(k_stride_tok=1 << 38)),
                                        ("attn", dict(q_stride_tok=4)), ("attn", dict(o_stride_head=-8)), ("attn", dict(tensor_change=dict(z=None))),
-                                       ("attn", dict(tensor_change=dict(z=0xB00002)))])
+                                       ("attn", dict(tensor_change=dict(z=0xB00002))), ("attn", dict(ws=0xC00080))])
 def test_refusals_of_row_tensors(fn, change):
     assert _call(fn, **change) == BAD
 
 
 def test_null_structures():
     assert ksa.lib().ksa_paged_append(None, None, None, None, None, None) == BAD
-    assert ksa.lib().ksa_paged_attn(None, None, None, None, None, None, None) == BAD
+    assert ksa.lib().ksa_paged_attn(None, None, None, None, None, None, 0, None, None) == BAD
+    n = ctypes.c_size_t()
+    assert ksa.lib().ksa_paged_workspace_bytes(None, ctypes.byref(n)) == BAD
 
 
 def test_binding_refusals():
