@@ -192,34 +192,45 @@ __global__ void __launch_bounds__(kRowThreads) ksa_paged_unpack_kernel(PagedArgs
     if (x0 >= see.hi || x0 + 128 <= see.lo || tile >= (summ ? u.summ_cols : u.text_cols)) return;
     const int page = b * u.seq_pages + slot;
     if (h == 0 && threadIdx.x == 0) (summ ? u.summ_table : u.text_table)[(int64_t)b * (summ ? u.summ_cols : u.text_cols) + tile] = page;
-    const int lane = threadIdx.x % kLanes;
-#pragma unroll 4
-    for (int r = threadIdx.x / kLanes; r < 128; r += kRowsPass) {
-        const int x = x0 + r;
-        if (x < see.lo || x >= see.hi || (x >= see.gap_lo && x < see.gap_hi)) continue;
-        const int from = paged_page(a, b, summ, x);
-        if (from < 0) {
-            atomicCAS(a.status, 0, KSA_PAGED_STATUS_BAD_PAGE);
+    // all of a thread's page lookups, then all of its loads, then its stores
+    constexpr int kPasses = 128 / kRowsPass;
+    const int lane = threadIdx.x % kLanes, in_page = (1 << a.page_shift) - 1;
+    int from[kPasses];
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+        const int x = x0 + threadIdx.x / kLanes + i * kRowsPass;
+        from[i] = x < see.lo || x >= see.hi || (x >= see.gap_lo && x < see.gap_hi) ? -3 : paged_page(a, b, summ, x);
+    }
+    uint4 yk[kPasses], yv[kPasses];
+    uint32_t ek[kPasses], ev[kPasses];
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+        if (from[i] < 0) {
+            if (from[i] != -3) atomicCAS(a.status, 0, KSA_PAGED_STATUS_BAD_PAGE);
             continue;
         }
-        const int in = x & ((1 << a.page_shift) - 1);
-        const int64_t at = from * a.page_st + h * a.head_st + in * a.row_st + lane * 16, se = (((int64_t)from * a.Hkv + h) << a.page_shift) + in;
-        const uint4 yk = __ldcg(reinterpret_cast<const uint4*>(a.kp + at)), yv = __ldcg(reinterpret_cast<const uint4*>(a.vp + at));
-        const float fk = e8m0_scale(__ldcg(a.ke + se)), fv = e8m0_scale(__ldcg(a.ve + se));
-        const int64_t to = (((int64_t)page * a.Hkv + h) * 128 + r) * D + lane * 16;
-        auto put = [](uint16_t* dst, const uint4& y, float f) {
-            uint4 z[2];
-            uint32_t* w = reinterpret_cast<uint32_t*>(z);
-            const uint32_t yw[4] = {y.x, y.y, y.z, y.w};
+        const int in = x0 + threadIdx.x / kLanes + i * kRowsPass & in_page;
+        const int64_t at = from[i] * a.page_st + h * a.head_st + in * a.row_st + lane * 16, se = (((int64_t)from[i] * a.Hkv + h) << a.page_shift) + in;
+        yk[i] = __ldcg(reinterpret_cast<const uint4*>(a.kp + at)); yv[i] = __ldcg(reinterpret_cast<const uint4*>(a.vp + at));
+        ek[i] = __ldcg(a.ke + se); ev[i] = __ldcg(a.ve + se);
+    }
+    auto put = [](uint16_t* dst, const uint4& y, float f) {
+        uint4 z[2];
+        uint32_t* w = reinterpret_cast<uint32_t*>(z);
+        const uint32_t yw[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 p = e4m3x2_to_f32(yw[i] & 0xffffu), q = e4m3x2_to_f32(yw[i] >> 16);
-                w[2 * i] = ptx::pack_bf16x2(p.x * f, p.y * f); w[2 * i + 1] = ptx::pack_bf16x2(q.x * f, q.y * f);
-            }
-            reinterpret_cast<uint4*>(dst)[0] = z[0]; reinterpret_cast<uint4*>(dst)[1] = z[1];
-        };
-        put(u.k + to, yk, fk);
-        put(u.v + to, yv, fv);
+        for (int i = 0; i < 4; ++i) {
+            const float2 p = e4m3x2_to_f32(yw[i] & 0xffffu), q = e4m3x2_to_f32(yw[i] >> 16);
+            w[2 * i] = ptx::pack_bf16x2(p.x * f, p.y * f); w[2 * i + 1] = ptx::pack_bf16x2(q.x * f, q.y * f);
+        }
+        reinterpret_cast<uint4*>(dst)[0] = z[0]; reinterpret_cast<uint4*>(dst)[1] = z[1];
+    };
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+        if (from[i] < 0) continue;
+        const int64_t to = (((int64_t)page * a.Hkv + h) * 128 + threadIdx.x / kLanes + i * kRowsPass) * D + lane * 16;
+        put(u.k + to, yk[i], e8m0_scale(ek[i]));
+        put(u.v + to, yv[i], e8m0_scale(ev[i]));
     }
 }
 
