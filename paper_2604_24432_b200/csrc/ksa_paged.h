@@ -36,6 +36,14 @@ cudaError_t setup_paged_attn();
 cudaError_t launch_paged_tc(const PagedArgs& a, bool e4m3, int num_sms, PagedEncode encode, cudaStream_t stream);
 cudaError_t setup_paged_tc();
 
+// Query tiles of a call at most, whatever its lengths: none is without a row, and only the last of a sequence's text tokens (of its
+// summaries) holds fewer than tokens_per_tile.
+inline int64_t paged_most_tiles(const PagedArgs& a)
+{
+    const int64_t n = ((int64_t)a.rows + (int64_t)a.B * (a.m > 0 ? 2 : 1) * (a.tokens_per_tile - 1)) / a.tokens_per_tile;
+    return n < a.rows ? n : a.rows;
+}
+
 #if defined(__CUDACC__)
 // ---- rows and pages -------------------------------------------------------------------------------------------------
 // (Lengths, tables and rows are read past L1: a kernel here may start while the one before the one in front of it still reads,

@@ -542,9 +542,7 @@ cudaError_t launch_paged_attn(const PagedArgs& args, bool e4m3, int num_sms, Pag
     const int n = (int64_t)a.rows * a.G <= 8 * (int64_t)a.B ? 1 : 2;
     a.tokens_per_tile = a.G <= 8 * n ? 8 * n / a.G : 1;
     a.head_blocks = (a.G + 8 * n - 1) / (8 * n);
-    // no tile without a row, none but a sequence's last of its kind with fewer than tokens_per_tile tokens
-    const int64_t most = (int64_t)a.rows / a.tokens_per_tile + (int64_t)a.B * (a.m > 0 ? 2 : 1);
-    const int64_t units = (most < a.rows ? most : a.rows) * a.Hkv * a.head_blocks;
+    const int64_t units = paged_most_tiles(a) * a.Hkv * a.head_blocks;
     const int64_t rows = ((int64_t)a.text_cols + (a.m > 0 ? a.summ_cols : 0)) << a.page_shift;      // of a sequence, at most
     a.nsplit = paged_splits(units, rows / 64, num_sms);
     const int panel = a.D * (e4m3 ? 1 : 2) < 128 ? 64 : 128;

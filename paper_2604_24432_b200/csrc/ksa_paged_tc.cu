@@ -30,6 +30,8 @@
 // for, the cluster's barriers are still passed, TMEM is freed.
 #include <cuda_bf16.h>
 
+#include <algorithm>
+
 #include "ksa_launch.h"
 #include "ksa_paged.h"
 #include "ksa_ptx.cuh"
@@ -40,7 +42,6 @@ namespace ksa {
 using namespace ptx;
 
 constexpr int kPtTile = 128;
-constexpr int kPtMaxSplit = 8;                       // the portable cluster size
 // log2 units: P stays below 2^12 (see ksa_text_tc.cu)
 constexpr float kPtRescale = 12.0f;
 
@@ -67,9 +68,10 @@ struct PtCfg {
     static constexpr int kRawFull = kVEmpty + kStagesV, kRawEmpty = kRawFull + kStagesRaw;
     static constexpr int kNumBars = kRawEmpty + kStagesRaw;
     static constexpr int kSmemBytes = kBarOff + 8 * kNumBars + 64 + 1024;   // + slack for 1024-byte alignment
-    // partial results, over Q, K and V once these are done with: O fp32 [256][D], then (maximum, sum) [256]
+    // partial results, over Q, K and V once these are done with: O fp32 [256][D], (maximum, sum) [256], then where each row's output
+    // and LSE go (offsets in elements; the first -1 for a row past the last)
     static constexpr int kPartMl = 256 * D * 4;
-    static_assert(kPartMl + 256 * 8 <= kBarOff, "partial results fit over the tiles");
+    static_assert(kPartMl + 256 * (8 + 16) <= kBarOff, "partial results fit over the tiles");
 };
 
 struct PagedMaps { CUtensorMap k, v; };
@@ -174,7 +176,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
 
     const int split = (int)blockIdx.x % a.nsplit, unit = (int)blockIdx.x / a.nsplit;
     const int hk = unit % a.Hkv;
-    const PagedTile t = paged_tile(a, unit / a.Hkv);       // up to 2 * per tokens
+    const PagedTile t = paged_tile<true>(a, unit / a.Hkv);       // up to 2 * per tokens
     const int per = a.tokens_per_tile / 2;
     if (t.b >= 0) {                                         // (the same for the whole cluster)
     const PtWalk w = pt_walk(a, t, split);
@@ -637,7 +639,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
         } else {
             // ---- partial results into shared memory, summed up over the cluster, a share of the rows by each CTA ----
             pt_named_barrier(1, 256);                         // both query tiles' products have read their K, V and Q
-            const uint32_t part_o = smem_base, part_ml = smem_base + Cfg::kPartMl;
+            const uint32_t part_o = smem_base, part_ml = smem_base + Cfg::kPartMl, part_to = part_ml + 256 * 8;
             if (tokens > 0) {
                 const uint32_t d = part_o + (uint32_t)((u * 128 + row) * D * 4);
 #pragma unroll
@@ -657,42 +659,58 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                         pt_st_shared4(d + (uint32_t)((c * 8 + (e ^ (row & 7))) * 16), o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
                 }
                 asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(part_ml + (u * 128 + row) * 8), "f"(m_used), "f"(l_run) : "memory");
+                const int64_t prow = paged_row(a, t, x);
+                const bool store = valid && ksa_in_bounds(prow >= 0 && prow < a.rows && head < a.Hq, a.status);
+                const uint64_t off = store ? (uint64_t)(prow * a.o_st + (int64_t)head * a.o_sh) : ~0ull, lse = (uint64_t)((int64_t)head * a.rows + prow);
+                pt_st_shared4(part_to + (u * 128 + row) * 16, (uint32_t)off, (uint32_t)(off >> 32), (uint32_t)lse, (uint32_t)(lse >> 32));
                 tc_fence_before();
             }
             __syncwarp();
             cluster_arrive(); cluster_wait();
-            // D / 4 lanes a row
-            constexpr int kLanes = D / 4, kRowsPass = 256 / kLanes;
-            const int total = t.n * a.G, c4 = tid % kLanes;
-            for (int i = split * kRowsPass + tid / kLanes; i < total; i += kRowsPass * a.nsplit) {
-                const int tok = i / a.G, hh = hk * a.G + i - tok * a.G;
-                const int pr = tok < per ? i : 128 + i - per * a.G;          // row of the partial results
-                const uint32_t at = part_o + (uint32_t)(pr * D * 4 + ((c4 & ~7) + ((c4 & 7) ^ (pr & 7))) * 16);
-                float2 ml[kPtMaxSplit];
-                float4 v[kPtMaxSplit];
+            // D / 4 lanes a row, kMerge rows and two CTAs at a time so that the reads of the other CTAs' memory overlap
+            constexpr int kLanes = D / 4, kRowsPass = 256 / kLanes, kMerge = 4;
+            const int rows0 = per * a.G, total = t.n * a.G, c4 = tid % kLanes, step = kRowsPass * a.nsplit;
+            for (int i0 = split * kRowsPass + tid / kLanes; i0 < total; i0 += kMerge * step) {
+                uint32_t at[kMerge], pr[kMerge];
+                float M[kMerge], L[kMerge];
+                float4 acc[kMerge];
 #pragma unroll
-                for (int s = 0; s < kPtMaxSplit; ++s)
-                    if (s < a.nsplit) {
-                        ml[s] = pt_ld_cluster2(mapa_shared(part_ml + pr * 8, s));
-                        v[s] = pt_ld_cluster4(mapa_shared(at, s));
+                for (int r = 0; r < kMerge; ++r) {
+                    const int i = min(i0 + r * step, total - 1);
+                    pr[r] = i < rows0 ? i : 128 + i - rows0;                          // row of the partial results
+                    at[r] = part_o + (uint32_t)(pr[r] * (D * 4) + ((c4 & ~7) + ((c4 ^ pr[r]) & 7)) * 16);
+                    M[r] = -INFINITY; L[r] = 0.f;
+                    acc[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+                for (int s0 = 0; s0 < a.nsplit; s0 += 2) {                            // (a power of two, and more than one)
+                    float2 ml[2][kMerge];
+                    float4 v[2][kMerge];
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const uint32_t other = mapa_shared(smem_base, s0 + s) - smem_base;
+#pragma unroll
+                        for (int r = 0; r < kMerge; ++r) { ml[s][r] = pt_ld_cluster2(part_ml + pr[r] * 8 + other); v[s][r] = pt_ld_cluster4(at[r] + other); }
                     }
-                float M = -INFINITY, L = 0.f;
 #pragma unroll
-                for (int s = 0; s < kPtMaxSplit; ++s) if (s < a.nsplit) M = fmaxf(M, ml[s].x);
-                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int s = 0; s < kPtMaxSplit; ++s)
-                    if (s < a.nsplit) {
-                        const float f = (ml[s].x == -INFINITY) ? 0.f : ex2_approx(ml[s].x - M);
-                        L += ml[s].y * f;
-                        acc.x += v[s].x * f; acc.y += v[s].y * f; acc.z += v[s].z * f; acc.w += v[s].w * f;
+                    for (int r = 0; r < kMerge; ++r) {
+                        const float m = fmax3(M[r], ml[0][r].x, ml[1][r].x), base = (m == -INFINITY) ? 0.f : m;
+                        const float al = ex2_approx(M[r] - base), f0 = ex2_approx(ml[0][r].x - base), f1 = ex2_approx(ml[1][r].x - base);
+                        M[r] = m;
+                        L[r] = fmaf(L[r], al, fmaf(ml[0][r].y, f0, ml[1][r].y * f1));
+                        acc[r].x = fmaf(acc[r].x, al, fmaf(v[0][r].x, f0, v[1][r].x * f1)); acc[r].y = fmaf(acc[r].y, al, fmaf(v[0][r].y, f0, v[1][r].y * f1));
+                        acc[r].z = fmaf(acc[r].z, al, fmaf(v[0][r].z, f0, v[1][r].z * f1)); acc[r].w = fmaf(acc[r].w, al, fmaf(v[0][r].w, f0, v[1][r].w * f1));
                     }
-                const float inv = 1.f / L;
-                const int64_t prow = paged_row(a, t, t.x0 + tok);
-                if (!ksa_in_bounds(prow >= 0 && prow < a.rows && hh < a.Hq, a.status)) continue;
-                *reinterpret_cast<uint2*>(a.out + prow * a.o_st + (int64_t)hh * a.o_sh + c4 * 4) =
-                    make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
-                if (c4 == 0) a.lse[(int64_t)hh * a.rows + prow] = (M + log2f(L)) * 0.6931471805599453f;
+                }
+#pragma unroll
+                for (int r = 0; r < kMerge; ++r) {
+                    if (i0 + r * step >= total) break;
+                    const uint4 to = pt_ld_shared4(part_to + pr[r] * 16);             // where the row's output and LSE go
+                    const int64_t off = (int64_t)((uint64_t)to.y << 32 | to.x), lse = (int64_t)((uint64_t)to.w << 32 | to.z);
+                    if (off < 0) continue;
+                    const float inv = 1.f / L[r];
+                    *reinterpret_cast<uint2*>(a.out + off + c4 * 4) = make_uint2(pack_bf16x2(acc[r].x * inv, acc[r].y * inv), pack_bf16x2(acc[r].z * inv, acc[r].w * inv));
+                    if (c4 == 0) a.lse[lse] = (M[r] + log2f(L[r])) * 0.6931471805599453f;
+                }
             }
             __syncwarp();
             cluster_arrive(); cluster_wait();                 // no CTA leaves while another reads its results
@@ -717,16 +735,28 @@ cudaError_t setup_paged_tc()
     return cudaSuccess;
 }
 
+// CTAs of one cluster for a call of `units` query tiles at most.  Joining the parts costs some 5 us of a CTA's time, so the key
+// tiles are split where SMs would stand idle: 16 query tiles of 17 (65) key tiles each on 1, 2, 4, 8 CTAs: 34.5, 28.1, 22.9,
+// 43 us (104, 63, 41, 63 us; clusters of eight CTAs that fill an SM find few places); and in two where a call of a few rounds
+// holds several sequences, whose lengths differ, the longest first: two sequences of 17,000 and 8,192 rows, 16/16 heads: 206 and
+// 186 us, eight of 1 to 577 new rows over up to 31,000: 71 and 57.5 us; but one sequence, 144 even query tiles: 74 and 96 us.
+static int tc_splits(int64_t units, int64_t key_tiles, int seqs, int num_sms)
+{
+    if (units * 4 <= num_sms && key_tiles >= 16) return 4;
+    if (units * 2 <= num_sms && key_tiles >= 12) return 2;
+    return seqs > 1 && units * 2 <= 4 * num_sms && key_tiles >= 32 ? 2 : 1;
+}
+
 cudaError_t launch_paged_tc(const PagedArgs& args, bool e4m3, int num_sms, PagedEncode encode, cudaStream_t stream)
 {
     PagedArgs a = args;
     a.tokens_per_tile = 2 * (kPtTile / a.G);                  // of a CTA: two query tiles
     a.head_blocks = 1;
-    const int64_t most = (int64_t)a.rows / a.tokens_per_tile + (int64_t)a.B * (a.m > 0 ? 2 : 1);
-    const int64_t units = (most < a.rows ? most : a.rows) * a.Hkv;
-    const int64_t key_tiles = (((int64_t)a.text_cols + (a.m > 0 ? a.summ_cols : 0)) << a.page_shift) / kPtTile;    // of a sequence, at most
-    a.nsplit = 1;
-    while (a.nsplit < kPtMaxSplit && units * a.nsplit * 2 <= num_sms && key_tiles >= 4 * a.nsplit) a.nsplit *= 2;
+    const int64_t units = paged_most_tiles(a) * a.Hkv;
+    // rows that a query tile sees, at most
+    const int64_t text = std::min((int64_t)a.text_cols << a.page_shift, ((int64_t)a.C + 2) * a.kk + a.tokens_per_tile);
+    const int64_t key_tiles = (text + (a.m > 0 ? (int64_t)a.summ_cols << a.page_shift : 0)) / kPtTile;
+    a.nsplit = tc_splits(units, key_tiles, a.B, num_sms);
     PagedMaps maps;
     const int box_bytes = e4m3 ? a.D : 128;
     const CUtensorMapSwizzle swizzle = e4m3 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B;
