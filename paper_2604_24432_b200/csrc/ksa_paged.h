@@ -24,8 +24,8 @@ struct PagedArgs {
     int32_t* status;
 };
 
-cudaError_t launch_paged_append(const PagedArgs& a, bool e4m3, cudaStream_t stream);
-cudaError_t launch_paged_gather(const PagedArgs& a, bool e4m3, cudaStream_t stream);
+cudaError_t launch_paged_append(const PagedArgs& a, bool e4m3, int num_sms, cudaStream_t stream);
+cudaError_t launch_paged_gather(const PagedArgs& a, bool e4m3, int num_sms, cudaStream_t stream);
 typedef CUresult (*PagedEncode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 // Map of a page pool, [D, page rows, KV heads, pages] with a box of box_rows rows of box_bytes bytes of one page and head.
@@ -48,10 +48,9 @@ inline int64_t paged_most_tiles(const PagedArgs& a)
 // ---- rows and pages -------------------------------------------------------------------------------------------------
 // (Lengths, tables and rows are read past L1: a kernel here may start while the one before the one in front of it still reads,
 // after which L1 may keep a line that the one in front rewrites.)
-// Lengths of sequence b, checked: false for what are no lengths (nothing of such a sequence is touched).
-__device__ __forceinline__ bool paged_seq(const PagedArgs& a, int row0, int r1, int b, int& n, int& first)
+// A sequence's lengths, checked: false for what are no lengths (nothing of such a sequence is touched).
+__device__ __forceinline__ bool paged_seq(const PagedArgs& a, int row0, int r1, int first, int& n)
 {
-    first = __ldcg(a.cached + b);
     n = r1 - row0;
     if (!paged_lengths_ok(a, row0, r1, first)) {
         atomicCAS(a.status, 0, KSA_PAGED_STATUS_BAD_ROWS);
@@ -81,7 +80,8 @@ __device__ __forceinline__ PagedTile paged_tile(const PagedArgs& a, int item)
         int row0 = 0, n = 0, first = 0, t0 = 0, nt = 0, tt = 0, ts = 0;
         if (base + lane < a.B) {
             row0 = __ldcg(a.cu + base + lane);
-            paged_seq(a, row0, __ldcg(a.cu + base + lane + 1), base + lane, n, first);
+            first = __ldcg(a.cached + base + lane);
+            paged_seq(a, row0, __ldcg(a.cu + base + lane + 1), first, n);
         }
         if (n > 0) {
             t0 = paged_texts(a, first);

@@ -332,7 +332,7 @@ def test_bad_pages_and_lengths_are_reported(ctx):
     """Entries that are no pages, columns past the table, lengths that are none: a status, nothing else touched, and the context
     goes on.  (That no such entry becomes an address is shown on the host: test_paged.py, test_entries_and_lengths.)"""
     for n in (1, 130):
-        s = Server(ctx, 8, 1, 4, 4, 2, 64, 16, "bf16", [200, 200], seed=6)
+        s = Server(ctx, 8, 1, 4, 4, 2, 64, 16, "bf16", [400, 200], seed=6)
         spans = [(60, n), (60, n)]
         s.fill(spans)
         good = s.batch(spans)
