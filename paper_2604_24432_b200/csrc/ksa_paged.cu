@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(kRowThreads) ksa_paged_unpack_kernel(PagedArgs
     const int b = blockIdx.z, h = blockIdx.y, slot = blockIdx.x;
     int n;
     const int first = __ldcg(a.cached + b);
-    if (!paged_seq(a, __ldcg(a.cu + b), __ldcg(a.cu + b + 1), first, n) || n == 0) return;
+    if (!paged_seq(a, __ldcg(a.cu + b), __ldcg(a.cu + b + 1), first, n) || n < a.rows_min || n > a.rows_max) return;
     const bool summ = slot >= u.text_pages;
     const PagedRange see = paged_range(a, first, n, summ);
     const int tile = summ ? slot - u.text_pages : see.lo / 128 + slot, x0 = tile * 128;
@@ -449,25 +449,43 @@ KSA_API int ksa_paged_attn(ksa_ctx* ctx, const ksa_paged_kv* kv, const void* q, 
             if (e != cudaSuccess) return e;
             ready = true;
         }
-        // up to 16 query rows a sequence: as many as the mma.sync kernel's tiles hold
-        if ((int64_t)a.rows * a.G <= 16 * (int64_t)a.B) return launch_paged_attn(a, e4m3, ksa_ctx_num_sms(ctx), encode, stream);
+        // Up to 16 query rows a sequence, on average: the mma.sync kernel for all.  More than 64, and several sequences: that one for
+        // those that fit into its tiles (single tokens beside prompts), and the tcgen05 kernel, which takes as long over one query
+        // row as over 256, beside it for the others: 24 tokens over 90,000 to 113,000 rows and 1,152 rows over 36,864, 32/8 heads:
+        // e4m3 484 -> 261 us, bf16 251 -> 259; the 24 over 1,000 to 3,500 rows: 152 -> 156, 126 -> 100.  A launch that finds no
+        // such sequence costs 4 us.
+        const int sms = ksa_ctx_num_sms(ctx);
+        const int64_t rows = (int64_t)a.rows * a.G;
+        a.rows_min = 1; a.rows_max = a.rows;
+        if (rows <= 16 * (int64_t)a.B) return launch_paged_attn(a, e4m3, rows <= 8 * (int64_t)a.B ? 8 : 16, sms, encode, stream);
+        const int small = a.B < 4 || rows <= 64 * (int64_t)a.B || a.G > 16 ? 0 : (a.G > 8 ? 16 : 8) / a.G;      // rows of a sequence for the former
         const UnpackLayout l = unpack_layout(p);
-        if (l.bytes > 0 && workspace && workspace_bytes >= (size_t)l.bytes) {
-            UnpackArgs u{};
+        const bool copy = l.bytes > 0 && workspace && workspace_bytes >= (size_t)l.bytes;
+        UnpackArgs u{};
+        if (copy) {
             u.k = (uint16_t*)workspace; u.v = u.k + l.kv_bytes / 2;
             u.text_table = (int32_t*)((char*)workspace + l.tables); u.summ_table = u.text_table + l.text_cols * a.B;
             u.text_cols = (int32_t)l.text_cols; u.summ_cols = (int32_t)l.summ_cols; u.text_pages = (int32_t)l.text_pages; u.seq_pages = (int32_t)l.seq_pages;
+            a.rows_min = small + 1;
             e = launch_dependent(a.D == 128 ? ksa_paged_unpack_kernel<128> : ksa_paged_unpack_kernel<64>,
                                  dim3((unsigned)l.seq_pages, (unsigned)a.Hkv, (unsigned)a.B), kRowThreads, 0, stream, a, u);
             if (e != cudaSuccess) return e;
             ksa_ctx_add_launches(ctx, 1);
-            // from here on the cache is the copy
+        }
+        if (small > 0) {
+            a.rows_min = 1; a.rows_max = small; a.beside = 1;
+            if ((e = launch_paged_attn(a, e4m3, small * a.G, sms, encode, stream)) != cudaSuccess) return e;
+            ksa_ctx_add_launches(ctx, 1);
+            a.beside = 2;
+        }
+        a.rows_min = small + 1; a.rows_max = a.rows;
+        if (copy) {                                            // from here on the cache is the copy
             a.kp = (uint8_t*)u.k; a.vp = (uint8_t*)u.v; a.ke = a.ve = nullptr;
             a.text_table = u.text_table; a.summ_table = u.summ_table; a.text_cols = u.text_cols; a.summ_cols = u.summ_cols;
             a.page_shift = 7; a.num_pages = (int32_t)(a.B * l.seq_pages);
             a.row_st = a.D * 2; a.head_st = 128 * a.row_st; a.page_st = a.Hkv * a.head_st;
             e4m3 = false;
         }
-        return launch_paged_tc(a, e4m3, ksa_ctx_num_sms(ctx), encode, stream);
+        return launch_paged_tc(a, e4m3, sms, encode, stream);
     });
 }

@@ -19,6 +19,8 @@ struct PagedArgs {
     int32_t B, rows, kk, m, C, Hq, Hkv, G, D;
     int32_t page_shift, num_pages, text_cols, summ_cols;             // page_rows = 1 << page_shift
     int32_t tokens_per_tile, head_blocks, nsplit;                    // attention: see the kernels
+    int32_t rows_min, rows_max;                                      // ... of sequences with as many rows in the call
+    int32_t beside;                                                  // 1: the kernel behind runs beside this one; 2: this one is it
     uint32_t flags;
     float scale_log2;
     int32_t* status;
@@ -30,8 +32,8 @@ typedef CUresult (*PagedEncode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, v
                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 // Map of a page pool, [D, page rows, KV heads, pages] with a box of box_rows rows of box_bytes bytes of one page and head.
 bool encode_pages(PagedEncode encode, CUtensorMap* map, void* base, const PagedArgs& a, bool e4m3, int box_bytes, int box_rows, CUtensorMapSwizzle swizzle);
-// Tiles of up to 16 query rows (mma.sync), and of up to 256 (tcgen05).
-cudaError_t launch_paged_attn(const PagedArgs& a, bool e4m3, int num_sms, PagedEncode encode, cudaStream_t stream);
+// Tiles of up to 8 or 16 query rows (mma.sync), and of up to 256 (tcgen05).
+cudaError_t launch_paged_attn(const PagedArgs& a, bool e4m3, int query_rows, int num_sms, PagedEncode encode, cudaStream_t stream);
 cudaError_t setup_paged_attn();
 cudaError_t launch_paged_tc(const PagedArgs& a, bool e4m3, int num_sms, PagedEncode encode, cudaStream_t stream);
 cudaError_t setup_paged_tc();
@@ -40,8 +42,9 @@ cudaError_t setup_paged_tc();
 // summaries) holds fewer than tokens_per_tile.
 inline int64_t paged_most_tiles(const PagedArgs& a)
 {
-    const int64_t n = ((int64_t)a.rows + (int64_t)a.B * (a.m > 0 ? 2 : 1) * (a.tokens_per_tile - 1)) / a.tokens_per_tile;
-    return n < a.rows ? n : a.rows;
+    const int64_t most = (int64_t)a.B * a.rows_max, rows = most < a.rows ? most : a.rows;
+    const int64_t n = (rows + (int64_t)a.B * (a.m > 0 ? 2 : 1) * (a.tokens_per_tile - 1)) / a.tokens_per_tile;
+    return n < rows ? n : rows;
 }
 
 #if defined(__CUDACC__)
@@ -70,44 +73,46 @@ __device__ __forceinline__ int paged_page(const PagedArgs& a, int b, bool summ, 
 
 // ---- query tiles ------------------------------------------------------------------------------------------------------
 // Tile `item` of the call, counted through the sequences (text tiles of a sequence before its summary tiles).  Executed by a
-// whole warp: 32 sequences at a time.  kLongestFirst: these in descending order of what their last row sees.
-template <bool kLongestFirst = false>
+// whole warp: 32 sequences at a time, these in descending order of what their last row sees.  kMix: a run of rows that fits into
+// a tile is one, text tokens and summaries together.
+template <bool kMix>
 __device__ __forceinline__ PagedTile paged_tile(const PagedArgs& a, int item)
 {
     const int lane = threadIdx.x & 31, per = a.tokens_per_tile;
-    PagedTile t{-1, false, 0, 0, 0, 0};
+    PagedTile t{-1, false, false, 0, 0, 0, 0};
     for (int base = 0; base < a.B; base += 32) {
         int row0 = 0, n = 0, first = 0, t0 = 0, nt = 0, tt = 0, ts = 0;
         if (base + lane < a.B) {
             row0 = __ldcg(a.cu + base + lane);
             first = __ldcg(a.cached + base + lane);
             paged_seq(a, row0, __ldcg(a.cu + base + lane + 1), first, n);
+            if (n < a.rows_min || n > a.rows_max) n = 0;
         }
         if (n > 0) {
             t0 = paged_texts(a, first);
             nt = paged_texts(a, first + n) - t0;
             tt = (nt + per - 1) / per;
             ts = (n - nt + per - 1) / per;
+            if (kMix && n <= per) { tt = 1; ts = 0; }
         }
         int seq = base + lane;
-        if constexpr (kLongestFirst) {
-            if (a.B > 1) {
-                // a lane's place among the 32, by the keys in view (as a number, ties by lane), then everything to its place
-                const PagedView w = paged_view(a, nt == 0, nt > 0 ? t0 + nt - 1 : max(first + n - t0 - 1, 0));
-                const int keys = n > 0 ? w.t_hi - w.t_lo + w.s_hi - w.s_lo : -1;
-                int place = 0;
+        if (a.B > 1) {
+            // a lane's place among the 32, by the keys in view (as a number, ties by lane), then everything to its place
+            const bool summ = n > 0 && nt == 0;
+            const PagedView w = paged_view(a, summ, summ ? first + n - t0 - 1 : t0 + max(nt - 1, 0));
+            const int keys = n > 0 ? w.t_hi - w.t_lo + w.s_hi - w.s_lo : -1;
+            int place = 0;
 #pragma unroll
-                for (int o = 0; o < 32; ++o) {
-                    const int other = __shfl_sync(0xffffffffu, keys, o);
-                    place += other > keys || (other == keys && o < lane);
-                }
-                int from = 0;
-#pragma unroll
-                for (int o = 0; o < 32; ++o) if (__shfl_sync(0xffffffffu, place, o) == lane) from = o;
-                seq = base + from;
-                row0 = __shfl_sync(0xffffffffu, row0, from); n = __shfl_sync(0xffffffffu, n, from); first = __shfl_sync(0xffffffffu, first, from);
-                t0 = __shfl_sync(0xffffffffu, t0, from); nt = __shfl_sync(0xffffffffu, nt, from); tt = __shfl_sync(0xffffffffu, tt, from); ts = __shfl_sync(0xffffffffu, ts, from);
+            for (int o = 0; o < 32; ++o) {
+                const int other = __shfl_sync(0xffffffffu, keys, o);
+                place += other > keys || (other == keys && o < lane);
             }
+            int from = 0;
+#pragma unroll
+            for (int o = 0; o < 32; ++o) if (__shfl_sync(0xffffffffu, place, o) == lane) from = o;
+            seq = base + from;
+            row0 = __shfl_sync(0xffffffffu, row0, from); n = __shfl_sync(0xffffffffu, n, from); first = __shfl_sync(0xffffffffu, first, from);
+            t0 = __shfl_sync(0xffffffffu, t0, from); nt = __shfl_sync(0xffffffffu, nt, from); tt = __shfl_sync(0xffffffffu, tt, from); ts = __shfl_sync(0xffffffffu, ts, from);
         }
         int sum = tt + ts;
 #pragma unroll
@@ -124,10 +129,11 @@ __device__ __forceinline__ PagedTile paged_tile(const PagedArgs& a, int item)
             t.b = __shfl_sync(0xffffffffu, seq, src);
             t.row0 = __shfl_sync(0xffffffffu, row0, src);
             t.first = __shfl_sync(0xffffffffu, first, src);
+            t.mixed = kMix && n <= per;
             t.summ = i >= tt;
             if (t.summ) i -= tt;
-            const int have = t.summ ? n - nt : nt;
-            t.x0 = (t.summ ? t.first - t0 : t0) + i * per;
+            const int have = t.mixed ? n : t.summ ? n - nt : nt;
+            t.x0 = t.mixed ? t.first : (t.summ ? t.first - t0 : t0) + i * per;
             t.n = min(per, have - i * per);
             return t;
         }

@@ -134,11 +134,12 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
         ptx::prefetch_tensormap(&maps.v);
     }
     __syncthreads();
-    ptx::pdl_launch_dependents();
+    if (a.beside == 0) ptx::pdl_launch_dependents();
     ptx::pdl_wait();
+    if (a.beside == 1) ptx::pdl_launch_dependents();           // the kernel behind does not wait for this one, but for those before
     const int split = (int)blockIdx.x % a.nsplit, unit = (int)blockIdx.x / a.nsplit;
     const int hb = unit % a.head_blocks, hk = unit / a.head_blocks % a.Hkv;
-    const PagedTile t = paged_tile<true>(a, unit / a.head_blocks / a.Hkv);
+    const PagedTile t = paged_tile<false>(a, unit / a.head_blocks / a.Hkv);
     if (t.b < 0) return;                                       // (the whole cluster)
     const int l4 = lane >> 2, c2 = (lane & 3) * 2;             // fragment row and column pair
     // the tile's rows: (token, head), heads `head0 ..` of the group
@@ -536,10 +537,10 @@ bool encode_pages(PagedEncode encode, CUtensorMap* map, void* base, const PagedA
                   CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-cudaError_t launch_paged_attn(const PagedArgs& args, bool e4m3, int num_sms, PagedEncode encode, cudaStream_t stream)
+cudaError_t launch_paged_attn(const PagedArgs& args, bool e4m3, int query_rows, int num_sms, PagedEncode encode, cudaStream_t stream)
 {
     PagedArgs a = args;
-    const int n = (int64_t)a.rows * a.G <= 8 * (int64_t)a.B ? 1 : 2;
+    const int n = query_rows <= 8 ? 1 : 2;
     a.tokens_per_tile = a.G <= 8 * n ? 8 * n / a.G : 1;
     a.head_blocks = (a.G + 8 * n - 1) / (8 * n);
     const int64_t units = paged_most_tiles(a) * a.Hkv * a.head_blocks;

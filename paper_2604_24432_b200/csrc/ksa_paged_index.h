@@ -37,16 +37,24 @@ template <class A> KSA_HD int paged_texts(const A& a, int row)
     return c * a.kk + (r < a.kk ? r : a.kk);
 }
 
-// A query tile: tokens_per_tile (or fewer) consecutive text tokens, or consecutive summaries, of one sequence.  Its rows
-// are (token, query head of the group), and what they see is one range of text and one of summaries each.
+// A query tile: tokens_per_tile (or fewer) consecutive text tokens, or consecutive summaries, of one sequence, or all of its rows
+// of the call as they come (`mixed`).  The tile's own rows are (token, query head of the group), and what one sees is one range
+// of text and one of summaries.
 struct PagedTile {
     int b;                   // sequence; -1: no such tile
-    bool summ;
-    int x0, n;               // first text token (summary) and how many
+    bool summ, mixed;
+    int x0, n;               // first text token (summary; mixed: the sequence's row `first`) and how many
     int64_t row0;            // packed row of the sequence's row `first`
     int first;
 };
 
+// Token i of a tile: its packed row, whether it is a summary, and its number among the sequence's summaries (text tokens).
+template <class A> KSA_HD int paged_token(const A& a, const PagedTile& t, int i, bool& summ)
+{
+    if (t.mixed) return paged_place(a, t.first + i, summ);
+    summ = t.summ;
+    return t.x0 + i;
+}
 // The packed row of a tile's text token (summary) x.
 template <class A> KSA_HD int64_t paged_row(const A& a, const PagedTile& t, int x)
 {
@@ -106,5 +114,49 @@ template <class A> KSA_HD PagedRange paged_range(const A& a, int first, int n, b
     }
     return r;
 }
+
+// The key tiles (kTile rows each, from multiples of it) that hold what a query tile sees: those of the summaries, but for the
+// ones inside a gap, then those of the text; part `split` of `parts` of them, [j0, j1).
+template <int kTile> struct PagedWalk {
+    PagedRange summ, text;
+    int a0, na, b0, nb, t0, j0, j1;
+    template <class A> KSA_HD void init(const A& a, const PagedTile& t, int split, int parts)
+    {
+        if (t.mixed) {
+            text = paged_range(a, t.first, t.n, false);
+            summ = paged_range(a, t.first, t.n, true);
+        } else {
+            const PagedView v = paged_tile_view(a, t);
+            text = PagedRange{v.t_lo, v.t_hi, 0, 0};
+            summ = PagedRange{v.s_lo, v.s_hi, 0, 0};
+        }
+        const bool gap = summ.gap_hi > summ.gap_lo;
+        const int a_hi = gap ? summ.gap_lo : summ.hi;
+        a0 = summ.lo / kTile;
+        na = a_hi > summ.lo ? (a_hi + kTile - 1) / kTile - a0 : 0;
+        b0 = gap ? summ.gap_hi / kTile : 0;
+        if (gap && b0 < a0 + na) b0 = a0 + na;                     // (a tile that holds rows from both sides comes once)
+        nb = gap && (summ.hi + kTile - 1) / kTile > b0 ? (summ.hi + kTile - 1) / kTile - b0 : 0;
+        t0 = text.lo / kTile;
+        const int tiles = na + nb + (text.hi + kTile - 1) / kTile - t0, per = (tiles + parts - 1) / parts;
+        j0 = split * per < tiles ? split * per : tiles;
+        j1 = j0 + per < tiles ? j0 + per : tiles;
+    }
+    // Tile j: its stream, its first row, and what of the stream is seen
+    struct Tile {
+        bool summ;
+        int x0;
+        PagedRange see;
+        KSA_HD bool sees(int x) const { return x >= see.lo && x < see.hi && !(x >= see.gap_lo && x < see.gap_hi); }
+        // any of the rows [x, x + n); all of the tile's
+        KSA_HD bool sees_any(int x, int n) const { return x < see.hi && x + n > see.lo && !(x >= see.gap_lo && x + n <= see.gap_hi); }
+        KSA_HD bool sees_all() const { return x0 >= see.lo && x0 + kTile <= see.hi && !(x0 < see.gap_hi && x0 + kTile > see.gap_lo); }
+    };
+    KSA_HD Tile at(int j) const
+    {
+        if (j < na + nb) return Tile{true, (j < na ? a0 + j : b0 + j - na) * kTile, summ};
+        return Tile{false, (t0 + j - na - nb) * kTile, text};
+    }
+};
 
 }  // namespace ksa

@@ -100,34 +100,6 @@ __device__ __forceinline__ float2 pt_ld_cluster2(uint32_t addr)
     return v;
 }
 
-// The share of the key tiles that a CTA walks: tiles [j0, j1) of the unit's summary tiles (from s_t0), then its text tiles.
-struct PtWalk {
-    PagedView see;
-    int s_tiles, s_t0, t_t0, j0, j1;
-    // tile j: its first row, its stream, and the rows [lo, hi) of that stream that anything in the unit sees
-    __device__ __forceinline__ bool at(int j, int& x0, int& lo, int& hi) const
-    {
-        const bool summ = j < s_tiles;
-        x0 = (summ ? s_t0 + j : t_t0 + j - s_tiles) * kPtTile;
-        lo = summ ? see.s_lo : see.t_lo;
-        hi = summ ? see.s_hi : see.t_hi;
-        return summ;
-    }
-};
-__device__ __forceinline__ PtWalk pt_walk(const PagedArgs& a, const PagedTile& t, int split)
-{
-    PtWalk w;
-    w.see = paged_tile_view(a, t);
-    w.s_t0 = w.see.s_lo / kPtTile;
-    w.s_tiles = w.see.s_hi > w.see.s_lo ? (w.see.s_hi + kPtTile - 1) / kPtTile - w.s_t0 : 0;
-    w.t_t0 = w.see.t_lo / kPtTile;
-    const int tiles = w.s_tiles + (w.see.t_hi + kPtTile - 1) / kPtTile - w.t_t0;
-    const int per = (tiles + a.nsplit - 1) / a.nsplit;
-    w.j0 = min(tiles, split * per);
-    w.j1 = min(tiles, w.j0 + per);
-    return w;
-}
-
 template <int D, bool E4M3>
 __global__ void __launch_bounds__(PtCfg<D, E4M3>::kThreads, 1)
 ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedMaps maps)
@@ -171,7 +143,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = ld_shared_u32(tmem_slot);
-    pdl_wait();
+    if (a.beside != 2) pdl_wait();                          // (beside the kernel in front, which has waited for those before it)
     pdl_launch_dependents();
 
     const int split = (int)blockIdx.x % a.nsplit, unit = (int)blockIdx.x / a.nsplit;
@@ -179,7 +151,8 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
     const PagedTile t = paged_tile<true>(a, unit / a.Hkv);       // up to 2 * per tokens
     const int per = a.tokens_per_tile / 2;
     if (t.b >= 0) {                                         // (the same for the whole cluster)
-    const PtWalk w = pt_walk(a, t, split);
+    PagedWalk<kPtTile> w;
+    w.init(a, t, split, a.nsplit);
     const int T = w.j1 - w.j0;
     const int nh = T == 0 ? 0 : t.n > per ? 2 : 1;          // query tiles
 
@@ -194,11 +167,10 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
             // the largest scales of K and of V among the rows in view: 16 rows at a time
             uint32_t top_k = 0, top_v = 0;
             for (int i = row; i < T * (kPtTile / 16); i += 128) {
-                int x0, lo, hi;
-                const bool summ = w.at(w.j0 + i / (kPtTile / 16), x0, lo, hi);
-                const int x = x0 + i % (kPtTile / 16) * 16;
-                if (x >= hi || x + 16 <= lo) continue;
-                const int page = paged_page(a, t.b, summ, x);
+                const auto tile = w.at(w.j0 + i / (kPtTile / 16));
+                const int x = tile.x0 + i % (kPtTile / 16) * 16;
+                if (!tile.sees_any(x, 16)) continue;
+                const int page = paged_page(a, t.b, tile.summ, x);
                 if (page < 0) continue;
                 const int64_t at = (((int64_t)page * a.Hkv + hk) << a.page_shift) + (x & ((1 << a.page_shift) - 1));
                 const uint4 k = __ldcg(reinterpret_cast<const uint4*>(a.ke + at)), v = __ldcg(reinterpret_cast<const uint4*>(a.ve + at));
@@ -206,9 +178,9 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                 uint32_t mk = 0, mv = 0;
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    uint32_t in = 0xffffffffu;                 // rows in view
-                    if (x + 4 * c < lo) in &= x + 4 * c + 4 <= lo ? 0u : 0xffffffffu << 8 * (lo - x - 4 * c);
-                    if (x + 4 * c + 4 > hi) in &= x + 4 * c >= hi ? 0u : 0xffffffffu >> 8 * (x + 4 * c + 4 - hi);
+                    uint32_t in = 0u;                          // rows in view
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) in |= tile.sees(x + 4 * c + e) ? 0xffu << (8 * e) : 0u;
                     mk = __vmaxu4(mk, kw[c] & in & ~__vcmpeq4(kw[c], 0xffffffffu));       // (255: a row of NaN)
                     mv = __vmaxu4(mv, vw[c] & in & ~__vcmpeq4(vw[c], 0xffffffffu));
                 }
@@ -232,11 +204,10 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
             auto scales = [&](int j, uint32_t& fk, uint32_t& fv) {
                 fk = fv = 0xffffffffu;
                 if (j >= w.j1) return;
-                int x0, lo, hi;
-                const bool summ = w.at(j, x0, lo, hi);
-                const int x = x0 + row;
-                if (x < lo || x >= hi) return;
-                const int page = paged_page(a, t.b, summ, x);
+                const auto tile = w.at(j);
+                const int x = tile.x0 + row;
+                if (!tile.sees(x)) return;
+                const int page = paged_page(a, t.b, tile.summ, x);
                 if (page < 0) return;
                 const int64_t at = (((int64_t)page * a.Hkv + hk) << a.page_shift) + (x & ((1 << a.page_shift) - 1));
                 fk = factor(__ldcg(a.ke + at), top_k);
@@ -313,12 +284,11 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
             if (lane == 0) { prefetch_tensormap(&maps.k); prefetch_tensormap(&maps.v); }
             // page of lane's rows of tile j; num_pages (a box of zeros) where nobody sees any of them
             auto find = [&](int j) {
-                int x0, lo, hi;
                 if (j >= w.j1 || lane >= pages) return a.num_pages;
-                const bool summ = w.at(j, x0, lo, hi);
-                const int x = x0 + (lane << a.page_shift);
-                if (x >= hi || x + (1 << a.page_shift) <= lo) return a.num_pages;
-                const int page = paged_page(a, t.b, summ, x);
+                const auto tile = w.at(j);
+                const int x = tile.x0 + (lane << a.page_shift);
+                if (!tile.sees_any(x, 1 << a.page_shift)) return a.num_pages;
+                const int page = paged_page(a, t.b, tile.summ, x);
                 if (page < 0) { atomicCAS(a.status, 0, KSA_PAGED_STATUS_BAD_PAGE); return a.num_pages; }
                 return page;
             };
@@ -399,12 +369,11 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                 for (int j = 0; j < T && alive; ++j) {
                     wait(bar(Cfg::kVFull) + 8u * stage, ring_phase, kStatusWaitKvFull);
                     if constexpr (!E4M3) {
-                        int x0, lo, hi_row;
-                        w.at(w.j0 + j, x0, lo, hi_row);
-                        if (alive && (x0 < lo || x0 + kPtTile > hi_row)) {      // rows outside the range: zeros
+                        const auto tile = w.at(w.j0 + j);
+                        if (alive && !tile.sees_all()) {       // rows that nobody sees: zeros
                             const uint32_t base = sV + stage * Cfg::kTileBytes + (uint32_t)(lane & 7) * 16u;
                             for (int r = lane >> 3; r < kPtTile; r += 4)
-                                if (x0 + r < lo || x0 + r >= hi_row)
+                                if (!tile.sees(tile.x0 + r))
 #pragma unroll
                                     for (int h = 0; h < Cfg::kHalves; ++h) pt_st_shared4(base + h * 16384 + r * 128, 0u, 0u, 0u, 0u);
                             fence_proxy_async();
@@ -446,7 +415,10 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
         float m_used = -INFINITY, l_run = 0.f;
         const int nrow = max(tokens, 0) * a.G;
         const int r_in = min(row, max(nrow - 1, 0));                           // rows past the last mimic it; never stored
-        const int x = t.x0 + u * per + r_in / a.G;
+        const int token = u * per + r_in / a.G;
+        bool is_summ;
+        const int x = paged_token(a, t, token, is_summ);
+        const int64_t prow = t.mixed ? t.row0 + token : paged_row(a, t, x);
         const int head = hk * a.G + r_in % a.G;
         const bool valid = row < nrow;
         bool alive = true;
@@ -454,7 +426,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
         if (u < nh) {
             // ---- Q: this thread's row, K-major with 128-byte swizzle ----
             {
-                const uint16_t* q = a.q + paged_row(a, t, x) * a.q_st + head * a.q_sh;
+                const uint16_t* q = a.q + prow * a.q_st + head * a.q_sh;
                 const uint32_t d = sQ + u * Cfg::kTileBytes + row * 128;
                 uint4 y[D / 8];
 #pragma unroll
@@ -486,7 +458,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
             v_back = e8m0_factor(top_v) * 0.0078125f;
         }
         if (u < nh) {
-            const PagedView see = paged_view(a, t.summ, x);
+            const PagedView see = paged_view(a, is_summ, x);
             const float scale_log2 = E4M3 ? a.scale_log2 * q_back : a.scale_log2;
             uint32_t sf_phase = 0, pv_phase = 0;
             int rel_k = 0, rel_v = 0;                        // the stages handed back next, by the last query tile's first thread
@@ -518,9 +490,8 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                 __syncwarp();
                 if (lane == 0) mbar_arrive_relaxed(bar(Cfg::kLoaded + u));
                 // the row's own range, where the tile holds an end of some row's
-                int x0, lo, hi;
-                const bool summ = w.at(w.j0 + j, x0, lo, hi);
-                const int ca = (summ ? see.s_lo : see.t_lo) - x0, cb = (summ ? see.s_hi : see.t_hi) - x0;    // visible columns
+                const auto tile = w.at(w.j0 + j);
+                const int ca = (tile.summ ? see.s_lo : see.t_lo) - tile.x0, cb = (tile.summ ? see.s_hi : see.t_hi) - tile.x0;    // visible columns
                 if (__any_sync(0xffffffffu, ca > 0 || cb < kPtTile)) {
                     const uint32_t width = (uint32_t)max(cb - ca, 0);
 #pragma unroll
@@ -609,7 +580,6 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
             // ---- epilogue: O / l -> bf16 at the row's place, LSE ----
             if (u < nh && alive) {
                 const float inv_l = v_back / l_run;
-                const int64_t prow = paged_row(a, t, x);
                 const bool store = valid && ksa_in_bounds(prow >= 0 && prow < a.rows && head < a.Hq, a.status);
                 // a row stands in one lane: four lanes exchange 64 bytes of their rows, so that a store touches 8 lines, not 32
                 const int64_t off = store ? prow * a.o_st + (int64_t)head * a.o_sh : -1;
@@ -659,7 +629,6 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                         pt_st_shared4(d + (uint32_t)((c * 8 + (e ^ (row & 7))) * 16), o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
                 }
                 asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(part_ml + (u * 128 + row) * 8), "f"(m_used), "f"(l_run) : "memory");
-                const int64_t prow = paged_row(a, t, x);
                 const bool store = valid && ksa_in_bounds(prow >= 0 && prow < a.rows && head < a.Hq, a.status);
                 const uint64_t off = store ? (uint64_t)(prow * a.o_st + (int64_t)head * a.o_sh) : ~0ull, lse = (uint64_t)((int64_t)head * a.rows + prow);
                 pt_st_shared4(part_to + (u * 128 + row) * 16, (uint32_t)off, (uint32_t)(off >> 32), (uint32_t)lse, (uint32_t)(lse >> 32));
@@ -718,6 +687,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
     }
     }
 
+    if (a.beside == 2) pdl_wait();                          // whoever waits for this kernel finds both done
     tc_fence_before();
     __syncthreads();
     if (warp == 8) tmem_dealloc(tmem, 512);

@@ -265,6 +265,7 @@ def test_peaked_and_spread_scores(ctx, fmt, n):
     (64, 8, 2, 16, 2, 64, 128, 0, [(66, 330), (70, 300)], 0),
     (8, 0, 1 << 20, 16, 4, 128, 64, 0, [(300, 520)], 0),
     (8, 1, 0, 32, 4, 128, 16, 0, [(9, 300)], 0),
+    (8, 1, 5, 16, 2, 128, 32, 0, [(900, 1), (13, 1400), (0, 0), (300, 2), (44, 17)], 2),      # single tokens among them
 ])
 def test_long_runs_over_e4m3(ctx, k, m, C, Hq, Hkv, D, ps, flags, spans, pad):
     """With the workspace (the rows in view as bf16 pages) and without: each against the reference.  Pages before every window are
@@ -280,6 +281,7 @@ def test_long_runs_over_e4m3(ctx, k, m, C, Hq, Hkv, D, ps, flags, spans, pad):
     ws.fill_(255)                                             # (as bf16: NaN)
     before = ctx.launch_count()
     for how, launches in ((dict(workspace=ws), 2), (dict(workspace=ws[:256]), 1), (dict(), 2)):
+        launches += len(spans) >= 4                           # the kernel for sequences of few rows, beside the other
         out, lse = s.attn(spans, pad, **how)
         assert ctx.launch_count() == before + launches
         before += launches
@@ -408,6 +410,23 @@ def test_pieces_equal_the_forward_pass_and_go_on_in_the_contiguous_cache(ctx):
     out, lse = s.attn([(L, 1)])
     s.check(out, lse, [(L, 1)])
     s.check(step_out, step_lse.t().contiguous(), [(L, 1)])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 128), (16, 1, 64), (16, 2, 64), (20, 1, 128)])
+def test_tokens_and_prompts_in_one_call(ctx, fmt, Hq, Hkv, D):
+    """Sequences of one row to hundreds in a call, more than 32 of them, in and out of order: every row by the kernel it falls to.  Many
+    calls after another, each appending what the next attends to."""
+    lens = [700, 40, 300, 33, 1, 9, 150] + [20 + 7 * i for i in range(30)]
+    s = Server(ctx, 8, 1, 4, Hq, Hkv, D, 16, fmt, lens, seed=23)
+    at = [n // 2 for n in lens]
+    s.append([(0, n) for n in at])
+    for step in range(3):
+        spans = [(a, min(lens[b] - a, [1, 130, 3, 0, 60, 2, 17][(b + step) % 7] if b < 7 else 1)) for b, a in enumerate(at)]
+        s.append(spans, pad=step)
+        out, lse = s.attn(spans, pad=step)
+        s.check(out, lse, spans, sample=6)
+        at = [a + n for a, n in spans]
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])

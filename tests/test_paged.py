@@ -22,9 +22,22 @@ int texts(const Shape* a, int row) { return ksa::paged_texts(*a, row); }
 int entry(const Shape* a, int e) { return ksa::paged_entry(*a, e); }
 int lengths_ok(const Shape* a, int row0, int r1, int first) { return ksa::paged_lengths_ok(*a, row0, r1, first); }
 void view(const Shape* a, int summ, int x, int* v) { auto w = ksa::paged_view(*a, summ, x); v[0] = w.t_lo; v[1] = w.t_hi; v[2] = w.s_lo; v[3] = w.s_hi; }
-void tile_view(const Shape* a, int summ, int x0, int n, int* v) { ksa::PagedTile t{0, summ != 0, x0, n, 0, 0}; auto w = ksa::paged_tile_view(*a, t); v[0] = w.t_lo; v[1] = w.t_hi; v[2] = w.s_lo; v[3] = w.s_hi; }
+void tile_view(const Shape* a, int summ, int x0, int n, int* v) { ksa::PagedTile t{0, summ != 0, false, x0, n, 0, 0}; auto w = ksa::paged_tile_view(*a, t); v[0] = w.t_lo; v[1] = w.t_hi; v[2] = w.s_lo; v[3] = w.s_hi; }
 void range(const Shape* a, int first, int n, int summ, int* v) { auto r = ksa::paged_range(*a, first, n, summ != 0); v[0] = r.lo; v[1] = r.hi; v[2] = r.gap_lo; v[3] = r.gap_hi; }
-long long row(const Shape* a, int summ, int x, int row0, int first) { ksa::PagedTile t{0, summ != 0, 0, 0, row0, first}; return ksa::paged_row(*a, t, x); }
+int token(const Shape* a, int first, int i, int* summ) { ksa::PagedTile t{0, false, true, first, 0, 0, first}; bool s; int x = ksa::paged_token(*a, t, i, s); *summ = s; return x; }
+// tiles of 16 rows: (stream, first row, first row seen of 16 as bits, all seen) of each
+int walk(const Shape* a, int mixed, int summ, int x0, int n, int split, int parts, int* out) {
+    ksa::PagedTile t{0, summ != 0, mixed != 0, x0, n, 0, x0};
+    ksa::PagedWalk<16> w;
+    w.init(*a, t, split, parts);
+    for (int j = w.j0; j < w.j1; ++j, out += 5) {
+        auto k = w.at(j);
+        out[0] = k.summ; out[1] = k.x0; out[2] = 0; out[3] = k.sees_all(); out[4] = 0;
+        for (int i = 0; i < 16; ++i) { out[2] |= k.sees(k.x0 + i) << i; if (i % 4 == 0) out[4] |= k.sees_any(k.x0 + i, 4) << (i / 4); }
+    }
+    return w.j1 - w.j0;
+}
+long long row(const Shape* a, int summ, int x, int row0, int first) { ksa::PagedTile t{0, summ != 0, false, 0, 0, row0, first}; return ksa::paged_row(*a, t, x); }
 }
 """
 
@@ -94,6 +107,40 @@ def test_what_a_run_of_rows_sees(index, k, m, C, flags):
                 want = [w[1] for i, w in enumerate(where) if see[i] and w[0] == kind]
                 # (text between the windows of two rows that are far apart is no case: a run's windows overlap or touch)
                 assert got == want, (first, n, kind)
+
+
+@pytest.mark.parametrize("k,m,C,flags", [(8, 1, 3, 0), (8, 1, 0, 0), (64, 8, 1, 0), (1, 1, 5, 0), (3, 2, 2, 1), (8, 0, 1 << 20, 0), (2, 1, 40, 0), (5, 3, 1, 0)])
+def test_key_tiles_of_a_query_tile(index, k, m, C, flags):
+    """Every key tile once, over any number of parts; of it exactly the rows that some row of the query tile sees."""
+    a = Shape(k, m, C, 1 << 20, 10, flags)
+    rows = 3 * (k + m) * max(2, min(C, 45)) + 4
+    where = ref.places(k, m, rows)
+    sees = [ref.visible(k, m, C, i, rows, bool(flags & 1)) for i in range(rows)]
+    buf = (ctypes.c_int * (5 * 4096))()
+    tiles = [(True, False, first, n, list(range(first, min(rows, first + n)))) for first in range(0, rows, max(1, rows // 40)) for n in (1, 2, 7, k + m, 40)]
+    for kind in (False, True):
+        of = [i for i, w in enumerate(where) if w[0] == kind]
+        tiles += [(False, kind, where[of[lo]][1], len(of[lo:lo + n]), of[lo:lo + n]) for lo in range(0, len(of), max(1, len(of) // 30)) for n in (1, 5, 33)]
+    for mixed, kind, x0, n, members in tiles:
+        if mixed and len(members) < n:
+            continue
+        see = np.any([sees[i] for i in members], axis=0)
+        want = {(w[0], w[1]) for i, w in enumerate(where) if see[i]}
+        for parts in (1, 3):
+            got, seen = [], set()
+            for split in range(parts):
+                cnt = index.walk(ctypes.byref(a), int(mixed), int(kind), x0, n, split, parts, buf)
+                for j in range(cnt):
+                    summ, first, bits, whole, quads = buf[5 * j:5 * j + 5]
+                    got.append((bool(summ), first))
+                    seen |= {(bool(summ), first + i) for i in range(16) if bits >> i & 1}
+                    assert bool(whole) == (bits == 0xffff)
+                    assert all(not (bits >> (4 * i) & 15) or quads >> i & 1 for i in range(4))     # (a run may be fetched for nothing, never missed)
+            assert len(set(got)) == len(got) and all(f % 16 == 0 for _, f in got)
+            assert seen == want, (mixed, kind, x0, n)
+    s = ctypes.c_int()
+    for i in range(30):
+        assert (index.token(ctypes.byref(a), 11, i, ctypes.byref(s)), bool(s.value)) == (ref.places(k, m, 12 + i)[11 + i][1], ref.places(k, m, 12 + i)[11 + i][0])
 
 
 def test_workspace_of_long_runs_over_e4m3():
