@@ -365,6 +365,7 @@ static PagedArgs paged_args(ksa_ctx* ctx, const ksa_paged_kv* kv, const ksa_page
     a.v_st = p->v_stride_tok; a.v_sh = p->v_stride_head; a.o_st = p->o_stride_tok; a.o_sh = p->o_stride_head;
     a.B = p->batch; a.rows = p->num_rows; a.kk = p->chunk_len; a.m = p->summaries_per_chunk; a.C = p->window_chunks;
     a.Hq = p->num_q_heads; a.Hkv = p->num_kv_heads; a.G = a.Hq / a.Hkv; a.D = p->head_dim;
+    a.by_chunk = PagedDiv::by(a.kk + a.m); a.by_k = PagedDiv::by(a.kk); a.by_m = PagedDiv::by(a.m);
     a.page_shift = p->page_rows == 16 ? 4 : p->page_rows == 32 ? 5 : p->page_rows == 64 ? 6 : 7;
     a.num_pages = p->num_pages; a.text_cols = p->text_cols; a.summ_cols = p->summ_cols;
     a.flags = p->flags;

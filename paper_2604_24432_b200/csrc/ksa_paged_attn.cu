@@ -137,9 +137,9 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
     if (a.beside == 0) ptx::pdl_launch_dependents();
     ptx::pdl_wait();
     if (a.beside == 1) ptx::pdl_launch_dependents();           // the kernel behind does not wait for this one, but for those before
-    const int split = (int)blockIdx.x % a.nsplit, unit = (int)blockIdx.x / a.nsplit;
-    const int hb = unit % a.head_blocks, hk = unit / a.head_blocks % a.Hkv;
-    const PagedTile t = paged_tile<false>(a, unit / a.head_blocks / a.Hkv);
+    const int unit = (int)blockIdx.x >> a.split_shift, split = (int)blockIdx.x - (unit << a.split_shift);
+    const int item = a.by_heads(unit), hkb = unit - item * a.Hkv * a.head_blocks, hk = a.by_group(hkb), hb = hkb - hk * a.head_blocks;
+    const PagedTile t = paged_tile<false>(a, item);
     if (t.b < 0) return;                                       // (the whole cluster)
     const int l4 = lane >> 2, c2 = (lane & 3) * 2;             // fragment row and column pair
     // the tile's rows: (token, head), heads `head0 ..` of the group
@@ -543,9 +543,12 @@ cudaError_t launch_paged_attn(const PagedArgs& args, bool e4m3, int query_rows, 
     const int n = query_rows <= 8 ? 1 : 2;
     a.tokens_per_tile = a.G <= 8 * n ? 8 * n / a.G : 1;
     a.head_blocks = (a.G + 8 * n - 1) / (8 * n);
+    a.by_tile = PagedDiv::by(a.tokens_per_tile);
     const int64_t units = paged_most_tiles(a) * a.Hkv * a.head_blocks;
     const int64_t rows = ((int64_t)a.text_cols + (a.m > 0 ? a.summ_cols : 0)) << a.page_shift;      // of a sequence, at most
     a.nsplit = paged_splits(units, rows / 64, num_sms);
+    while (1 << a.split_shift < a.nsplit) ++a.split_shift;
+    a.by_heads = PagedDiv::by(a.Hkv * a.head_blocks); a.by_group = PagedDiv::by(a.head_blocks);
     const int panel = a.D * (e4m3 ? 1 : 2) < 128 ? 64 : 128;
     const CUtensorMapSwizzle swizzle = panel == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B;
     PgMaps maps;

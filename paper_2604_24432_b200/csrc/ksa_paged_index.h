@@ -1,6 +1,6 @@
 // Index arithmetic of the paged KV cache: which row is which token, where it lies, what it sees.  Plain C++ for both sides: the
 // kernels use it, and the tests compile it for the host and compare it with Eqs. 1 and 3 row by row.
-// `A` holds kk, m, C (chunk length, summaries, window), flags, rows and num_pages.
+// `A` holds kk, m, C (chunk length, summaries, window), by_chunk, by_k, by_m (divisors k + m, k and m), flags, rows and num_pages.
 #pragma once
 #include <stdint.h>
 
@@ -15,6 +15,22 @@
 
 namespace ksa {
 
+// x / d for 0 <= x < 2^31 as a product: with l the least number with 2^l >= d and mul = floor(2^32 (2^l - d) / d) + 1,
+// x / d = (floor(x mul / 2^32) + x) >> l (Granlund and Montgomery, 1994).  (A division is some twenty dependent instructions, and a kernel
+// goes through about ten before its first load.)
+struct PagedDiv {
+    uint32_t mul; int32_t shift;
+    static inline PagedDiv by(int d)                   // (host)
+    {
+        PagedDiv v{0, 0};
+        if (d < 1) return v;
+        while ((1ll << v.shift) < d) ++v.shift;
+        v.mul = (uint32_t)((((1ull << v.shift) - (uint64_t)d) << 32) / (uint64_t)d + 1);
+        return v;
+    }
+    KSA_HD int operator()(int x) const { return (int)(((uint32_t)(((uint64_t)(uint32_t)x * mul) >> 32) + (uint32_t)x) >> shift); }
+};
+
 // Whether a sequence can have the packed rows [row0, r1), the first of them its row `first` (at most 2^30 rows a sequence).
 template <class A> KSA_HD bool paged_lengths_ok(const A& a, int row0, int r1, int first)
 {
@@ -26,14 +42,14 @@ template <class A> KSA_HD int paged_entry(const A& a, int entry) { return entry 
 // A row of Eq. 1: text or summary, and its number among those.
 template <class A> KSA_HD int paged_place(const A& a, int row, bool& summ)
 {
-    const int s = a.kk + a.m, c = row / s, r = row - c * s;
+    const int c = a.by_chunk(row), r = row - c * (a.kk + a.m);
     summ = r >= a.kk;
     return summ ? c * a.m + (r - a.kk) : c * a.kk + r;
 }
 // Text tokens (summaries) among the first `row` rows of a sequence.
 template <class A> KSA_HD int paged_texts(const A& a, int row)
 {
-    const int s = a.kk + a.m, c = row / s, r = row - c * s;
+    const int c = a.by_chunk(row), r = row - c * (a.kk + a.m);
     return c * a.kk + (r < a.kk ? r : a.kk);
 }
 
@@ -59,7 +75,8 @@ template <class A> KSA_HD int paged_token(const A& a, const PagedTile& t, int i,
 template <class A> KSA_HD int64_t paged_row(const A& a, const PagedTile& t, int x)
 {
     const int64_t s = a.kk + a.m;
-    const int64_t row = t.summ ? (int64_t)(x / a.m) * s + a.kk + x % a.m : (int64_t)(x / a.kk) * s + x % a.kk;
+    const int c = t.summ ? a.by_m(x) : a.by_k(x);
+    const int64_t row = t.summ ? c * s + a.kk + (x - c * a.m) : c * s + (x - c * a.kk);
     return t.row0 + (row - t.first);
 }
 
@@ -69,11 +86,11 @@ template <class A> KSA_HD PagedView paged_view(const A& a, bool summ, int x)
 {
     PagedView w;
     if (!summ) {                                       // Eq. 3
-        const int c = x / a.kk, far = c > a.C ? c - a.C : 0;
+        const int c = a.by_k(x), far = c > a.C ? c - a.C : 0;
         w.t_lo = far * a.kk; w.t_hi = x + 1;
         w.s_lo = 0; w.s_hi = far * a.m;
     } else {                                           // own chunk (Sec. 2.2.1)
-        const int c = x / a.m;
+        const int c = a.by_m(x);
         w.t_lo = c * a.kk; w.t_hi = w.t_lo + a.kk;
         w.s_lo = c * a.m;
         w.s_hi = (a.flags & KSA_FLAG_SUMMARY_TEXT_ONLY) ? w.s_lo : x + 1;

@@ -120,7 +120,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
 
     if (tid == 0) {
         for (int t = 0; t < 2; ++t) {
-            mbar_init(bar(Cfg::kQFull + t), 128);       // one arrival per row's thread
+            mbar_init(bar(Cfg::kQFull + t), 128);       // one arrival per thread that writes it
             mbar_init(bar(Cfg::kSFull + t), 1);
             mbar_init(bar(Cfg::kLoaded + t), 4);        // one arrival per softmax warp
             mbar_init(bar(Cfg::kPFull + t), 4);
@@ -146,9 +146,9 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
     if (a.beside != 2) pdl_wait();                          // (beside the kernel in front, which has waited for those before it)
     pdl_launch_dependents();
 
-    const int split = (int)blockIdx.x % a.nsplit, unit = (int)blockIdx.x / a.nsplit;
-    const int hk = unit % a.Hkv;
-    const PagedTile t = paged_tile<true>(a, unit / a.Hkv);       // up to 2 * per tokens
+    const int unit = (int)blockIdx.x >> a.split_shift, split = (int)blockIdx.x - (unit << a.split_shift);
+    const int item = a.by_heads(unit), hk = unit - item * a.Hkv;
+    const PagedTile t = paged_tile<true>(a, item);       // up to 2 * per tokens
     const int per = a.tokens_per_tile / 2;
     if (t.b >= 0) {                                         // (the same for the whole cluster)
     PagedWalk<kPtTile> w;
@@ -415,36 +415,45 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
         float m_used = -INFINITY, l_run = 0.f;
         const int nrow = max(tokens, 0) * a.G;
         const int r_in = min(row, max(nrow - 1, 0));                           // rows past the last mimic it; never stored
-        const int token = u * per + r_in / a.G;
+        const int in_tile = a.by_group(r_in), token = u * per + in_tile;
         bool is_summ;
         const int x = paged_token(a, t, token, is_summ);
         const int64_t prow = t.mixed ? t.row0 + token : paged_row(a, t, x);
-        const int head = hk * a.G + r_in % a.G;
+        const int head = hk * a.G + r_in - in_tile * a.G;
         const bool valid = row < nrow;
         bool alive = true;
         float q_back = 1.f, v_back = 1.f;                                      // e4m3: what the scores and O are to be multiplied with
         if (u < nh) {
-            // ---- Q: this thread's row, K-major with 128-byte swizzle ----
+            // ---- Q: a warp's 32 rows, K-major with 128-byte swizzle; D / 8 lanes bring a row (a row per thread took 4.4 us of a
+            // CTA's 11.7 with one key tile) ----
             {
-                const uint16_t* q = a.q + prow * a.q_st + head * a.q_sh;
-                const uint32_t d = sQ + u * Cfg::kTileBytes + row * 128;
-                uint4 y[D / 8];
+                constexpr int kLanes = D / 8, kRowsPass = 32 / kLanes;
+                const int64_t off = prow * a.q_st + head * a.q_sh;
+                const int c = lane % kLanes, r0 = lane / kLanes;
+                uint4 y[kLanes];
 #pragma unroll
-                for (int c = 0; c < D / 8; ++c) y[c] = __ldcg(reinterpret_cast<const uint4*>(q + c * 8));
+                for (int i = 0; i < kLanes; ++i)
+                    y[i] = __ldcg(reinterpret_cast<const uint4*>(a.q + __shfl_sync(0xffffffffu, off, i * kRowsPass + r0) + c * 8));
                 if constexpr (E4M3) {                        // as f16, the row's largest value taken to 2^8 or more (below 2^9)
-                    uint32_t top = 0;
 #pragma unroll
-                    for (int c = 0; c < D / 8; ++c)
-                        top = __vmaxu2(top, __vmaxu2(__vmaxu2(y[c].x & 0x7fff7fffu, y[c].y & 0x7fff7fffu), __vmaxu2(y[c].z & 0x7fff7fffu, y[c].w & 0x7fff7fffu)));
-                    const int e = min(max((int)(max(top >> 16, top & 0xffffu) >> 7) - 8, 1), 253);
-                    const float f = __uint_as_float((uint32_t)(254 - e) << 23);
-                    q_back = __uint_as_float((uint32_t)e << 23);
-                    auto two = [&](uint32_t& z) { z = pack_f16x2(__uint_as_float(z << 16) * f, __uint_as_float(z & 0xffff0000u) * f); };
+                    for (int i = 0; i < kLanes; ++i) {
+                        uint32_t top = __vmaxu2(__vmaxu2(y[i].x & 0x7fff7fffu, y[i].y & 0x7fff7fffu), __vmaxu2(y[i].z & 0x7fff7fffu, y[i].w & 0x7fff7fffu));
 #pragma unroll
-                    for (int c = 0; c < D / 8; ++c) { two(y[c].x); two(y[c].y); two(y[c].z); two(y[c].w); }
+                        for (int o = kLanes / 2; o > 0; o >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
+                        const int e = min(max((int)(max(top >> 16, top & 0xffffu) >> 7) - 8, 1), 253);
+                        const float f = __uint_as_float((uint32_t)(254 - e) << 23);
+                        auto two = [&](uint32_t& z) { z = pack_f16x2(__uint_as_float(z << 16) * f, __uint_as_float(z & 0xffff0000u) * f); };
+                        two(y[i].x); two(y[i].y); two(y[i].z); two(y[i].w);
+                        const int mine = __shfl_sync(0xffffffffu, e, lane % kRowsPass * kLanes);
+                        if (lane / kRowsPass == i) q_back = __uint_as_float((uint32_t)mine << 23);      // (of this thread's own row)
+                    }
                 }
+                const uint32_t d = sQ + u * Cfg::kTileBytes + (c >> 3) * 16384 + (row & 96) * 128;
 #pragma unroll
-                for (int c = 0; c < D / 8; ++c) pt_st_shared4(d + (c >> 3) * 16384 + (((c & 7) ^ (row & 7)) << 4), y[c].x, y[c].y, y[c].z, y[c].w);
+                for (int i = 0; i < kLanes; ++i) {
+                    const int r = i * kRowsPass + r0;
+                    pt_st_shared4(d + r * 128 + (((c ^ r) & 7) << 4), y[i].x, y[i].y, y[i].z, y[i].w);
+                }
                 fence_proxy_async();
                 mbar_arrive(bar(Cfg::kQFull + u));
             }
@@ -722,11 +731,14 @@ cudaError_t launch_paged_tc(const PagedArgs& args, bool e4m3, int num_sms, Paged
     PagedArgs a = args;
     a.tokens_per_tile = 2 * (kPtTile / a.G);                  // of a CTA: two query tiles
     a.head_blocks = 1;
+    a.by_tile = PagedDiv::by(a.tokens_per_tile); a.by_group = PagedDiv::by(a.G);
     const int64_t units = paged_most_tiles(a) * a.Hkv;
     // rows that a query tile sees, at most
     const int64_t text = std::min((int64_t)a.text_cols << a.page_shift, ((int64_t)a.C + 2) * a.kk + a.tokens_per_tile);
     const int64_t key_tiles = (text + (a.m > 0 ? (int64_t)a.summ_cols << a.page_shift : 0)) / kPtTile;
     a.nsplit = tc_splits(units, key_tiles, a.B, num_sms);
+    a.split_shift = a.nsplit == 4 ? 2 : a.nsplit == 2 ? 1 : 0;
+    a.by_heads = PagedDiv::by(a.Hkv);
     PagedMaps maps;
     const int box_bytes = e4m3 ? a.D : 128;
     const CUtensorMapSwizzle swizzle = e4m3 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B;

@@ -15,18 +15,23 @@ from tests import paged_ref as ref
 
 HOST = r"""
 #include "ksa_paged_index.h"
-struct Shape { int kk, m, C, rows, num_pages; unsigned flags; };
+struct Given { int kk, m, C, rows, num_pages; unsigned flags; };
+struct Shape : Given {
+    ksa::PagedDiv by_chunk, by_k, by_m;
+    Shape(const Given& g) : Given(g), by_chunk(ksa::PagedDiv::by(g.kk + g.m)), by_k(ksa::PagedDiv::by(g.kk)), by_m(ksa::PagedDiv::by(g.m)) {}
+};
 extern "C" {
-int place(const Shape* a, int row, int* summ) { bool s; int x = ksa::paged_place(*a, row, s); *summ = s; return x; }
-int texts(const Shape* a, int row) { return ksa::paged_texts(*a, row); }
-int entry(const Shape* a, int e) { return ksa::paged_entry(*a, e); }
-int lengths_ok(const Shape* a, int row0, int r1, int first) { return ksa::paged_lengths_ok(*a, row0, r1, first); }
-void view(const Shape* a, int summ, int x, int* v) { auto w = ksa::paged_view(*a, summ, x); v[0] = w.t_lo; v[1] = w.t_hi; v[2] = w.s_lo; v[3] = w.s_hi; }
-void tile_view(const Shape* a, int summ, int x0, int n, int* v) { ksa::PagedTile t{0, summ != 0, false, x0, n, 0, 0}; auto w = ksa::paged_tile_view(*a, t); v[0] = w.t_lo; v[1] = w.t_hi; v[2] = w.s_lo; v[3] = w.s_hi; }
-void range(const Shape* a, int first, int n, int summ, int* v) { auto r = ksa::paged_range(*a, first, n, summ != 0); v[0] = r.lo; v[1] = r.hi; v[2] = r.gap_lo; v[3] = r.gap_hi; }
-int token(const Shape* a, int first, int i, int* summ) { ksa::PagedTile t{0, false, true, first, 0, 0, first}; bool s; int x = ksa::paged_token(*a, t, i, s); *summ = s; return x; }
+int divide(int x, int d) { return ksa::PagedDiv::by(d)(x); }
+int place(const Given* g, int row, int* summ) { Shape shape(*g); const Shape* a = &shape; bool s; int x = ksa::paged_place(*a, row, s); *summ = s; return x; }
+int texts(const Given* g, int row) { Shape shape(*g); const Shape* a = &shape; return ksa::paged_texts(*a, row); }
+int entry(const Given* g, int e) { Shape shape(*g); const Shape* a = &shape; return ksa::paged_entry(*a, e); }
+int lengths_ok(const Given* g, int row0, int r1, int first) { Shape shape(*g); const Shape* a = &shape; return ksa::paged_lengths_ok(*a, row0, r1, first); }
+void view(const Given* g, int summ, int x, int* v) { Shape shape(*g); const Shape* a = &shape; auto w = ksa::paged_view(*a, summ, x); v[0] = w.t_lo; v[1] = w.t_hi; v[2] = w.s_lo; v[3] = w.s_hi; }
+void tile_view(const Given* g, int summ, int x0, int n, int* v) { Shape shape(*g); const Shape* a = &shape; ksa::PagedTile t{0, summ != 0, false, x0, n, 0, 0}; auto w = ksa::paged_tile_view(*a, t); v[0] = w.t_lo; v[1] = w.t_hi; v[2] = w.s_lo; v[3] = w.s_hi; }
+void range(const Given* g, int first, int n, int summ, int* v) { Shape shape(*g); const Shape* a = &shape; auto r = ksa::paged_range(*a, first, n, summ != 0); v[0] = r.lo; v[1] = r.hi; v[2] = r.gap_lo; v[3] = r.gap_hi; }
+int token(const Given* g, int first, int i, int* summ) { Shape shape(*g); const Shape* a = &shape; ksa::PagedTile t{0, false, true, first, 0, 0, first}; bool s; int x = ksa::paged_token(*a, t, i, s); *summ = s; return x; }
 // tiles of 16 rows: (stream, first row, first row seen of 16 as bits, all seen) of each
-int walk(const Shape* a, int mixed, int summ, int x0, int n, int split, int parts, int* out) {
+int walk(const Given* g, int mixed, int summ, int x0, int n, int split, int parts, int* out) { Shape shape(*g); const Shape* a = &shape;
     ksa::PagedTile t{0, summ != 0, mixed != 0, x0, n, 0, x0};
     ksa::PagedWalk<16> w;
     w.init(*a, t, split, parts);
@@ -37,7 +42,7 @@ int walk(const Shape* a, int mixed, int summ, int x0, int n, int split, int part
     }
     return w.j1 - w.j0;
 }
-long long row(const Shape* a, int summ, int x, int row0, int first) { ksa::PagedTile t{0, summ != 0, false, 0, 0, row0, first}; return ksa::paged_row(*a, t, x); }
+long long row(const Given* g, int summ, int x, int row0, int first) { Shape shape(*g); const Shape* a = &shape; ksa::PagedTile t{0, summ != 0, false, 0, 0, row0, first}; return ksa::paged_row(*a, t, x); }
 }
 """
 
@@ -166,6 +171,14 @@ def test_entries_and_lengths(index):
     assert ok(0, 0, 0) and ok(0, 100, 0) and ok(99, 100, 2**30 - 1) and ok(100, 100, 2**30)
     assert not ok(-1, 5, 0) and not ok(5, 4, 0) and not ok(0, 101, 0) and not ok(0, 1, -1) and not ok(0, 1, 2**30)
     assert not ok(-2**31, 2**31 - 1, 0) and not ok(0, -5, 0) and not ok(0, 1, 2**31 - 1)
+
+
+def test_division(index):
+    rng = np.random.default_rng(0)
+    for d in [1, 2, 3, 5, 7, 8, 9, 64, 72, 127, 128, 641, 65535, 65536, 10**9, 2**30] + [int(x) for x in rng.integers(1, 2**31 - 1, 40)]:
+        for x in [0, 1, d - 1, d, d + 1, 2 * d - 1, 2**31 - 1, 2**31 - 2, 2**30] + [int(v) for v in rng.integers(0, 2**31, 60)] + [int(q) * d + r for q in rng.integers(0, 2**31 // d + 1, 20) for r in (-1, 0)]:
+            if 0 <= x < 2**31:
+                assert index.divide(x, d) == x // d, (x, d)
 
 
 def test_e4m3_reference_matches_torch():
