@@ -593,7 +593,7 @@ class PagedBatch:
         # what every call passes of the batch
         summ = self.summ_table
         for name, value in (("_size", B), ("_index", self.cached.get_device()), ("_cols", (self.text_table.shape[1], 0 if summ is None else summ.shape[1])),
-                            ("_ptrs", (self.text_table.data_ptr(), 0 if summ is None else summ.data_ptr(), self.cached.data_ptr(), self.cu_rows.data_ptr()))):
+                            ("_ptrs", struct.pack("@4N", self.text_table.data_ptr(), 0 if summ is None else summ.data_ptr(), self.cached.data_ptr(), self.cu_rows.data_ptr()))):
             object.__setattr__(self, name, value)
 
 
@@ -642,29 +642,38 @@ class PagedCache:
         self._fixed = (s.k, s.m, s.C, s.Hq, s.Hkv, s.D, s.scale, s.flags, KSA_KV_E4M3 if s.fmt == "e4m3" else KSA_KV_BF16, s.page_rows, s.num_pages)
         self._strides = self.kpages.stride()[:3]
         self._quantised = s.fmt == "e4m3"
-        self._pools = tuple(0 if t is None else t.data_ptr() for t in self._tensors)
+        self._pools = struct.pack("@4N", *(0 if t is None else t.data_ptr() for t in self._tensors))
+        self._packed = {}                            # parameter structures by the numbers in them
+        L = lib()
+        self._append, self._gather, self._attn = L.ksa_paged_append, L.ksa_paged_gather, L.ksa_paged_attn
 
     def _rows(self, t, rows: int, H: int):
         """Strides of a tensor of rows, checked."""
         D = self._spec.D
-        st = t.stride()
-        if t.shape != (rows, H, D) or t.dtype is not self._bf16 or t.get_device() != self._index or st[2] != 1:
+        st, sh, d = t.stride()
+        if t.shape != (rows, H, D) or t.dtype is not self._bf16 or t.get_device() != self._index or d != 1:
             raise ValueError("rows must be bf16 [num_rows, heads, head_dim] = %s on cuda:%d, head_dim contiguous" % ((rows, H, D), self._index))
-        return st[0] if rows > 1 else H * D, st[1] if H > 1 else D
+        return st if rows > 1 else H * D, sh if H > 1 else D
 
-    def _params(self, batch: PagedBatch, rows: int, q, k, v, o) -> bytes:
-        # (The structures are packed as bytes: this runs in every call, and a call of one token takes the device some 6 us.)
+    def _params(self, batch: PagedBatch, rows: int, *strides) -> bytes:
+        """ksa_paged_params as bytes.  (Every call passes them, and a call of one token takes the device some 6 us: what the
+        structure is made of is checked each time, the same structure is packed once.)"""
+        key = (batch._size, rows, batch._cols, strides)
+        p = self._packed.get(key)
+        if p is None:
+            if len(self._packed) >= 256:
+                self._packed.clear()
+            p = self._packed[key] = _PAGED_PARAMS.pack(_PAGED_PARAMS.size, batch._size, rows, *self._fixed, *batch._cols, *self._strides, *(x for st in strides for x in st))
         if batch._index != self._index or (batch._cols[1] == 0 and self._spec.m > 0):
             raise ValueError("the batch must be on cuda:%d, with a summ_table" % self._index)
-        return _PAGED_PARAMS.pack(_PAGED_PARAMS.size, batch._size, rows, *self._fixed, *batch._cols, *self._strides, *q, *k, *v, *o)
-
-    def _kv(self, batch: PagedBatch) -> bytes:
-        return _PAGED_KV.pack(*self._pools, *batch._ptrs)
+        return p
 
     def _move(self, fn, name: str, batch: PagedBatch, k, v, stream):
         rows, H = k.shape[0], self._spec.Hkv
         p = self._params(batch, rows, _NO_ROWS, self._rows(k, rows, H), self._rows(v, rows, H), _NO_ROWS)
-        _check(fn(self.ctx.handle, self._kv(batch), k.data_ptr(), v.data_ptr(), p, _current_stream(self.device) if stream is None else stream), name)
+        status = fn(self.ctx.handle, self._pools + batch._ptrs, k.data_ptr(), v.data_ptr(), p, _current_stream(self.device) if stream is None else stream)
+        if status != KSA_OK:
+            raise KsaError(status, name)
 
     def _workspace(self, p: bytes, stream):
         """The workspace that makes the call faster, from torch's allocator (which keeps it until the work before its next use
@@ -681,11 +690,11 @@ class PagedCache:
 
     def append(self, batch: PagedBatch, k, v, stream: Optional[int] = None):
         """ksa_paged_append: k, v [num_rows, Hkv, D] of the batch's new rows into their pages (quantised on the way)."""
-        self._move(lib().ksa_paged_append, "ksa_paged_append", batch, k, v, stream)
+        self._move(self._append, "ksa_paged_append", batch, k, v, stream)
 
     def gather(self, batch: PagedBatch, k, v, stream: Optional[int] = None):
         """ksa_paged_gather: the rows cached[b] .. of every sequence back into k, v [num_rows, Hkv, D]."""
-        self._move(lib().ksa_paged_gather, "ksa_paged_gather", batch, k, v, stream)
+        self._move(self._gather, "ksa_paged_gather", batch, k, v, stream)
 
     def attn(self, batch: PagedBatch, q, out, lse, stream: Optional[int] = None, workspace=None):
         """ksa_paged_attn: q, out [num_rows, Hq, D], lse fp32 [Hq, num_rows]; the rows' own K and V have been appended.
@@ -697,10 +706,11 @@ class PagedCache:
         if workspace is None and self._quantised and rows > batch._size:
             workspace = self._workspace(p, stream)
         ws, nbytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-        _check(lib().ksa_paged_attn(self.ctx.handle, self._kv(batch), q.data_ptr(), out.data_ptr(), lse.data_ptr(), ws, nbytes, p,
-                                    _current_stream(self.device) if stream is None else stream), "ksa_paged_attn")
+        status = self._attn(self.ctx.handle, self._pools + batch._ptrs, q.data_ptr(), out.data_ptr(), lse.data_ptr(), ws, nbytes, p,
+                            _current_stream(self.device) if stream is None else stream)
+        if status != KSA_OK:
+            raise KsaError(status, "ksa_paged_attn")
 
 
 _PAGED_PARAMS = struct.Struct("@9i f I 5i 11q")      # ksa_paged_params
-_PAGED_KV = struct.Struct("@8N")                     # ksa_paged_kv
 _NO_ROWS = (0, 0)                                    # strides of a tensor that a call does not take

@@ -74,74 +74,85 @@ __device__ __forceinline__ int paged_page(const PagedArgs& a, int b, bool summ, 
 }
 
 // ---- query tiles ------------------------------------------------------------------------------------------------------
-// Tile `item` of the call, counted through the sequences (text tiles of a sequence before its summary tiles).  Executed by a
-// whole warp: 32 sequences at a time, these in descending order of what their last row sees.  kMix: a run of rows that fits into
-// a tile is one, text tokens and summaries together.
+// Tile `item` of the call, counted through the sequences (text tiles of a sequence before its summary tiles), for the whole block.
+// The first warp looks for it, 32 sequences at a time, these in descending order of what their last row sees (the others would only
+// compete with it for shuffles and shared memory), and leaves it in `found`.  kMix: a run of rows that fits into a tile is one,
+// text tokens and summaries together.
+struct PagedFound { PagedTile tile; int order[32], keys[32]; };
 template <bool kMix>
-__device__ __forceinline__ PagedTile paged_tile(const PagedArgs& a, int item)
+__device__ __forceinline__ PagedTile paged_tile(const PagedArgs& a, int item, PagedFound& found)
 {
-    const int lane = threadIdx.x & 31, per = a.tokens_per_tile;
-    PagedTile t{-1, false, false, 0, 0, 0, 0};
-    for (int base = 0; base < a.B; base += 32) {
-        int row0 = 0, n = 0, first = 0, t0 = 0, nt = 0, tt = 0, ts = 0;
-        if (base + lane < a.B) {
-            row0 = __ldcg(a.cu + base + lane);
-            first = __ldcg(a.cached + base + lane);
-            paged_seq(a, row0, __ldcg(a.cu + base + lane + 1), first, n);
-            if (n < a.rows_min || n > a.rows_max) n = 0;
-        }
-        if (n > 0) {
-            t0 = paged_texts(a, first);
-            nt = paged_texts(a, first + n) - t0;
-            tt = a.by_tile(nt + per - 1);
-            ts = a.by_tile(n - nt + per - 1);
-            if (kMix && n <= per) { tt = 1; ts = 0; }
-        }
-        int seq = base + lane;
-        if (a.B > 1) {
-            // a lane's place among the 32, by the keys in view (as a number, ties by lane), then everything to its place
-            const bool summ = n > 0 && nt == 0;
-            const PagedView w = paged_view(a, summ, summ ? first + n - t0 - 1 : t0 + max(nt - 1, 0));
-            const int keys = n > 0 ? w.t_hi - w.t_lo + w.s_hi - w.s_lo : -1;
-            int place = 0;
-#pragma unroll
-            for (int o = 0; o < 32; ++o) {
-                const int other = __shfl_sync(0xffffffffu, keys, o);
-                place += other > keys || (other == keys && o < lane);
+    if (threadIdx.x < 32) {
+        const int lane = threadIdx.x, per = a.tokens_per_tile;
+        PagedTile t{-1, false, false, 0, 0, 0, 0};
+        for (int base = 0; base < a.B; base += 32) {
+            int row0 = 0, n = 0, first = 0, t0 = 0, nt = 0, tt = 0, ts = 0;
+            if (base + lane < a.B) {
+                row0 = __ldcg(a.cu + base + lane);
+                first = __ldcg(a.cached + base + lane);
+                paged_seq(a, row0, __ldcg(a.cu + base + lane + 1), first, n);
+                if (n < a.rows_min || n > a.rows_max) n = 0;
             }
-            int from = 0;
+            if (n > 0) {
+                t0 = paged_texts(a, first);
+                nt = paged_texts(a, first + n) - t0;
+                tt = a.by_tile(nt + per - 1);
+                ts = a.by_tile(n - nt + per - 1);
+                if (kMix && n <= per) { tt = 1; ts = 0; }
+            }
+            int seq = base + lane;
+            if (a.B > 1) {
+                // a lane's place among the 32, by the keys in view (ties by lane), then everything to its place
+                const bool summ = n > 0 && nt == 0;
+                const PagedView w = paged_view(a, summ, summ ? first + n - t0 - 1 : t0 + max(nt - 1, 0));
+                const int keys = n > 0 ? w.t_hi - w.t_lo + w.s_hi - w.s_lo : -1;
+                found.keys[lane] = keys;
+                __syncwarp();
+                int place = 0;
 #pragma unroll
-            for (int o = 0; o < 32; ++o) if (__shfl_sync(0xffffffffu, place, o) == lane) from = o;
-            seq = base + from;
-            row0 = __shfl_sync(0xffffffffu, row0, from); n = __shfl_sync(0xffffffffu, n, from); first = __shfl_sync(0xffffffffu, first, from);
-            t0 = __shfl_sync(0xffffffffu, t0, from); nt = __shfl_sync(0xffffffffu, nt, from); tt = __shfl_sync(0xffffffffu, tt, from); ts = __shfl_sync(0xffffffffu, ts, from);
-        }
-        int sum = tt + ts;
+                for (int o = 0; o < 32; o += 4) {
+                    const int4 k = *reinterpret_cast<const int4*>(found.keys + o);
+                    place += (k.x > keys || (k.x == keys && o < lane)) + (k.y > keys || (k.y == keys && o + 1 < lane)) +
+                             (k.z > keys || (k.z == keys && o + 2 < lane)) + (k.w > keys || (k.w == keys && o + 3 < lane));
+                }
+                found.order[place] = lane;
+                __syncwarp();
+                const int from = found.order[lane];
+                seq = base + from;
+                row0 = __shfl_sync(0xffffffffu, row0, from); n = __shfl_sync(0xffffffffu, n, from); first = __shfl_sync(0xffffffffu, first, from);
+                t0 = __shfl_sync(0xffffffffu, t0, from); nt = __shfl_sync(0xffffffffu, nt, from); tt = __shfl_sync(0xffffffffu, tt, from); ts = __shfl_sync(0xffffffffu, ts, from);
+            }
+            int sum = tt + ts;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int up = __shfl_up_sync(0xffffffffu, sum, o);
-            if (lane >= o) sum += up;
+            for (int o = 1; o < 32; o <<= 1) {
+                const int up = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += up;
+            }
+            const int total = __shfl_sync(0xffffffffu, sum, 31);
+            if (item < total) {
+                const int src = __ffs(__ballot_sync(0xffffffffu, sum > item)) - 1;
+                if (lane == src) {
+                    int i = item - (sum - tt - ts);
+                    t.b = seq;
+                    t.row0 = row0;
+                    t.first = first;
+                    t.mixed = kMix && n <= per;
+                    t.summ = i >= tt;
+                    if (t.summ) i -= tt;
+                    const int have = t.mixed ? n : t.summ ? n - nt : nt;
+                    t.x0 = t.mixed ? first : (t.summ ? first - t0 : t0) + i * per;
+                    t.n = min(per, have - i * per);
+                    found.tile = t;
+                }
+                item = -1;
+                break;
+            }
+            item -= total;
         }
-        const int total = __shfl_sync(0xffffffffu, sum, 31);
-        if (item < total) {
-            const int src = __ffs(__ballot_sync(0xffffffffu, sum > item)) - 1;
-            int i = item - __shfl_sync(0xffffffffu, sum - tt - ts, src);
-            tt = __shfl_sync(0xffffffffu, tt, src); nt = __shfl_sync(0xffffffffu, nt, src); t0 = __shfl_sync(0xffffffffu, t0, src);
-            n = __shfl_sync(0xffffffffu, n, src);
-            t.b = __shfl_sync(0xffffffffu, seq, src);
-            t.row0 = __shfl_sync(0xffffffffu, row0, src);
-            t.first = __shfl_sync(0xffffffffu, first, src);
-            t.mixed = kMix && n <= per;
-            t.summ = i >= tt;
-            if (t.summ) i -= tt;
-            const int have = t.mixed ? n : t.summ ? n - nt : nt;
-            t.x0 = t.mixed ? t.first : (t.summ ? t.first - t0 : t0) + i * per;
-            t.n = min(per, have - i * per);
-            return t;
-        }
-        item -= total;
+        if (item >= 0 && lane == 0) found.tile = t;
     }
-    return t;
+    __syncthreads();
+    return found.tile;
 }
 
 // ---- e4m3 rows ------------------------------------------------------------------------------------------------------------

@@ -45,16 +45,21 @@ struct PgCfg {
     static constexpr int kPanelB = kRowB < 128 ? kRowB : 128;   // a box's width: 128 bytes at most with a swizzle
     static constexpr int kPanels = kRowB / kPanelB;
     static constexpr int kRunB = kPgRun * kRowB;                // of K or of V: its panels, 16 rows each
-    static constexpr int kVOff = kSubs * kRunB, kScaleOff = 2 * kVOff;
-    static constexpr int kStageB = kScaleOff + (E4M3 ? 1024 : 0);       // K, V, scale bytes (run by run 16 of K, 16 of V)
+    static constexpr int kVOff = kSubs * kRunB;
+    static constexpr int kStageB = 2 * kVOff;                   // K, V (multiples of 1,024 bytes, which the swizzles repeat after)
+    static constexpr int kScaleB = E4M3 ? 2 * kKeys : 0;        // a stage's scale bytes: run by run 16 of K, 16 of V
     static constexpr int kTxBytes = 2 * kVOff + (E4M3 ? 2 * kKeys : 0);
     static constexpr int kStages = 3;
     static constexpr int kRingB = kStages * kStageB;            // of a warp
     // log2 units.  The reference maximum moves when a score outgrows it by this
     static constexpr float kRescale = 8.0f;
     static constexpr int kLd = D + 4;                           // floats from one row of partial results to the next
-    static constexpr int kMergeB = (kWarps + 1) * kRows * (kLd + 2) * 4;
-    static constexpr int kBarOff = kWarps * kRingB > kMergeB ? kWarps * kRingB : kMergeB;
+    static constexpr int kMergeB = kWarps * kRows * (kLd + 2) * 4;      // the warps' results, over the ring
+    // what the cluster's other CTAs push: memory of its own, this CTA may still be at work
+    static constexpr int kPushOff = kWarps * kRingB > kMergeB ? kWarps * kRingB : kMergeB;
+    static constexpr int kPushO = (kRows * (D / 4) + kPgMaxSplit) * 16, kPushMl = kPgMaxSplit * kRows * 8;
+    static constexpr int kScaleOff = kPushOff + kPushO + kPushMl;       // [warps][stages]
+    static constexpr int kBarOff = kScaleOff + kWarps * kStages * kScaleB;
     static constexpr int kSmemBytes = kBarOff + 8 * kWarps * kStages + 16 + 1024;       // + slack for 1024-byte alignment
     // 16-byte vector c of row r of a run, as the boxes' swizzles place them
     __device__ static __forceinline__ uint32_t at(int r, int c)
@@ -102,18 +107,6 @@ __device__ __forceinline__ uint32_t pg_ld_u8(uint32_t addr)
     asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr));
     return v;
 }
-__device__ __forceinline__ float2 pg_ld_cluster2(uint32_t addr)
-{
-    float2 v;
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ float4 pg_ld_cluster4(uint32_t addr)
-{
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-    return v;
-}
 
 template <int D, bool E4M3, int N>
 __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PgMaps maps)
@@ -134,12 +127,14 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
         ptx::prefetch_tensormap(&maps.v);
     }
     __syncthreads();
+    if (a.nsplit > 1) ptx::cluster_arrive();                   // (waited for before the first access to another CTA's memory)
     if (a.beside == 0) ptx::pdl_launch_dependents();
     ptx::pdl_wait();
     if (a.beside == 1) ptx::pdl_launch_dependents();           // the kernel behind does not wait for this one, but for those before
     const int unit = (int)blockIdx.x >> a.split_shift, split = (int)blockIdx.x - (unit << a.split_shift);
     const int item = a.by_heads(unit), hkb = unit - item * a.Hkv * a.head_blocks, hk = a.by_group(hkb), hb = hkb - hk * a.head_blocks;
-    const PagedTile t = paged_tile<false>(a, item);
+    __shared__ __align__(16) PagedFound found;
+    const PagedTile t = paged_tile<false>(a, item, found);
     if (t.b < 0) return;                                       // (the whole cluster)
     const int l4 = lane >> 2, c2 = (lane & 3) * 2;             // fragment row and column pair
     // the tile's rows: (token, head), heads `head0 ..` of the group
@@ -148,11 +143,26 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
     const PagedView see = paged_tile_view(a, t), first = paged_view(a, t.summ, t.x0), last = paged_view(a, t.summ, t.x0 + t.n - 1);
     const int s_t0 = see.s_lo / kTile, s_tiles = see.s_hi > see.s_lo ? (see.s_hi + kTile - 1) / kTile - s_t0 : 0;
     const int t_t0 = see.t_lo / kTile, tiles = s_tiles + (see.t_hi + kTile - 1) / kTile - t_t0;
-    const int per = (tiles + a.nsplit - 1) / a.nsplit;
+    // the cluster's CTAs that take part: a CTA without two key tiles of its own leaves (the others' barriers do not count it)
+    const int parts = min(a.nsplit, max(1, tiles >> 1));
+    if (split >= parts) return;
+    const int per = (tiles + parts - 1) / parts;
     const int my0 = min(tiles, split * per), my1 = min(tiles, my0 + per);
 
     // First row of the warp's tile j in its stream.
     auto tile_at = [&](int j, bool& summ) { summ = j < s_tiles; return (summ ? s_t0 + j : t_t0 + j - s_tiles) * kTile + warp * kKeys; };
+    // Q, as it comes: columns 4 t .. 4 t + 3 of 16 (bf16 rows: 2 t, 2 t + 1 and 8 + 2 t, 9 + 2 t); on its way beside the first keys
+    uint2 qw[N][D / 16];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int r = min(n * 8 + l4, nrow - 1);
+        const uint16_t* q = a.q + paged_row(a, t, t.x0 + r / heads) * a.q_st + (head0 + r % heads) * a.q_sh;
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+            if constexpr (E4M3) qw[n][kk] = __ldcg(reinterpret_cast<const uint2*>(q + kk * 16 + c2 * 2));
+            else qw[n][kk] = make_uint2(__ldcg(reinterpret_cast<const uint32_t*>(q + kk * 16 + c2)), __ldcg(reinterpret_cast<const uint32_t*>(q + kk * 16 + 8 + c2)));
+        }
+    }
     // Lane u < kSubs brings the tile's run u.  Its page-table entry is fetched a tile ahead of its use; -3: nobody sees the rows.
     auto find_entry = [&](int j) {
         bool summ;
@@ -160,7 +170,7 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
         if (lane >= kSubs || j >= my1 || x >= (summ ? see.s_hi : see.t_hi) || x + kPgRun <= (summ ? see.s_lo : see.t_lo)) return -3;
         return col < cols ? __ldcg((summ ? a.summ_table : a.text_table) + (int64_t)t.b * cols + col) : -2;
     };
-    const uint32_t ring = sbase + warp * Cfg::kRingB, full = bars + 8 * warp * kStages;
+    const uint32_t ring = sbase + warp * Cfg::kRingB, full = bars + 8 * warp * kStages, scales = sbase + Cfg::kScaleOff + warp * kStages * Cfg::kScaleB;
     auto load_tile = [&](int j, int stage, int entry) {
         if (lane == 0) ptx::mbar_arrive_expect_tx(full + 8 * stage, Cfg::kTxBytes);
         __syncwarp();
@@ -180,7 +190,7 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
             }
             if constexpr (E4M3) {
                 const int64_t at = page < a.num_pages ? (((int64_t)page * a.Hkv + hk) << a.page_shift) + row : 0;
-                const uint32_t se = ring + stage * Cfg::kStageB + Cfg::kScaleOff + lane * 32;
+                const uint32_t se = scales + stage * Cfg::kScaleB + lane * 32;
                 pg_bulk16(se, a.ke + at, bar);
                 pg_bulk16(se + 16, a.ve + at, bar);
             }
@@ -201,42 +211,27 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
     float qf[N][2];                                            // e4m3: what the scores of rows 8 n + c2, + 1 are to be multiplied with
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        const int r = min(n * 8 + l4, nrow - 1);
         const bool ok = n * 8 + l4 < nrow;
-        const uint16_t* q = a.q + paged_row(a, t, t.x0 + r / heads) * a.q_st + (head0 + r % heads) * a.q_sh;
         if constexpr (E4M3) {
-            // columns 4 t .. 4 t + 3.  As f16, the row scaled by a power of two to a largest value of 2^8 .. 2^9: exact down to 2^-22
-            // of that, and off by 2^-33 of it below
-            uint2 w[D / 16];
+            // As f16, the row scaled by a power of two to a largest value of 2^8 .. 2^9: exact down to 2^-22 of that, and off by 2^-33 of
+            // it below
             uint32_t top = 0;
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-                w[kk] = __ldcg(reinterpret_cast<const uint2*>(q + kk * 16 + c2 * 2));
-                top = __vmaxu2(top, __vmaxu2(w[kk].x & 0x7fff7fffu, w[kk].y & 0x7fff7fffu));
-            }
+            for (int kk = 0; kk < D / 16; ++kk) top = __vmaxu2(top, __vmaxu2(qw[n][kk].x & 0x7fff7fffu, qw[n][kk].y & 0x7fff7fffu));
             top = max(top >> 16, top & 0xffffu);
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
             const int e = min(max((int)(top >> 7) - 8, 1), 253);                  // the scale is 2^(127 - e), its inverse 2^(e - 127)
             const float f = __uint_as_float((uint32_t)(254 - e) << 23);
-            auto two = [&](uint32_t x) {
-                const uint32_t h = pack_f16x2(__uint_as_float(x << 16) * f, __uint_as_float(x & 0xffff0000u) * f);
-                return ok ? h : 0u;
-            };
+            auto two = [&](uint32_t x) { const uint32_t h = pack_f16x2(__uint_as_float(x << 16) * f, __uint_as_float(x & 0xffff0000u) * f); return ok ? h : 0u; };
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-                qb[kk][n][0] = two(w[kk].x);
-                qb[kk][n][1] = two(w[kk].y);
-            }
+            for (int kk = 0; kk < D / 16; ++kk) { qb[kk][n][0] = two(qw[n][kk].x); qb[kk][n][1] = two(qw[n][kk].y); }
             const float back = __uint_as_float((uint32_t)e << 23);             // (lane 4 i holds row i)
             qf[n][0] = __shfl_sync(0xffffffffu, back, c2 * 4);
             qf[n][1] = __shfl_sync(0xffffffffu, back, c2 * 4 + 4);
         } else {
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-                qb[kk][n][0] = ok ? __ldcg(reinterpret_cast<const uint32_t*>(q + kk * 16 + c2)) : 0u;
-                qb[kk][n][1] = ok ? __ldcg(reinterpret_cast<const uint32_t*>(q + kk * 16 + 8 + c2)) : 0u;
-            }
+            for (int kk = 0; kk < D / 16; ++kk) { qb[kk][n][0] = ok ? qw[n][kk].x : 0u; qb[kk][n][1] = ok ? qw[n][kk].y : 0u; }
         }
     }
     float o[D / 16][N][4];
@@ -262,7 +257,7 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
             }
             break;
         }
-        const uint32_t sk = ring + stage * Cfg::kStageB, sv = sk + Cfg::kVOff;
+        const uint32_t sk = ring + stage * Cfg::kStageB, sv = sk + Cfg::kVOff, sc = scales + stage * Cfg::kScaleB;
         if (++stage == kStages) { stage = 0; phase ^= 1u; }
         bool summ;
         const int x0 = tile_at(j, summ);
@@ -298,7 +293,7 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
                         for (int n = 0; n < N; ++n) pg_mma_f16(s[u][n], a0, a1, a2, a3, qb[kk * 2 + i][n]);
                     }
                 }
-                const uint32_t se = sk + Cfg::kScaleOff + u * 32 + l4;
+                const uint32_t se = sc + u * 32 + l4;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {                  // keys l4, l4 + 8
                     const float fk = a.scale_log2 * e8m0_factor(pg_ld_u8(se + 8 * h));
@@ -420,9 +415,7 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
     __syncthreads();
     constexpr int kRows = Cfg::kRows, kLd = Cfg::kLd;
     float* sm_o = reinterpret_cast<float*>(pgsm);                      // [warps][rows][kLd]
-    float* ct_o = sm_o + kWarps * kRows * kLd;                       // this CTA's: [rows][kLd]
-    float* sm_ml = ct_o + kRows * kLd;                                 // [warps][rows][2]
-    float* ct_ml = sm_ml + kWarps * kRows * 2;                       // [rows][2]
+    float* sm_ml = sm_o + kWarps * kRows * kLd;                        // [warps][rows][2]
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -436,7 +429,21 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
             if (l4 == 0) *reinterpret_cast<float2*>(sm_ml + (warp * kRows + n * 8 + c2 + e) * 2) = make_float2(m[n][e], l[n][e]);
         }
     __syncthreads();
-    for (int idx = threadIdx.x; idx < nrow * (D / 4); idx += kThreads) {
+    auto write = [&](int g, int d, const float4& acc, float M, float L) {
+        const float inv = 1.f / L;
+        const int64_t row = paged_row(a, t, t.x0 + g / heads);
+        const int h = head0 + g % heads;
+        if (!ksa_in_bounds(row >= 0 && row < a.rows && h < a.Hq, a.status)) return;
+        *reinterpret_cast<uint2*>(a.out + row * a.o_st + h * a.o_sh + d) =
+            make_uint2(ptx::pack_bf16x2(acc.x * inv, acc.y * inv), ptx::pack_bf16x2(acc.z * inv, acc.w * inv));
+        if (d == 0) a.lse[(int64_t)h * a.rows + row] = (M + log2f(L)) * 0.6931471805599453f;
+    };
+    // Each CTA of the cluster sums up a share of the output's elements (4 columns of a row each), `share` of them: the others
+    // write what they have of these into its memory, where the one barrier finds everything.
+    const int total = nrow * (D / 4), share = (total + parts - 1) / parts;
+    const uint32_t push_o = sbase + Cfg::kPushOff, push_ml = push_o + Cfg::kPushO;       // [parts][share] of 16 bytes, [parts][rows] of 8
+    if (parts > 1) ptx::cluster_wait();                        // they have all started
+    for (int idx = threadIdx.x; idx < total; idx += kThreads) {
         const int g = idx / (D / 4), d = (idx - g * (D / 4)) * 4;
         float2 ml[kWarps];
         float M = -INFINITY;
@@ -451,49 +458,39 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
             L += ml[w].y * f;
             acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
         }
-        *reinterpret_cast<float4*>(ct_o + g * kLd + d) = acc;
-        if (d == 0) *reinterpret_cast<float2*>(ct_ml + g * 2) = make_float2(M, L);
-    }
-    if (a.nsplit > 1) { ptx::cluster_arrive(); ptx::cluster_wait(); } else __syncthreads();
-    // the cluster's CTAs share the output's elements
-    const uint32_t so = ptx::smem_u32(ct_o), sml = ptx::smem_u32(ct_ml);
-    for (int idx = split * kThreads + threadIdx.x; idx < nrow * (D / 4); idx += kThreads * a.nsplit) {
-        const int g = idx / (D / 4), d = (idx - g * (D / 4)) * 4;
-        float M = -INFINITY, L = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int w0 = 0; w0 < kPgMaxSplit; w0 += 8) {
-            if (w0 >= a.nsplit) break;
-            float2 ml[8];
-            float4 v[8];
-#pragma unroll
-            for (int w = 0; w < 8; ++w)
-                if (w0 + w < a.nsplit) {
-                    ml[w] = pg_ld_cluster2(ptx::mapa_shared(sml + g * 8, w0 + w));
-                    v[w] = pg_ld_cluster4(ptx::mapa_shared(so + (g * kLd + d) * 4, w0 + w));
-                }
-            float mx = M;
-#pragma unroll
-            for (int w = 0; w < 8; ++w) if (w0 + w < a.nsplit) mx = fmaxf(mx, ml[w].x);
-            const float al = (mx == -INFINITY) ? 1.f : ptx::ex2_approx(M - mx);
-            M = mx; L *= al; acc.x *= al; acc.y *= al; acc.z *= al; acc.w *= al;
-#pragma unroll
-            for (int w = 0; w < 8; ++w)
-                if (w0 + w < a.nsplit) {
-                    const float f = (ml[w].x == -INFINITY) ? 0.f : ptx::ex2_approx(ml[w].x - M);
-                    L += ml[w].y * f;
-                    acc.x += v[w].x * f; acc.y += v[w].y * f; acc.z += v[w].z * f; acc.w += v[w].w * f;
-                }
+        if (parts == 1) {
+            write(g, d, acc, M, L);
+        } else {
+            const int to = idx / share;
+            asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};"
+                         ::"r"(ptx::mapa_shared(push_o + (split * share + idx - to * share) * 16, to)), "f"(acc.x), "f"(acc.y), "f"(acc.z), "f"(acc.w) : "memory");
+            if (d == 0)
+                for (int p = 0; p < parts; ++p)
+                    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(ptx::mapa_shared(push_ml + (split * kRows + g) * 8, p)), "f"(M), "f"(L) : "memory");
         }
-        const float inv = 1.f / L;
-        const int64_t row = paged_row(a, t, t.x0 + g / heads);
-        const int h = head0 + g % heads;
-        if (!ksa_in_bounds(row >= 0 && row < a.rows && h < a.Hq, a.status)) continue;
-        *reinterpret_cast<uint2*>(a.out + row * a.o_st + h * a.o_sh + d) =
-            make_uint2(ptx::pack_bf16x2(acc.x * inv, acc.y * inv), ptx::pack_bf16x2(acc.z * inv, acc.w * inv));
-        if (d == 0) a.lse[(int64_t)h * a.rows + row] = (M + log2f(L)) * 0.6931471805599453f;
     }
-    if (a.nsplit > 1) { ptx::cluster_arrive(); ptx::cluster_wait(); }      // no CTA leaves while another reads its results
+    if (parts > 1) {
+        __syncwarp();
+        ptx::cluster_arrive();
+        ptx::cluster_wait();
+        const float4* po = reinterpret_cast<const float4*>(pgsm + Cfg::kPushOff);
+        const float2* pm = reinterpret_cast<const float2*>(pgsm + Cfg::kPushOff + Cfg::kPushO);
+        for (int e = threadIdx.x; e < share && split * share + e < total; e += kThreads) {
+            const int idx = split * share + e, g = idx / (D / 4), d = (idx - g * (D / 4)) * 4;
+            float M = -INFINITY, L = 0.f;
+            for (int p = 0; p < parts; ++p) M = fmaxf(M, pm[p * kRows + g].x);
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+            for (int p = 0; p < parts; ++p) {
+                const float2 ml = pm[p * kRows + g];
+                const float4 v = po[p * share + e];
+                const float f = (ml.x == -INFINITY) ? 0.f : ptx::ex2_approx(ml.x - M);
+                L += ml.y * f;
+                acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
+            }
+            write(g, d, acc, M, L);
+        }
+    }
 }
 
 // f(kernel, shared memory) for each or one of the kernels

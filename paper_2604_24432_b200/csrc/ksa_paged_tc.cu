@@ -148,7 +148,8 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
 
     const int unit = (int)blockIdx.x >> a.split_shift, split = (int)blockIdx.x - (unit << a.split_shift);
     const int item = a.by_heads(unit), hk = unit - item * a.Hkv;
-    const PagedTile t = paged_tile<true>(a, item);       // up to 2 * per tokens
+    __shared__ __align__(16) PagedFound found;
+    const PagedTile t = paged_tile<true>(a, item, found);   // up to 2 * per tokens
     const int per = a.tokens_per_tile / 2;
     if (t.b >= 0) {                                         // (the same for the whole cluster)
     PagedWalk<kPtTile> w;
