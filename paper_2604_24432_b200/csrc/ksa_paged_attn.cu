@@ -48,7 +48,7 @@ struct PgCfg {
     static constexpr int kVOff = kSubs * kRunB;
     static constexpr int kStageB = 2 * kVOff;                   // K, V (multiples of 1,024 bytes, which the swizzles repeat after)
     static constexpr int kScaleB = E4M3 ? 2 * kKeys : 0;        // a stage's scale bytes: run by run 16 of K, 16 of V
-    static constexpr int kTxBytes = 2 * kVOff + (E4M3 ? 2 * kKeys : 0);
+    static constexpr int kTxBytes = 2 * kVOff;
     static constexpr int kStages = 3;
     static constexpr int kRingB = kStages * kStageB;            // of a warp
     // log2 units.  The reference maximum moves when a score outgrows it by this
@@ -68,11 +68,6 @@ struct PgCfg {
     }
 };
 
-// untiled copy of 16 bytes global -> shared, counted on an mbarrier
-__device__ __forceinline__ void pg_bulk16(uint32_t dst, const void* src, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 16, [%2];" ::"r"(dst), "l"(src), "r"(bar) : "memory");
-}
 __device__ __forceinline__ void pg_ldsm(uint32_t (&r)[4], uint32_t addr)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -173,26 +168,33 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
     const uint32_t ring = sbase + warp * Cfg::kRingB, full = bars + 8 * warp * kStages, scales = sbase + Cfg::kScaleOff + warp * kStages * Cfg::kScaleB;
     auto load_tile = [&](int j, int stage, int entry) {
         if (lane == 0) ptx::mbar_arrive_expect_tx(full + 8 * stage, Cfg::kTxBytes);
+        bool summ;
+        const int row0 = tile_at(j, summ) & ((1 << a.page_shift) - 1);
+        int page = paged_entry(a, entry);
+        if (page < 0) {
+            if (lane < kSubs && entry != -3) atomicCAS(a.status, 0, KSA_PAGED_STATUS_BAD_PAGE);
+            page = a.num_pages;                                // outside the pool: a box of zeros
+        }
+        int box_page = page;
+        if constexpr (kSubs == 2) {                            // one box for both runs: the page of the one that is seen
+            const int other = __shfl_sync(0xffffffffu, page, 1);
+            if (a.box_rows == 2 * kPgRun && page == a.num_pages) box_page = other;
+        }
         __syncwarp();
-        if (lane < kSubs) {
-            bool summ;
-            const int row = tile_at(j, summ) + kPgRun * lane & ((1 << a.page_shift) - 1);
-            int page = paged_entry(a, entry);
-            if (page < 0) {
-                if (entry != -3) atomicCAS(a.status, 0, KSA_PAGED_STATUS_BAD_PAGE);
-                page = a.num_pages;                            // outside the pool: a box of zeros
-            }
+        if (lane < kSubs && (lane == 0 || a.box_rows == kPgRun)) {
             const uint32_t sk = ring + stage * Cfg::kStageB + lane * Cfg::kRunB, bar = full + 8 * stage;
+            const int row = row0 + lane * kPgRun & ((1 << a.page_shift) - 1);
 #pragma unroll
             for (int p = 0; p < Cfg::kPanels; ++p) {
-                ptx::tma_load_4d(sk + p * (kPgRun * 128), &maps.k, bar, p * (Cfg::kPanelB / (E4M3 ? 1 : 2)), row, hk, page);
-                ptx::tma_load_4d(sk + Cfg::kVOff + p * (kPgRun * 128), &maps.v, bar, p * (Cfg::kPanelB / (E4M3 ? 1 : 2)), row, hk, page);
+                ptx::tma_load_4d(sk + p * (kPgRun * 128), &maps.k, bar, p * (Cfg::kPanelB / (E4M3 ? 1 : 2)), row, hk, box_page);
+                ptx::tma_load_4d(sk + Cfg::kVOff + p * (kPgRun * 128), &maps.v, bar, p * (Cfg::kPanelB / (E4M3 ? 1 : 2)), row, hk, box_page);
             }
-            if constexpr (E4M3) {
-                const int64_t at = page < a.num_pages ? (((int64_t)page * a.Hkv + hk) << a.page_shift) + row : 0;
-                const uint32_t se = scales + stage * Cfg::kScaleB + lane * 32;
-                pg_bulk16(se, a.ke + at, bar);
-                pg_bulk16(se + 16, a.ve + at, bar);
+        }
+        if constexpr (E4M3) {                                  // lanes 0, 1: the runs' scale bytes of K, lanes 2, 3: of V
+            const int u = lane & 1, from = __shfl_sync(0xffffffffu, page, u);
+            if (lane < 4 && from < a.num_pages) {
+                const int64_t at = (((int64_t)from * a.Hkv + hk) << a.page_shift) + (row0 + u * kPgRun & ((1 << a.page_shift) - 1));
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(scales + stage * Cfg::kScaleB + u * 32 + (lane >> 1) * 16), "l"((lane < 2 ? a.ke : a.ve) + at) : "memory");
             }
         }
     };
@@ -203,8 +205,10 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
         for (int s = 0; s < kStages - 1; ++s) early[s] = find_entry(my0 + s);
         entry = find_entry(my0 + kStages - 1);
 #pragma unroll
-        for (int s = 0; s < kStages - 1; ++s)
+        for (int s = 0; s < kStages - 1; ++s) {
             if (my0 + s < my1) load_tile(my0 + s, s, early[s]);
+            if constexpr (E4M3) asm volatile("cp.async.commit_group;" ::: "memory");
+        }
     }
     // Q^T fragments (B operand, D x 8 N); rows past the tile's are zero
     uint32_t qb[D / 16][N][2];
@@ -248,7 +252,9 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
     for (int j = my0; j < my1; ++j) {
         __syncwarp();                                          // the tile before has been read by every lane
         if (j + kStages - 1 < my1) load_tile(j + kStages - 1, stage == 0 ? kStages - 1 : stage - 1, entry);
+        if constexpr (E4M3) asm volatile("cp.async.commit_group;" ::: "memory");
         entry = find_entry(j + kStages);
+        if constexpr (E4M3) asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
         const bool ok = bounded_wait(full + 8 * stage, phase, abort_addr, a.status, kStatusWaitKvFull);
         if (!__all_sync(0xffffffffu, ok)) {                    // given up: no copy is left in flight behind
             for (int i = j, st = stage; i < min(j + kStages, my1); ++i) {
@@ -257,6 +263,7 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
             }
             break;
         }
+        __syncwarp();
         const uint32_t sk = ring + stage * Cfg::kStageB, sv = sk + Cfg::kVOff, sc = scales + stage * Cfg::kScaleB;
         if (++stage == kStages) { stage = 0; phase ^= 1u; }
         bool summ;
@@ -411,6 +418,7 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
         for (int e = 0; e < 2; ++e)
 #pragma unroll
             for (int b = 4; b < 32; b <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], b);
+    if constexpr (E4M3) asm volatile("cp.async.wait_all;" ::: "memory");
     // the warps' results: rows of (maximum, sum) and of O each
     __syncthreads();
     constexpr int kRows = Cfg::kRows, kLd = Cfg::kLd;
@@ -546,10 +554,12 @@ cudaError_t launch_paged_attn(const PagedArgs& args, bool e4m3, int query_rows, 
     a.nsplit = paged_splits(units, rows / 64, num_sms);
     while (1 << a.split_shift < a.nsplit) ++a.split_shift;
     a.by_heads = PagedDiv::by(a.Hkv * a.head_blocks); a.by_group = PagedDiv::by(a.head_blocks);
+    // (a box of the warp's whole tile where a page holds it: every box costs the warp that asks for it some 50 cycles)
+    a.box_rows = e4m3 && a.page_shift > 4 ? 2 * kPgRun : kPgRun;
     const int panel = a.D * (e4m3 ? 1 : 2) < 128 ? 64 : 128;
     const CUtensorMapSwizzle swizzle = panel == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B;
     PgMaps maps;
-    if (!encode_pages(encode, &maps.k, a.kp, a, e4m3, panel, kPgRun, swizzle) || !encode_pages(encode, &maps.v, a.vp, a, e4m3, panel, kPgRun, swizzle))
+    if (!encode_pages(encode, &maps.k, a.kp, a, e4m3, panel, a.box_rows, swizzle) || !encode_pages(encode, &maps.v, a.vp, a, e4m3, panel, a.box_rows, swizzle))
         return cudaErrorInvalidValue;
     cudaLaunchAttribute attr[2]{};
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
