@@ -27,7 +27,7 @@
  * tensors; rows from cu_rows[batch] on are not read, and left as they were.  A sequence may have no rows.
  *
  * Tensors (DEVICE; bf16 unless said otherwise; 16-byte aligned; strides in elements, multiples of 8 for bf16 and of 16 for
- * e4m3; head_dim contiguous):
+ * e4m3, of pages and of what is written not 0; head_dim contiguous):
  *   q, out : [num_rows, num_q_heads, head_dim]     k, v : [num_rows, num_kv_heads, head_dim]
  *   lse    : fp32 [num_q_heads, num_rows], natural log of the softmax denominator
  *   text_table : int32 [batch, text_cols]   summ_table : int32 [batch, summ_cols]   cached : int32 [batch]
@@ -92,7 +92,7 @@ int ksa_paged_gather(ksa_ctx* ctx, const ksa_paged_kv* kv, void* k, void* v, con
  * KSA_FLAG_SUMMARY_TEXT_ONLY).  Query head h reads KV head h / (num_q_heads / num_kv_heads).  Pages that no row of a sequence
  * sees are not looked up.  What stands in rows that no row of the call sees -- behind the sequence, before its windows --
  * does not matter; rows that one of the call's rows sees must be finite (or NaN reaches rows of the same sequence that do
- * not see them).
+ * not see them, and LSEs too).  e4m3 pages hold no NaN codes (0x7f, 0xff): a row of NaN is said by its scale byte.
  */
 int ksa_paged_attn(ksa_ctx* ctx, const ksa_paged_kv* kv, const void* q, void* out, float* lse, void* workspace, size_t workspace_bytes,
                    const ksa_paged_params* p, void* cuda_stream);

@@ -703,8 +703,11 @@ class PagedCache:
         if lse.shape != (H, rows) or lse.dtype is not self._f32 or lse.get_device() != self._index or not lse.is_contiguous():
             raise ValueError("lse must be contiguous fp32 [heads, num_rows] = %s on cuda:%d" % ((H, rows), self._index))
         p = self._params(batch, rows, self._rows(q, rows, H), _NO_ROWS, _NO_ROWS, self._rows(out, rows, H))
-        if workspace is None and self._quantised and rows > batch._size:
-            workspace = self._workspace(p, stream)
+        if workspace is None:
+            if self._quantised and rows > batch._size:
+                workspace = self._workspace(p, stream)
+        elif workspace.get_device() != self._index or not workspace.is_contiguous():
+            raise ValueError("the workspace must be contiguous, on cuda:%d" % self._index)
         ws, nbytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
         status = self._attn(self.ctx.handle, self._pools + batch._ptrs, q.data_ptr(), out.data_ptr(), lse.data_ptr(), ws, nbytes, p,
                             _current_stream(self.device) if stream is None else stream)

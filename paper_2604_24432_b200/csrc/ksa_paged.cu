@@ -328,12 +328,11 @@ static int validate_shape(const ksa_paged_params* p)
     if (p->num_q_heads / p->num_kv_heads > 64 || p->num_q_heads > 1024 || p->batch > 65535 || p->num_rows > (1 << 24)) return KSA_ERR_UNSUPPORTED;
     if ((int64_t)p->chunk_len + p->summaries_per_chunk > (1 << 30)) return KSA_ERR_UNSUPPORTED;
     const int64_t unit = p->kv_format == KSA_KV_BF16 ? 8 : 16;              // 16 bytes
-    for (int64_t st : {p->page_stride, p->head_stride, p->row_stride}) {
-        if (st < 0 || st % unit != 0) return KSA_ERR_INVALID_ARG;
-        if (st >= (1ll << 38)) return KSA_ERR_UNSUPPORTED;
-    }
-    if (p->row_stride < p->head_dim) return KSA_ERR_INVALID_ARG;
-    return KSA_OK;
+    auto stride_of = [&](int64_t st) { return st <= 0 || st % unit != 0 ? KSA_ERR_INVALID_ARG : st >= (1ll << 38) ? KSA_ERR_UNSUPPORTED : KSA_OK; };
+    int rc = p->row_stride < p->head_dim ? KSA_ERR_INVALID_ARG : stride_of(p->row_stride);
+    if (rc == KSA_OK && p->num_kv_heads > 1) rc = stride_of(p->head_stride);             // (of one head, of one page: any)
+    if (rc == KSA_OK && p->num_pages > 1) rc = stride_of(p->page_stride);
+    return rc;
 }
 
 static int validate_paged(const ksa_paged_params* p, const ksa_paged_kv* kv)
@@ -360,7 +359,8 @@ static PagedArgs paged_args(ksa_ctx* ctx, const ksa_paged_kv* kv, const ksa_page
     a.kp = (uint8_t*)kv->kpages; a.vp = (uint8_t*)kv->vpages; a.ke = kv->kscale; a.ve = kv->vscale;
     a.text_table = kv->text_table; a.summ_table = kv->summ_table; a.cached = kv->cached; a.cu = kv->cu_rows;
     const int64_t width = p->kv_format == KSA_KV_BF16 ? 2 : 1;
-    a.page_st = p->page_stride * width; a.head_st = p->head_stride * width; a.row_st = p->row_stride * width;
+    a.page_st = p->num_pages > 1 ? p->page_stride * width : 0; a.head_st = p->num_kv_heads > 1 ? p->head_stride * width : 0;
+    a.row_st = p->row_stride * width;
     a.q_st = p->q_stride_tok; a.q_sh = p->q_stride_head; a.k_st = p->k_stride_tok; a.k_sh = p->k_stride_head;
     a.v_st = p->v_stride_tok; a.v_sh = p->v_stride_head; a.o_st = p->o_stride_tok; a.o_sh = p->o_stride_head;
     a.B = p->batch; a.rows = p->num_rows; a.kk = p->chunk_len; a.m = p->summaries_per_chunk; a.C = p->window_chunks;
@@ -389,9 +389,8 @@ struct OnDevice {
 }  // namespace
 
 template <class F>
-static int paged_call(ksa_ctx* ctx, const ksa_paged_params* p, F launch)
+static int paged_call(ksa_ctx* ctx, F launch)
 {
-    if (p->num_rows == 0) return KSA_OK;
     OnDevice on(ksa_ctx_device(ctx));
     cudaError_t e = on.err;
     if (e == cudaSuccess) e = launch();
@@ -404,20 +403,24 @@ KSA_API int ksa_paged_append(ksa_ctx* ctx, const ksa_paged_kv* kv, const void* k
 {
     const int rc = validate_paged(p, kv);
     if (rc != KSA_OK) return rc;
-    if (!ctx || !tensor_ok(k, p->k_stride_tok, p->k_stride_head) || !tensor_ok(v, p->v_stride_tok, p->v_stride_head)) return KSA_ERR_INVALID_ARG;
+    if (!ctx) return KSA_ERR_INVALID_ARG;
+    if (p->num_rows == 0) return KSA_OK;
+    if (!tensor_ok(k, p->k_stride_tok, p->k_stride_head) || !tensor_ok(v, p->v_stride_tok, p->v_stride_head)) return KSA_ERR_INVALID_ARG;
     PagedArgs a = paged_args(ctx, kv, p);
     a.k = (uint16_t*)k; a.v = (uint16_t*)v;
-    return paged_call(ctx, p, [&] { return launch_paged_append(a, p->kv_format == KSA_KV_E4M3, ksa_ctx_num_sms(ctx), (cudaStream_t)cuda_stream); });
+    return paged_call(ctx, [&] { return launch_paged_append(a, p->kv_format == KSA_KV_E4M3, ksa_ctx_num_sms(ctx), (cudaStream_t)cuda_stream); });
 }
 
 KSA_API int ksa_paged_gather(ksa_ctx* ctx, const ksa_paged_kv* kv, void* k, void* v, const ksa_paged_params* p, void* cuda_stream)
 {
     const int rc = validate_paged(p, kv);
     if (rc != KSA_OK) return rc;
-    if (!ctx || !tensor_ok(k, p->k_stride_tok, p->k_stride_head) || !tensor_ok(v, p->v_stride_tok, p->v_stride_head)) return KSA_ERR_INVALID_ARG;
+    if (!ctx) return KSA_ERR_INVALID_ARG;
+    if (p->num_rows == 0) return KSA_OK;
+    if (!tensor_ok(k, p->k_stride_tok, p->k_stride_head) || !tensor_ok(v, p->v_stride_tok, p->v_stride_head)) return KSA_ERR_INVALID_ARG;
     PagedArgs a = paged_args(ctx, kv, p);
     a.k = (uint16_t*)k; a.v = (uint16_t*)v;
-    return paged_call(ctx, p, [&] { return launch_paged_gather(a, p->kv_format == KSA_KV_E4M3, ksa_ctx_num_sms(ctx), (cudaStream_t)cuda_stream); });
+    return paged_call(ctx, [&] { return launch_paged_gather(a, p->kv_format == KSA_KV_E4M3, ksa_ctx_num_sms(ctx), (cudaStream_t)cuda_stream); });
 }
 
 KSA_API int ksa_paged_workspace_bytes(const ksa_paged_params* p, size_t* bytes)
@@ -434,12 +437,14 @@ KSA_API int ksa_paged_attn(ksa_ctx* ctx, const ksa_paged_kv* kv, const void* q, 
 {
     const int rc = validate_paged(p, kv);
     if (rc != KSA_OK) return rc;
-    if (!ctx || !tensor_ok(q, p->q_stride_tok, p->q_stride_head) || !tensor_ok(out, p->o_stride_tok, p->o_stride_head) || !lse || ((uintptr_t)lse & 3)) return KSA_ERR_INVALID_ARG;
+    if (!ctx) return KSA_ERR_INVALID_ARG;
+    if (p->num_rows == 0) return KSA_OK;
+    if (!tensor_ok(q, p->q_stride_tok, p->q_stride_head) || !tensor_ok(out, p->o_stride_tok, p->o_stride_head) || !lse || ((uintptr_t)lse & 3)) return KSA_ERR_INVALID_ARG;
     if (workspace && ((uintptr_t)workspace & 255)) return KSA_ERR_INVALID_ARG;
     PagedArgs a = paged_args(ctx, kv, p);
     a.q = (const uint16_t*)q; a.out = (uint16_t*)out; a.lse = lse;
     bool e4m3 = p->kv_format == KSA_KV_E4M3;
-    return paged_call(ctx, p, [&]() -> cudaError_t {
+    return paged_call(ctx, [&]() -> cudaError_t {
         bool& ready = *ksa_ctx_paged_ready(ctx);                // shared-memory opt-in: a per-device setting
         const PagedEncode encode = (PagedEncode)ksa_ctx_encode_tiled(ctx);
         const cudaStream_t stream = (cudaStream_t)cuda_stream;

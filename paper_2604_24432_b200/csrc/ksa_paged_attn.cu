@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
             __syncwarp();
         }
         // S^T (16 keys x 8 N query rows, run by run) = K Q^T, in log2 units
-        float s[kSubs][N][4], back[kSubs][2];                  // e4m3: with the value rows' exponents, and 2^(127 - e) of these
+        float s[kSubs][N][4], back[kSubs][2], tiny[kSubs][2];  // e4m3: with the value rows' exponents, 2^(127 - 20 - e) of these, see below
 #pragma unroll
         for (int u = 0; u < kSubs; ++u) {
 #pragma unroll
@@ -305,8 +305,12 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
                 for (int h = 0; h < 2; ++h) {                  // keys l4, l4 + 8
                     const float fk = a.scale_log2 * e8m0_factor(pg_ld_u8(se + 8 * h));
                     const uint32_t e = pg_ld_u8(se + 16 + 8 * h);
-                    const float ef = e == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(0x4b000000u | e) - (8388608.f + 127.f);
-                    back[u][h] = __uint_as_float((uint32_t)max((int)(254u - e) << 23, 0x00400000));
+                    // Exponents below -64 count as -64 (a row of zeros has -110, and its share of the sum must not underflow), and
+                    // what is left of such a row's values goes into its probability.
+                    const uint32_t ec = max(e, 63u);
+                    tiny[u][h] = e < 63u ? __uint_as_float((e + 64u) << 23) : 1.f;
+                    const float ef = e == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(0x4b000000u | ec) - (8388608.f + 127.f);
+                    back[u][h] = __uint_as_float((uint32_t)max((int)(234u - ec) << 23, 0x00400000));      // (2^-20: sums stay far below 2^128)
 #pragma unroll
                     for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -378,7 +382,7 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
                     if constexpr (E4M3) {
                         l[n][0] = fmaf(p0, back[u][h], l[n][0]);
                         l[n][1] = fmaf(p1, back[u][h], l[n][1]);
-                        pb[n][h] = pg_transpose(pack_f16x2(p0, p1));
+                        pb[n][h] = pg_transpose(pack_f16x2(p0 * tiny[u][h], p1 * tiny[u][h]));
                     } else {
                         l[n][0] += p0;
                         l[n][1] += p1;
@@ -437,14 +441,15 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
             if (l4 == 0) *reinterpret_cast<float2*>(sm_ml + (warp * kRows + n * 8 + c2 + e) * 2) = make_float2(m[n][e], l[n][e]);
         }
     __syncthreads();
+    constexpr float kUnit = E4M3 ? 20.f : 0.f, kInv = E4M3 ? 1.f / (1 << 20) : 1.f;      // of the sums, see `back`
     auto write = [&](int g, int d, const float4& acc, float M, float L) {
-        const float inv = 1.f / L;
+        const float inv = kInv / L;
         const int64_t row = paged_row(a, t, t.x0 + g / heads);
         const int h = head0 + g % heads;
         if (!ksa_in_bounds(row >= 0 && row < a.rows && h < a.Hq, a.status)) return;
         *reinterpret_cast<uint2*>(a.out + row * a.o_st + h * a.o_sh + d) =
             make_uint2(ptx::pack_bf16x2(acc.x * inv, acc.y * inv), ptx::pack_bf16x2(acc.z * inv, acc.w * inv));
-        if (d == 0) a.lse[(int64_t)h * a.rows + row] = (M + log2f(L)) * 0.6931471805599453f;
+        if (d == 0) a.lse[(int64_t)h * a.rows + row] = (M + kUnit + log2f(L)) * 0.6931471805599453f;
     };
     // Each CTA of the cluster sums up a share of the output's elements (4 columns of a row each), `share` of them: the others
     // write what they have of these into its memory, where the one barrier finds everything.

@@ -41,9 +41,10 @@ class Server:
         self.q, self.key, self.val = [norm(n, Hq) for n in lens], [norm(n, Hkv) for n in lens], [norm(n, Hkv) for n in lens]
         cols_t = max(1, max(-(-_texts(k, m, n) // ps) for n in lens))
         cols_s = max(1, max(-(-(n - _texts(k, m, n)) // ps) for n in lens))
-        pages = rng.permutation(len(lens) * (cols_t + cols_s) + spare)
+        of_summ = len(lens) * cols_s if m else 0
+        pages = rng.permutation(len(lens) * cols_t + of_summ + spare)
         self.text = pages[:len(lens) * cols_t].reshape(len(lens), cols_t).copy()
-        self.summ = pages[len(lens) * cols_t:len(lens) * (cols_t + cols_s)].reshape(len(lens), cols_s).copy()
+        self.summ = pages[len(lens) * cols_t:len(lens) * cols_t + of_summ].reshape(len(lens), -1).copy() if m else np.full((len(lens), 1), -1)
         self.scale = float(np.float32(D ** -0.5))
         spec = ksa.PagedSpec(k, m, C, Hq, Hkv, D, self.scale, ps, len(pages), fmt, flags)
         self.cache = ksa.PagedCache(ctx, spec, *(pools(len(pages)) if pools else ()))
@@ -288,6 +289,39 @@ def test_long_runs_over_e4m3(ctx, k, m, C, Hq, Hkv, D, ps, flags, spans, pad):
         s.check(out, lse, spans, sample=24)
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("n", [1, 150, 700])
+@pytest.mark.parametrize("what", ["all V", "some V", "all K", "tiny V", "huge V"])
+def test_rows_of_zeros_and_of_extreme_size(ctx, fmt, n, what):
+    """Rows of zeros have the least scale: their keys count in the sums all the same.  V of 1e-15 or 1e30 scales the output."""
+    s = Server(ctx, 8, 1, 100, 8, 2, 128, 32, fmt, [1100], seed=9)
+    rows = (s.val if "V" in what else s.key)[0]
+    if what.startswith("all"):
+        rows.zero_()
+    elif what == "some V":
+        rows[::3] = 0
+        s.q[0] *= 3.0                                          # scores far apart: zero rows dominate some sums, not others
+    else:
+        rows.copy_((rows.float() * (1e-15 if what == "tiny V" else 1e30)).bfloat16())
+    spans = [(1100 - n, n)]
+    s.fill(spans)
+    out, lse = s.attn(spans)
+    s.check(out, lse, spans, sample=12)
+
+
+def test_one_page_and_one_head_of_any_stride(ctx):
+    """Strides of a dimension of one are not looked at."""
+    D = 64
+    base = torch.empty(5 * 128 * D + 3 * D, dtype=torch.bfloat16, device=DEV)
+    pools = lambda n: tuple(torch.as_strided(base, (1, 1, 128, D), (3, 5, D, 1), off) for off in (0, 128 * D + 2 * D))
+    for n in (1, 90):
+        s = Server(ctx, 8, 0, 100, 4, 1, D, 128, "bf16", [100], seed=2, spare=0, pools=pools)
+        spans = [(100 - n, n)]
+        s.fill(spans)
+        out, lse = s.attn(spans)
+        s.check(out, lse, spans, sample=20)
+
+
 def test_strided_pools_and_rows(ctx):
     """Pages as [page, row, head, d] and padded heads; q a slice of a fused projection; out a slice of a wider tensor."""
     k, m, C, Hq, Hkv, D, ps = 8, 1, 3, 8, 2, 128, 32
@@ -473,6 +507,44 @@ def test_captured_calls_follow_lengths_and_tables(ctx, fmt, n):
     assert ctx.device_status() == 0
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_many_calls_in_a_row_in_a_graph(ctx, fmt):
+    """Eight steps of append and attn, one after another without a pause, kernels beside one another: as each step alone, twice."""
+    lens = [500, 60, 340, 90, 340, 700]
+    s = Server(ctx, 8, 1, 5, 16, 2, 128, 16, fmt, lens, seed=41)
+    start = [n // 2 for n in lens]
+    steps = [[(start[b] + (i if b % 2 else 20 * i), 1 if b % 2 else 20) for b in range(len(lens))] for i in range(8)]
+    s.append([(0, n) for n in start])
+    pools = [t.clone() for t in (s.cache.kpages, s.cache.vpages)] + [t.clone() for t in (s.cache.kscale, s.cache.vscale) if t is not None]
+    calls, want = [], []
+    for spans in steps:
+        b, q, k, v = s.batch(spans), s.rows(s.q, spans), s.rows(s.key, spans), s.rows(s.val, spans)
+        out, lse = torch.empty_like(q), torch.empty((16, q.shape[0]), device=DEV)
+        s.cache.append(b, k, v)
+        torch.cuda.synchronize()
+        s.cache.attn(b, q, out, lse)
+        torch.cuda.synchronize()
+        s.check(out, lse, spans, sample=3)
+        want.append((out.clone(), lse.clone()))
+        calls.append((b, q, k, v, out, lse))
+    side = torch.cuda.Stream()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        for b, q, k, v, out, lse in calls:
+            s.cache.append(b, k, v)
+            s.cache.attn(b, q, out, lse)
+    for _ in range(3):
+        for t, p in zip([s.cache.kpages, s.cache.vpages, s.cache.kscale, s.cache.vscale], pools):
+            t.copy_(p)
+        for c in calls:
+            c[4].fill_(7.0); c[5].fill_(7.0)
+        g.replay()
+        torch.cuda.synchronize()
+        for c, (out, lse) in zip(calls, want):
+            assert torch.equal(c[4], out) and torch.equal(c[5], lse)
+    assert ctx.device_status() == 0
+
+
 def test_two_streams_and_repeated_calls_agree(ctx):
     """The same calls on two streams at once, and again: bit for bit the same (sums are in a fixed order)."""
     for n in (1, 5, 200):
@@ -502,8 +574,12 @@ def test_nothing_to_do(ctx):
     s.cache.append(s.batch([(10, 0)]), torch.zeros((3, 2, 64), dtype=torch.bfloat16, device=DEV), torch.zeros((3, 2, 64), dtype=torch.bfloat16, device=DEV))
     assert torch.isnan(s.cache.kpages).all() and ctx.launch_count() == before + 1
     s.attn([(10, 0)], pad=4)
-    with pytest.raises(ksa.KsaError):                          # no rows: no address to pass
-        s.cache.append(s.batch([(10, 0)]), empty, empty)
+    before = ctx.launch_count()
+    s.cache.append(s.batch([(10, 0)]), empty, empty)
+    s.cache.gather(s.batch([(10, 0)]), empty, empty)
+    none = torch.empty((0, 4, 64), dtype=torch.bfloat16, device=DEV)
+    s.cache.attn(s.batch([(10, 0)]), none, none, torch.empty((4, 0), device=DEV))
+    assert ctx.launch_count() == before
 
 
 def test_refusals_of_tensors(ctx):
