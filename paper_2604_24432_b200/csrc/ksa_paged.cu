@@ -267,9 +267,9 @@ static UnpackLayout unpack_layout(const ksa_paged_params* p)
 {
     UnpackLayout l{};
     const int64_t G = p->num_q_heads / p->num_kv_heads;
-    // From 2,048 query rows (eight tiles of 256) a sequence on: converting a key tile once costs as much as converting it in three to
-    // four query tiles, and a launch
-    if (p->kv_format != KSA_KV_E4M3 || p->num_rows * G < 2048 * (int64_t)p->batch) return l;
+    // From 1,024 query rows (four tiles of 256) a sequence on: the tcgen05 kernel converts a key tile once for each of them.  256 rows over
+    // 36,864, 32/8 heads: 65 us without the copy, 59 with it; 128 rows: 43 and 46; 1,152: 122 and 89.
+    if (p->kv_format != KSA_KV_E4M3 || p->num_rows * G < 1024 * (int64_t)p->batch) return l;
     const int64_t text = (int64_t)p->text_cols * p->page_rows, summ = p->summaries_per_chunk > 0 ? (int64_t)p->summ_cols * p->page_rows : 0;
     l.text_cols = (text + 127) / 128; l.summ_cols = (summ + 127) / 128;
     const int64_t seen = ((int64_t)p->window_chunks + 2) * p->chunk_len + p->num_rows;        // text tokens in view, at most
@@ -455,15 +455,17 @@ KSA_API int ksa_paged_attn(ksa_ctx* ctx, const ksa_paged_kv* kv, const void* q, 
             if (e != cudaSuccess) return e;
             ready = true;
         }
-        // Up to 16 query rows a sequence, on average: the mma.sync kernel for all.  More than 64, and several sequences: that one for
-        // those that fit into its tiles (single tokens beside prompts), and the tcgen05 kernel, which takes as long over one query
-        // row as over 256, beside it for the others: 24 tokens over 90,000 to 113,000 rows and 1,152 rows over 36,864, 32/8 heads:
+        // Up to 16 query rows a sequence, on average (64 over e4m3 pages): the mma.sync kernel for all.  16 sequences of 3, 4, 5, 6, 8 rows
+        // over 800 to 37,000, 32/8 heads (12 to 32 query rows), that one and the tcgen05 kernel: bf16 50, 50, 55, 86, 86 and 48, 51, 51,
+        // 52, 55 us, e4m3 40, 41, 48, 57, 60 and 78, 81, 82, 84, 90 us.  More, and several sequences: that one for those that fit into
+        // its tiles (single tokens beside prompts), and the tcgen05 kernel, which takes as long over one query row as over 256,
+        // beside it for the others: 24 tokens over 90,000 to 113,000 rows and 1,152 rows over 36,864, 32/8 heads:
         // e4m3 484 -> 261 us, bf16 251 -> 259; the 24 over 1,000 to 3,500 rows: 152 -> 156, 126 -> 100.  A launch that finds no
         // such sequence costs 4 us.
         const int sms = ksa_ctx_num_sms(ctx);
         const int64_t rows = (int64_t)a.rows * a.G;
         a.rows_min = 1; a.rows_max = a.rows;
-        if (rows <= 16 * (int64_t)a.B) return launch_paged_attn(a, e4m3, rows <= 8 * (int64_t)a.B ? 8 : 16, sms, encode, stream);
+        if (rows <= (e4m3 ? 64 : 16) * (int64_t)a.B) return launch_paged_attn(a, e4m3, rows <= 8 * (int64_t)a.B ? 8 : 16, sms, encode, stream);
         const int small = a.B < 4 || rows <= 64 * (int64_t)a.B || a.G > 16 ? 0 : (a.G > 8 ? 16 : 8) / a.G;      // rows of a sequence for the former
         const UnpackLayout l = unpack_layout(p);
         const bool copy = l.bytes > 0 && workspace && workspace_bytes >= (size_t)l.bytes;

@@ -526,13 +526,14 @@ cudaError_t setup_paged_attn()
     return cudaSuccess;
 }
 
-// CTAs of one cluster for a call of `units` query tiles at most: up to four CTAs a SM (two are resident), as far as there are
-// key tiles to split.  128 units of 17,300 rows each, e4m3 (1, 2, 4, 8 CTAs a unit): 186, 100, 108, 125 us; 116 units of 700 to
-// 17,400 rows: 199, 112, 63, 73 us; 8 units of 2,000 rows, bf16: 29, 17.7, 11.6, 8.9 us.
+// CTAs of one cluster for a call of `units` query tiles at most, as far as there are key tiles to split: two up to ten CTAs an SM in
+// the grid, more up to five (two are resident).  128 units of 17,300 rows each, e4m3 (1, 2, 4, 8 CTAs a unit): 186, 94, 102,
+// 117 us; 116 units of 700 to 17,400 rows: 199, 103, 59, 65 us; 8 units of 2,000 rows, bf16: 29, 17, 10.7, 7.8 us; up to 384 units,
+// 16 sequences of 6 drafted rows, e4m3 (1, 2): 70, 57 us.
 static int paged_splits(int64_t units, int64_t key_tiles, int num_sms)
 {
     int n = 1;
-    while (n < kPgMaxSplit && units * n * 2 <= 4 * num_sms && key_tiles >= 2 * n) n *= 2;
+    while (n < kPgMaxSplit && units * n * 2 <= (n == 1 ? 10 : 5) * num_sms && key_tiles >= 2 * n) n *= 2;
     return n;
 }
 

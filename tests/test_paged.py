@@ -158,7 +158,7 @@ def test_workspace_of_long_runs_over_e4m3():
         return n.value if rc == 0 else rc
     pages = (130 * 8 + 1152) // 128 + 2 + 35
     assert need() == 2 * pages * 8 * 128 * 128 * 2 + (300 + 35) * 4
-    assert need(num_rows=511) == need(batch=3) == need(kv_format=ksa.KSA_KV_BF16, page_stride=65536) == 0
+    assert need(num_rows=255) == need(batch=5) == need(kv_format=ksa.KSA_KV_BF16, page_stride=65536) == 0
     assert need(text_cols=5, num_rows=512) == 2 * (3 + 35) * 8 * 128 * 128 * 2 + (3 + 35) * 4
     assert need(window_chunks=1 << 30, chunk_len=8, summaries_per_chunk=0, summ_cols=0, text_cols=1 << 24) == 0       # over 2 GB: the cache itself
     assert need(head_dim=96) == ksa.KSA_ERR_UNSUPPORTED
