@@ -18,9 +18,9 @@ struct PagedArgs {
     int64_t q_st, q_sh, k_st, k_sh, v_st, v_sh, o_st, o_sh;          // in elements
     int32_t B, rows, kk, m, C, Hq, Hkv, G, D;
     PagedDiv by_chunk, by_k, by_m, by_tile;                          // divisors k + m, k, m, tokens_per_tile
-    PagedDiv by_heads, by_group;                                     // ... of a CTA's number and of a tile's row, see the kernels
+    PagedDiv by_heads, by_group, by_split;                           // ... of a CTA's number and of a tile's row, see the kernels
     int32_t page_shift, num_pages, text_cols, summ_cols;             // page_rows = 1 << page_shift
-    int32_t tokens_per_tile, head_blocks, nsplit, split_shift, box_rows;                    // attention: see the kernels
+    int32_t tokens_per_tile, head_blocks, nsplit, box_rows;                    // attention: see the kernels
     int32_t rows_min, rows_max;                                      // ... of sequences with as many rows in the call
     int32_t beside;                                                  // 1: the kernel behind runs beside this one; 2: this one is it
     uint32_t flags;

@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
     if (a.beside == 0) ptx::pdl_launch_dependents();
     ptx::pdl_wait();
     if (a.beside == 1) ptx::pdl_launch_dependents();           // the kernel behind does not wait for this one, but for those before
-    const int unit = (int)blockIdx.x >> a.split_shift, split = (int)blockIdx.x - (unit << a.split_shift);
+    const int unit = a.by_split((int)blockIdx.x), split = (int)blockIdx.x - unit * a.nsplit;
     const int item = a.by_heads(unit), hkb = unit - item * a.Hkv * a.head_blocks, hk = a.by_group(hkb), hb = hkb - hk * a.head_blocks;
     __shared__ __align__(16) PagedFound found;
     const PagedTile t = paged_tile<false>(a, item, found);
@@ -558,7 +558,7 @@ cudaError_t launch_paged_attn(const PagedArgs& args, bool e4m3, int query_rows, 
     const int64_t units = paged_most_tiles(a) * a.Hkv * a.head_blocks;
     const int64_t rows = ((int64_t)a.text_cols + (a.m > 0 ? a.summ_cols : 0)) << a.page_shift;      // of a sequence, at most
     a.nsplit = paged_splits(units, rows / 64, num_sms);
-    while (1 << a.split_shift < a.nsplit) ++a.split_shift;
+    a.by_split = PagedDiv::by(a.nsplit);
     a.by_heads = PagedDiv::by(a.Hkv * a.head_blocks); a.by_group = PagedDiv::by(a.head_blocks);
     // (a box of the warp's whole tile where a page holds it: every box costs the warp that asks for it some 50 cycles)
     a.box_rows = e4m3 && a.page_shift > 4 ? 2 * kPgRun : kPgRun;

@@ -146,7 +146,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
     if (a.beside != 2) pdl_wait();                          // (beside the kernel in front, which has waited for those before it)
     pdl_launch_dependents();
 
-    const int unit = (int)blockIdx.x >> a.split_shift, split = (int)blockIdx.x - (unit << a.split_shift);
+    const int unit = a.by_split((int)blockIdx.x), split = (int)blockIdx.x - unit * a.nsplit;
     const int item = a.by_heads(unit), hk = unit - item * a.Hkv;
     __shared__ __align__(16) PagedFound found;
     const PagedTile t = paged_tile<true>(a, item, found);   // up to 2 * per tokens
@@ -661,14 +661,18 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                     M[r] = -INFINITY; L[r] = 0.f;
                     acc[r] = make_float4(0.f, 0.f, 0.f, 0.f);
                 }
-                for (int s0 = 0; s0 < a.nsplit; s0 += 2) {                            // (a power of two, and more than one)
+                for (int s0 = 0; s0 < a.nsplit; s0 += 2) {
                     float2 ml[2][kMerge];
                     float4 v[2][kMerge];
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
-                        const uint32_t other = mapa_shared(smem_base, s0 + s) - smem_base;
+                        const uint32_t other = mapa_shared(smem_base, min(s0 + s, a.nsplit - 1)) - smem_base;
 #pragma unroll
                         for (int r = 0; r < kMerge; ++r) { ml[s][r] = pt_ld_cluster2(part_ml + pr[r] * 8 + other); v[s][r] = pt_ld_cluster4(at[r] + other); }
+                    }
+                    if (s0 + 1 == a.nsplit) {                                         // (the last of an odd number comes alone)
+#pragma unroll
+                        for (int r = 0; r < kMerge; ++r) ml[1][r].x = -INFINITY;
                     }
 #pragma unroll
                     for (int r = 0; r < kMerge; ++r) {
@@ -717,12 +721,15 @@ cudaError_t setup_paged_tc()
 
 // CTAs of one cluster for a call of `units` query tiles at most.  Joining the parts costs some 5 us of a CTA's time, so the key
 // tiles are split where SMs would stand idle: 16 query tiles of 17 (65) key tiles each on 1, 2, 4, 8 CTAs: 34.5, 28.1, 22.9,
-// 43 us (104, 63, 41, 63 us; clusters of eight CTAs that fill an SM find few places); and in two where a call of a few rounds
+// 43 us (104, 63, 41, 63 us; clusters of eight CTAs that fill an SM find few places).  More than two take seven tenths of the
+// SMs at most, since clusters of them leave SMs of a group of SMs over: 32 query tiles of some 60 key tiles on 2, 3, 4: 43.5,
+// 37.6, 40.7 us; 16 on 3, 4, 6, 8: 34.3, 30.9, 28.1, 48.7 us.  And in two where a call of a few rounds
 // holds several sequences, whose lengths differ, the longest first: two sequences of 17,000 and 8,192 rows, 16/16 heads: 206 and
 // 186 us, eight of 1 to 577 new rows over up to 31,000: 71 and 57.5 us; but one sequence, 144 even query tiles: 74 and 96 us.
 static int tc_splits(int64_t units, int64_t key_tiles, int seqs, int num_sms)
 {
-    if (units * 4 <= num_sms && key_tiles >= 16) return 4;
+    for (int n : {6, 4, 3})
+        if (units * n * 10 <= num_sms * 7 && key_tiles >= (n > 4 ? 32 : 16)) return n;
     if (units * 2 <= num_sms && key_tiles >= 12) return 2;
     return seqs > 1 && units * 2 <= 4 * num_sms && key_tiles >= 32 ? 2 : 1;
 }
@@ -738,7 +745,7 @@ cudaError_t launch_paged_tc(const PagedArgs& args, bool e4m3, int num_sms, Paged
     const int64_t text = std::min((int64_t)a.text_cols << a.page_shift, ((int64_t)a.C + 2) * a.kk + a.tokens_per_tile);
     const int64_t key_tiles = (text + (a.m > 0 ? (int64_t)a.summ_cols << a.page_shift : 0)) / kPtTile;
     a.nsplit = tc_splits(units, key_tiles, a.B, num_sms);
-    a.split_shift = a.nsplit == 4 ? 2 : a.nsplit == 2 ? 1 : 0;
+    a.by_split = PagedDiv::by(a.nsplit);
     a.by_heads = PagedDiv::by(a.Hkv);
     PagedMaps maps;
     const int box_bytes = e4m3 ? a.D : 128;

@@ -245,6 +245,19 @@ def test_long_context_with_released_pages(ctx, fmt, Hq, Hkv, D, n):
     s.check(out, lse, spans, sample=25)
 
 
+@pytest.mark.parametrize("fmt,k,m,D,ctx_rows,n", [
+    ("bf16", 8, 0, 128, 4300, 40), ("e4m3", 8, 0, 64, 4300, 70), ("bf16", 8, 1, 64, 4200, 90),     # six CTAs a query tile
+    ("bf16", 8, 0, 64, 2200, 600), ("e4m3", 8, 0, 128, 2200, 150),                                # four
+    ("bf16", 8, 0, 64, 1200, 1000), ("e4m3", 8, 0, 64, 1200, 1000),                               # three
+])
+def test_long_views_on_several_ctas(ctx, fmt, k, m, D, ctx_rows, n):
+    s = Server(ctx, k, m, 1 << 20, 8, 2, D, 64, fmt, [ctx_rows + n], seed=n)
+    spans = [(ctx_rows, n)]
+    s.fill(spans)
+    out, lse = s.attn(spans)
+    s.check(out, lse, spans, sample=40)
+
+
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("n", [1, 150])
 def test_peaked_and_spread_scores(ctx, fmt, n):
