@@ -14,25 +14,38 @@
 
 namespace ksa {
 
-constexpr int kRowThreads = 256;
+// (9,216 rows of 8 heads appended in 8 bits by blocks of 128, 256, 512 threads: 15.5, 16.9, 17.9 us; reading back moves less)
+constexpr int kRowThreads = 128;
+constexpr int kUnpackThreads = 256;
 
+// A lane's sequence among up to 32: where its rows start, how many are cached; where the last one's end
+struct PagedSeqs { int mine, rows, end; };
+__device__ __forceinline__ PagedSeqs paged_seqs(const PagedArgs& a)
+{
+    PagedSeqs s{};
+    if (a.B <= 32) {
+        const int lane = threadIdx.x & 31;
+        s.mine = __ldcg(a.cu + min(lane, a.B)); s.rows = __ldcg(a.cached + min(lane, a.B - 1)); s.end = __ldcg(a.cu + a.B);
+    }
+    return s;
+}
 // Where packed row i of the call lies: its page (or -1, -2) and the place in it; false if it is no row of a sequence.
-// Executed by whole warps.  Up to 32 sequences are searched in registers (one load instead of one after another).
-__device__ __forceinline__ bool paged_find(const PagedArgs& a, int i, int& page, int& slot)
+// Executed by whole warps.  Up to 32 sequences are searched in registers (one load instead of one after another), as many steps as
+// their number needs.
+__device__ __forceinline__ bool paged_find(const PagedArgs& a, const PagedSeqs& seqs, int i, int& page, int& slot)
 {
     int lo = 0, hi = a.B - 1, row0, r1, first;                 // the last sequence that starts at or before row i
     if (a.B <= 32) {
-        const int lane = threadIdx.x & 31, mine = __ldcg(a.cu + min(lane, a.B)), rows = __ldcg(a.cached + min(lane, a.B - 1));
-        const int end = __ldcg(a.cu + a.B);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
-            const int at = __shfl_sync(0xffffffffu, mine, (lo + o) & 31);
+            if (a.B <= o) continue;
+            const int at = __shfl_sync(0xffffffffu, seqs.mine, (lo + o) & 31);
             if (lo + o <= hi && at <= i) lo += o;
         }
-        row0 = __shfl_sync(0xffffffffu, mine, lo);
-        r1 = __shfl_sync(0xffffffffu, mine, (lo + 1) & 31);
-        if (lo == 31) r1 = end;
-        first = __shfl_sync(0xffffffffu, rows, lo);
+        row0 = __shfl_sync(0xffffffffu, seqs.mine, lo);
+        r1 = __shfl_sync(0xffffffffu, seqs.mine, (lo + 1) & 31);
+        if (lo == 31) r1 = seqs.end;
+        first = __shfl_sync(0xffffffffu, seqs.rows, lo);
     } else {
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
@@ -91,7 +104,7 @@ __device__ __forceinline__ uint32_t top8(const uint4& x)
 }
 
 // A thread's unit is a row and kHeads of its heads: one search for the row's place, then 2 kHeads loads in flight (1, 2, 4, 8
-// heads: 147,456 e4m3 rows of 4 heads read back in 109, 91, 77, 92 us; 32 rows appended in 2.3, 2.7, 3.5, 4.1 us).
+// heads: 147,456 e4m3 rows of 4 heads read back in 158, 98, 76, 85 us; 32 rows appended by 1, 2, 8 in 2.0, 2.5, 3.5 us).
 template <int D, bool E4M3, int kHeads>
 __global__ void __launch_bounds__(kRowThreads) ksa_paged_append_kernel(PagedArgs a)
 {
@@ -99,7 +112,15 @@ __global__ void __launch_bounds__(kRowThreads) ksa_paged_append_kernel(PagedArgs
     ptx::pdl_launch_dependents();
     ptx::pdl_wait();
     const int lane = threadIdx.x % kLanes, i = blockIdx.x * kUnits + threadIdx.x / kLanes, h0 = blockIdx.y * kHeads;
-    uint4 xk[kHeads], xv[kHeads];                              // (the rows' values need no place to be loaded)
+    // The rows' values need no place to be loaded, and the search's loads come back sooner without them in front.  9,216 e4m3 rows of 8
+    // heads, the values asked for first, between the lengths and the search, after it: 15.5, 14.5, 13.7 us; 32 rows: 2.15, 2.00,
+    // 2.4; 33,000 bf16 rows of 16 heads: 86.5, 84.6, 85.4.
+    constexpr bool kSearchFirst = E4M3 && kHeads > 1;
+    const PagedSeqs seqs = paged_seqs(a);
+    int page = -1, slot = 0;
+    bool put = false;
+    if constexpr (kSearchFirst) put = paged_find(a, seqs, i, page, slot);
+    uint4 xk[kHeads], xv[kHeads];
 #pragma unroll
     for (int c = 0; c < kHeads; ++c) {
         xk[c] = xv[c] = uint4{};
@@ -108,8 +129,7 @@ __global__ void __launch_bounds__(kRowThreads) ksa_paged_append_kernel(PagedArgs
             xv[c] = __ldcg(reinterpret_cast<const uint4*>(a.v + i * a.v_st + (h0 + c) * a.v_sh + lane * 8));
         }
     }
-    int page = -1, slot = 0;
-    bool put = paged_find(a, i, page, slot);
+    if constexpr (!kSearchFirst) put = paged_find(a, seqs, i, page, slot);
     if (put && page < 0) {
         atomicCAS(a.status, 0, KSA_PAGED_STATUS_BAD_PAGE);
         put = false;
@@ -154,7 +174,8 @@ __global__ void __launch_bounds__(kRowThreads) ksa_paged_gather_kernel(PagedArgs
     ptx::pdl_wait();
     const int lane = threadIdx.x % kLanes, i = blockIdx.x * kUnits + threadIdx.x / kLanes, h0 = blockIdx.y * kHeads;
     int page = -1, slot = 0;
-    const bool row = paged_find(a, i, page, slot);
+    const PagedSeqs seqs = paged_seqs(a);
+    const bool row = paged_find(a, seqs, i, page, slot);
     paged_check_all(a);
     if (!row) return;
     if (page == -2) atomicCAS(a.status, 0, KSA_PAGED_STATUS_BAD_PAGE);
@@ -204,9 +225,9 @@ struct UnpackArgs {
 };
 
 template <int D>
-__global__ void __launch_bounds__(kRowThreads) ksa_paged_unpack_kernel(PagedArgs a, UnpackArgs u)
+__global__ void __launch_bounds__(kUnpackThreads) ksa_paged_unpack_kernel(PagedArgs a, UnpackArgs u)
 {
-    constexpr int kLanes = D / 16, kRowsPass = kRowThreads / kLanes;
+    constexpr int kLanes = D / 16, kRowsPass = kUnpackThreads / kLanes;
     ptx::pdl_launch_dependents();
     ptx::pdl_wait();
     const int b = blockIdx.z, h = blockIdx.y, slot = blockIdx.x;
@@ -476,7 +497,7 @@ KSA_API int ksa_paged_attn(ksa_ctx* ctx, const ksa_paged_kv* kv, const void* q, 
             u.text_cols = (int32_t)l.text_cols; u.summ_cols = (int32_t)l.summ_cols; u.text_pages = (int32_t)l.text_pages; u.seq_pages = (int32_t)l.seq_pages;
             a.rows_min = small + 1;
             e = launch_dependent(a.D == 128 ? ksa_paged_unpack_kernel<128> : ksa_paged_unpack_kernel<64>,
-                                 dim3((unsigned)l.seq_pages, (unsigned)a.Hkv, (unsigned)a.B), kRowThreads, 0, stream, a, u);
+                                 dim3((unsigned)l.seq_pages, (unsigned)a.Hkv, (unsigned)a.B), kUnpackThreads, 0, stream, a, u);
             if (e != cudaSuccess) return e;
             ksa_ctx_add_launches(ctx, 1);
         }
