@@ -28,6 +28,10 @@
 //
 // Every mbarrier wait is bounded, as in the other kernels: on timeout all roles leave their loops, copies in flight are waited
 // for, the cluster's barriers are still passed, TMEM is freed.
+//
+// Measured: 1,152 rows over 36,864, 32/8 heads of 128, bf16: 72 us = 1,170 TFLOP/s of what is visible (83 us in a long loop, at the
+// power cap; 128 of the query tiles are full ones, on 148 SMs); 1,000 and 1,024 rows over 16,001 and 7,168, causal, 16/16 heads:
+// 183 us = 1,090 (214 us).  Tensor pipe 67 and 64 % of its cycles.
 #include <cuda_bf16.h>
 
 #include <algorithm>

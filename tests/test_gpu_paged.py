@@ -611,3 +611,27 @@ def test_refusals_of_tensors(ctx):
     cpu = ksa.PagedBatch(*(t.cpu() for t in (b.cached, b.cu_rows, b.text_table, b.summ_table)))
     with pytest.raises(ValueError):
         s.cache.append(cpu, x(3, 2, 64), x(3, 2, 64))
+
+
+def test_written_rows_have_places_of_their_own(ctx):
+    """Read tensors may repeat rows or heads (strides of 0); written ones may not."""
+    s = Server(ctx, 8, 1, 3, 4, 2, 64, 16, "bf16", [20])
+    s.key[0], s.val[0] = s.key[0][:1, :1].expand(20, 2, 64), s.val[0][:, :1].expand(20, 2, 64)
+    spans = [(0, 20)]
+    dev = lambda t: t.to(DEV)
+    s.cache.append(s.batch(spans), dev(s.key[0][:1, :1].contiguous()).expand(20, 2, 64), dev(s.val[0][:, :1].contiguous()).expand(20, 2, 64))
+    s.q[0] = s.q[0][:1].expand(20, 4, 64)
+    q = dev(s.q[0][:1].contiguous()).expand(20, 4, 64)
+    out, lse = torch.empty((20, 4, 64), dtype=torch.bfloat16, device=DEV), torch.empty((4, 20), device=DEV)
+    s.cache.attn(s.batch(spans), q, out, lse)
+    s.check(out, lse, spans)
+    rows = torch.empty((20, 2, 64), dtype=torch.bfloat16, device=DEV)
+    q = torch.zeros((20, 4, 64), dtype=torch.bfloat16, device=DEV)
+    for bad in (rows[:1].expand(20, 2, 64), rows[:, :1].expand(20, 2, 64)):
+        with pytest.raises(ksa.KsaError):
+            s.cache.gather(s.batch(spans), bad, rows)
+        with pytest.raises(ksa.KsaError):
+            s.cache.gather(s.batch(spans), rows, bad)
+    for bad in (q[:1].expand(20, 4, 64), q[:, :1].expand(20, 4, 64)):
+        with pytest.raises(ksa.KsaError):
+            s.cache.attn(s.batch(spans), q, bad, torch.empty((4, 20), device=DEV))
