@@ -106,7 +106,7 @@ __device__ __forceinline__ uint32_t pg_ld_u8(uint32_t addr)
     return v;
 }
 
-template <int D, bool E4M3, int N>
+template <int D, bool E4M3, int N, bool kMany>
 __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PgMaps maps)
 {
     using Cfg = PgCfg<D, E4M3, N>;
@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
     const int unit = a.by_split((int)blockIdx.x), split = (int)blockIdx.x - unit * a.nsplit;
     const int item = a.by_heads(unit), hkb = unit - item * a.Hkv * a.head_blocks, hk = a.by_group(hkb), hb = hkb - hk * a.head_blocks;
     __shared__ __align__(16) PagedFound found;
-    const PagedTile t = paged_tile<false>(a, item, found);
+    const PagedTile t = paged_tile<false, kMany, Cfg::kThreads>(a, item, found);
     if (t.b < 0) return;                                       // (the whole cluster)
     const int l4 = lane >> 2, c2 = (lane & 3) * 2;             // fragment row and column pair
     // the tile's rows: (token, head), heads `head0 ..` of the group
@@ -509,23 +509,28 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
     }
 }
 
-// f(kernel, shared memory) for each or one of the kernels
-template <int D, bool E4M3, int N, class F> static cudaError_t with_kernel(F f) { return f(ksa_paged_attn_kernel<D, E4M3, N>, PgCfg<D, E4M3, N>::kSmemBytes, PgCfg<D, E4M3, N>::kThreads); }
-template <int D, class F> static cudaError_t with_kernel(bool e4m3, int n, F f)
+// f(kernel, shared memory, threads) for one of the kernels
+template <int D, bool E4M3, int N, class F> static cudaError_t with_kernel(bool many, F f)
 {
-    if (e4m3) return n == 1 ? with_kernel<D, true, 1>(f) : with_kernel<D, true, 2>(f);
-    return n == 1 ? with_kernel<D, false, 1>(f) : with_kernel<D, false, 2>(f);
+    using Cfg = PgCfg<D, E4M3, N>;
+    return many ? f(ksa_paged_attn_kernel<D, E4M3, N, true>, Cfg::kSmemBytes, Cfg::kThreads) : f(ksa_paged_attn_kernel<D, E4M3, N, false>, Cfg::kSmemBytes, Cfg::kThreads);
+}
+template <int D, class F> static cudaError_t with_kernel(bool e4m3, int n, bool many, F f)
+{
+    if (e4m3) return n == 1 ? with_kernel<D, true, 1>(many, f) : with_kernel<D, true, 2>(many, f);
+    return n == 1 ? with_kernel<D, false, 1>(many, f) : with_kernel<D, false, 2>(many, f);
 }
 cudaError_t setup_paged_attn()
 {
-    for (int i = 0; i < 8; ++i) {
-        auto set = [](auto kernel, int smem, int) {
-            const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-            return e != cudaSuccess ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        };
-        const cudaError_t e = i & 4 ? with_kernel<128>(i & 1, i & 2 ? 2 : 1, set) : with_kernel<64>(i & 1, i & 2 ? 2 : 1, set);
-        if (e != cudaSuccess) return e;
-    }
+    auto set = [](auto kernel, int smem, int) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        return e != cudaSuccess ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    };
+    for (bool many : {false, true})
+        for (int n : {1, 2})
+            for (bool e4m3 : {false, true})
+                for (const cudaError_t e : {with_kernel<128>(e4m3, n, many, set), with_kernel<64>(e4m3, n, many, set)})
+                    if (e != cudaSuccess) return e;
     return cudaSuccess;
 }
 
@@ -536,7 +541,7 @@ cudaError_t setup_paged_attn()
 static int paged_splits(int64_t units, int64_t key_tiles, int num_sms)
 {
     int n = 1;
-    while (n < kPgMaxSplit && units * n * 2 <= (n == 1 ? 10 : 5) * num_sms && key_tiles >= 2 * n) n *= 2;
+    while (n < kPgMaxSplit && units * n * 2 <= (n == 1 ? 10 : 5) * num_sms && key_tiles >= 4 * n) n *= 2;       // (a CTA takes two tiles at least)
     return n;
 }
 
@@ -560,7 +565,7 @@ cudaError_t launch_paged_attn(const PagedArgs& args, bool e4m3, int query_rows, 
     a.by_tile = PagedDiv::by(a.tokens_per_tile);
     const int64_t units = paged_most_tiles(a) * a.Hkv * a.head_blocks;
     const int64_t rows = ((int64_t)a.text_cols + (a.m > 0 ? a.summ_cols : 0)) << a.page_shift;      // of a sequence, at most
-    a.nsplit = paged_splits(units, rows / 64, num_sms);
+    a.nsplit = paged_splits(units, rows / (e4m3 ? 128 : 64), num_sms);
     a.by_split = PagedDiv::by(a.nsplit);
     a.by_heads = PagedDiv::by(a.Hkv * a.head_blocks); a.by_group = PagedDiv::by(a.head_blocks);
     // (a box of the warp's whole tile where a page holds it: every box costs the warp that asks for it some 50 cycles)
@@ -583,7 +588,8 @@ cudaError_t launch_paged_attn(const PagedArgs& args, bool e4m3, int query_rows, 
         cfg.dynamicSmemBytes = (size_t)smem;
         return cudaLaunchKernelEx(&cfg, kernel, a, maps);
     };
-    return a.D == 128 ? with_kernel<128>(e4m3, n, go) : with_kernel<64>(e4m3, n, go);
+    const bool many = a.B > 64;                                // (see paged_tile)
+    return a.D == 128 ? with_kernel<128>(e4m3, n, many, go) : with_kernel<64>(e4m3, n, many, go);
 }
 
 }  // namespace ksa

@@ -153,7 +153,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
     const int unit = a.by_split((int)blockIdx.x), split = (int)blockIdx.x - unit * a.nsplit;
     const int item = a.by_heads(unit), hk = unit - item * a.Hkv;
     __shared__ __align__(16) PagedFound found;
-    const PagedTile t = paged_tile<true>(a, item, found);   // up to 2 * per tokens
+    const PagedTile t = paged_tile<true, true, Cfg::kThreads>(a, item, found);   // up to 2 * per tokens
     const int per = a.tokens_per_tile / 2;
     if (t.b >= 0) {                                         // (the same for the whole cluster)
     PagedWalk<kPtTile> w;

@@ -258,6 +258,21 @@ def test_long_views_on_several_ctas(ctx, fmt, k, m, D, ctx_rows, n):
     s.check(out, lse, spans, sample=40)
 
 
+@pytest.mark.parametrize("fmt,B,most", [("bf16", 65, 1), ("e4m3", 65, 3), ("bf16", 1100, 1), ("e4m3", 1100, 2), ("bf16", 2049, 2),   # single tokens' kernel
+                                        ("bf16", 33, 30), ("bf16", 800, 11), ("e4m3", 90, 40), ("bf16", 1537, 11)])                  # the other
+def test_many_sequences(ctx, fmt, B, most):
+    """Tens to thousands of sequences, some without rows, in whole groups too, of lengths from nothing to a few pages."""
+    rng = np.random.default_rng(B + most)
+    spans = [(int(a), int(n)) for a, n in zip(rng.integers(0, 60, B), rng.integers(0 if most > 1 else 1, most + 1, B))]
+    for b in range(32, min(B, 64)):
+        spans[b] = (spans[b][0], 0)
+    spans[B - 1] = (37, most)
+    s = Server(ctx, 8, 1, 3, 4, 1, 64, 16, fmt, [max(1, a + n) for a, n in spans], seed=B)
+    s.fill(spans)
+    out, lse = s.attn(spans, pad=3)
+    s.check(out, lse, spans, sample=2)
+
+
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("n", [1, 150])
 def test_peaked_and_spread_scores(ctx, fmt, n):
