@@ -650,3 +650,55 @@ def test_written_rows_have_places_of_their_own(ctx):
     for bad in (q[:1].expand(20, 4, 64), q[:, :1].expand(20, 4, 64)):
         with pytest.raises(ksa.KsaError):
             s.cache.attn(s.batch(spans), q, bad, torch.empty((4, 20), device=DEV))
+
+
+@pytest.mark.parametrize("fmt,n", [("bf16", 1), ("bf16", 90), ("e4m3", 1), ("e4m3", 90), ("e4m3", 700)])
+def test_pools_past_32_bits(ctx, fmt, n):
+    """Pages 2^28 elements apart, the last of them past 2^32 elements."""
+    D, ps, far = 64, 128, 1 << 28
+    base = []
+
+    def pools(pages):
+        base.append(torch.empty((pages - 1) * far + 4 * ps * D, dtype=torch.bfloat16 if fmt == "bf16" else torch.float8_e4m3fn, device=DEV))
+        return tuple(torch.as_strided(base[0], (pages, 2, ps, D), (far, ps * D, D, 1), off) for off in (0, 2 * ps * D))
+
+    s = Server(ctx, 8, 1, 4, 8, 2, D, ps, fmt, [1000, 900], seed=n, pools=pools)
+    assert s.cache.spec.num_pages > 16
+    spans = [(1000 - n, n), (900 - n // 3, n // 3)]
+    s.fill(spans)
+    out, lse = s.attn(spans)
+    s.check(out, lse, spans, sample=20)
+    got = [torch.empty((1000, 2, D), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    s.cache.gather(s.batch([(0, 1000), (0, 0)]), *got)
+    for g, rows in zip(got, (s.key, s.val)):
+        assert (g.double().cpu().numpy() == s.cached_values(rows[0])).all()
+
+
+def test_two_captured_calls_with_workspaces_run_at_once(ctx):
+    """Long runs over e4m3 pages (which the calls copy to workspaces of their own), captured twice and replayed on two streams."""
+    k, n = 8, 700
+    s = Server(ctx, k, 1, 12, 16, 2, 128, 32, "e4m3", [1500, 1200], seed=3)
+    calls = []
+    for spans in ([(800, n), (500, n)], [(400, n), (450, n)]):
+        s.fill(spans)
+        want = s.attn(spans)
+        s.check(*want, spans, sample=8)
+        calls.append((s.batch(spans), s.rows(s.q, spans), torch.zeros_like(want[0]), torch.zeros_like(want[1]), want))
+    s.append([(0, 1500), (0, 1200)])
+    streams, graphs = [torch.cuda.Stream() for _ in calls], []
+    for st, (b, q, out, lse, _) in zip(streams, calls):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            s.cache.attn(b, q, out, lse)
+        graphs.append(g)
+    for _ in range(5):
+        for c in calls:
+            c[2].fill_(7.0); c[3].fill_(7.0)
+        torch.cuda.synchronize()
+        for st, g in zip(streams, graphs):
+            with torch.cuda.stream(st):
+                g.replay(); g.replay()
+        torch.cuda.synchronize()
+        for _, _, out, lse, want in calls:
+            assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    assert ctx.device_status() == 0
