@@ -52,6 +52,12 @@ extern "C" {
 #define KSA_KV_BF16  0
 #define KSA_KV_E4M3  1
 
+/* ksa_paged_attn takes what it expects to be faster for the call's sizes: the kernel for few query rows (mma.sync) for all
+ * sequences, or the one for many (tcgen05), beside it the former for sequences of few rows where there are several.  These hold it
+ * to the first or the second; results differ in the order of roundings only.  Not both. */
+#define KSA_FLAG_PAGED_MMA_SYNC  0x20u
+#define KSA_FLAG_PAGED_TCGEN05   0x40u
+
 typedef struct {
     int32_t  struct_size;        /* sizeof(ksa_paged_params) */
     int32_t  batch;              /* sequences of the call, >= 1 */
@@ -62,7 +68,7 @@ typedef struct {
     int32_t  num_q_heads, num_kv_heads;   /* group size num_q_heads / num_kv_heads <= 64 */
     int32_t  head_dim;           /* 64 or 128 */
     float    softmax_scale;
-    uint32_t flags;              /* KSA_FLAG_SUMMARY_TEXT_ONLY */
+    uint32_t flags;              /* KSA_FLAG_SUMMARY_TEXT_ONLY, KSA_FLAG_PAGED_* */
     int32_t  kv_format;          /* KSA_KV_* */
     int32_t  page_rows;          /* 16, 32, 64 or 128 */
     int32_t  num_pages;          /* >= 1 */

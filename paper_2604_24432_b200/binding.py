@@ -29,6 +29,8 @@ KSA_FLAG_REFERENCE_KERNEL = 0x2
 KSA_FLAG_SINGLE_CTA_KERNEL = 0x4
 KSA_FLAG_CTA_PAIR_KERNEL = 0x8
 KSA_FLAG_BWD_MMA_SYNC_KERNELS = 0x10
+KSA_FLAG_PAGED_MMA_SYNC = 0x20
+KSA_FLAG_PAGED_TCGEN05 = 0x40
 KSA_STREAM_TEXT, KSA_STREAM_SUMMARY = 0, 1
 KSA_KV_BF16, KSA_KV_E4M3 = 0, 1
 KSA_PAGED_STATUS_BAD_PAGE, KSA_PAGED_STATUS_BAD_ROWS = 103, 104

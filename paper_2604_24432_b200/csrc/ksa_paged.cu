@@ -343,7 +343,8 @@ static int validate_shape(const ksa_paged_params* p)
     if (p->batch < 1 || p->num_rows < 0 || p->chunk_len < 1 || p->summaries_per_chunk < 0 || p->window_chunks < 0) return KSA_ERR_INVALID_ARG;
     if (p->num_q_heads < 1 || p->num_kv_heads < 1 || p->num_q_heads % p->num_kv_heads != 0) return KSA_ERR_INVALID_ARG;
     if (!(p->softmax_scale > 0.f) || p->softmax_scale > 1e30f) return KSA_ERR_INVALID_ARG;
-    if (p->flags & ~KSA_FLAG_SUMMARY_TEXT_ONLY) return KSA_ERR_INVALID_ARG;
+    constexpr uint32_t kOne = KSA_FLAG_PAGED_MMA_SYNC | KSA_FLAG_PAGED_TCGEN05;
+    if (p->flags & ~(KSA_FLAG_SUMMARY_TEXT_ONLY | kOne) || (p->flags & kOne) == kOne) return KSA_ERR_INVALID_ARG;
     if (p->kv_format != KSA_KV_BF16 && p->kv_format != KSA_KV_E4M3) return KSA_ERR_INVALID_ARG;
     if (p->num_pages < 1 || p->text_cols < 1 || p->summ_cols < (p->summaries_per_chunk > 0 ? 1 : 0)) return KSA_ERR_INVALID_ARG;
     if (p->head_dim != 64 && p->head_dim != 128) return KSA_ERR_UNSUPPORTED;
@@ -485,18 +486,22 @@ KSA_API int ksa_paged_attn(ksa_ctx* ctx, const ksa_paged_kv* kv, const void* q, 
         }
         // Up to 16 query rows a sequence, on average (64 over e4m3 pages): the mma.sync kernel for all.  16 sequences of 3, 4, 5, 6, 8 rows
         // over 800 to 37,000, 32/8 heads (12 to 32 query rows), that one and the tcgen05 kernel: bf16 50, 50, 55, 86, 86 and 48, 51, 51,
-        // 52, 55 us, e4m3 40, 41, 48, 57, 60 and 78, 81, 82, 84, 90 us.  More, and several sequences: that one for those that fit into
+        // 52, 55 us, e4m3 40, 41, 48, 57, 60 and 78, 81, 82, 84, 90 us.  More: the same where it is expected to be faster, since
+        // it finds work for more SMs in small calls (115 rows over 720, 4/4 heads: 8.3 and 17 us; 191 e4m3 rows over 7,000,
+        // 10/2 heads: 15 and 26).  Else, with several sequences, that one for those that fit into
         // its tiles (single tokens beside prompts), and the tcgen05 kernel, which takes as long over one query row as over 256,
         // beside it for the others: 24 tokens over 90,000 to 113,000 rows and 1,152 rows over 36,864, 32/8 heads:
         // e4m3 484 -> 261 us, bf16 251 -> 259; the 24 over 1,000 to 3,500 rows: 152 -> 156, 126 -> 100.  A launch that finds no
         // such sequence costs 4 us.
-        const int sms = ksa_ctx_num_sms(ctx);
+        const int sms = ksa_ctx_num_sms(ctx), query_rows = (int64_t)a.rows * a.G <= 8 * (int64_t)a.B ? 8 : 16;
         const int64_t rows = (int64_t)a.rows * a.G;
         a.rows_min = 1; a.rows_max = a.rows;
-        if (rows <= (e4m3 ? 64 : 16) * (int64_t)a.B) return launch_paged_attn(a, e4m3, rows <= 8 * (int64_t)a.B ? 8 : 16, sms, encode, stream);
-        const int small = a.B < 4 || rows <= 64 * (int64_t)a.B || a.G > 16 ? 0 : (a.G > 8 ? 16 : 8) / a.G;      // rows of a sequence for the former
         const UnpackLayout l = unpack_layout(p);
         const bool copy = l.bytes > 0 && workspace && workspace_bytes >= (size_t)l.bytes;
+        bool few = rows <= (e4m3 ? 64 : 16) * (int64_t)a.B || paged_attn_us(a, e4m3, query_rows, sms) < paged_tc_us(a, e4m3 && !copy, sms) + (copy ? 6.0f : 0.0f);
+        if (p->flags & (KSA_FLAG_PAGED_MMA_SYNC | KSA_FLAG_PAGED_TCGEN05)) few = p->flags & KSA_FLAG_PAGED_MMA_SYNC;
+        if (few) return launch_paged_attn(a, e4m3, query_rows, sms, encode, stream);
+        const int small = a.B < 4 || rows <= 64 * (int64_t)a.B || a.G > 16 ? 0 : (a.G > 8 ? 16 : 8) / a.G;      // rows of a sequence for the former
         UnpackArgs u{};
         if (copy) {
             u.k = (uint16_t*)workspace; u.v = u.k + l.kv_bytes / 2;

@@ -10,6 +10,8 @@ from tests import paged_ref as ref
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
+# the kernel as the call takes it, and held to the one for many query rows
+BY_RULE, MANY, FEW = 0, ksa.KSA_FLAG_PAGED_TCGEN05, ksa.KSA_FLAG_PAGED_MMA_SYNC
 
 
 @pytest.fixture(scope="module")
@@ -98,7 +100,7 @@ class Server:
                 key, val = self.cached_values(self.key[b][:a + n]), self.cached_values(self.val[b][:a + n])
                 picks = range(n) if sample is None or n <= sample else sorted(set([0, n - 1, *np.random.default_rng(b).integers(0, n, sample)]))
                 for i in picks:
-                    r = ref.attention(self.q[b][a + i:a + i + 1].double().numpy(), key[:a + i + 1], val[:a + i + 1], self.k, self.m, self.C, a + i, self.scale, bool(self.flags))
+                    r = ref.attention(self.q[b][a + i:a + i + 1].double().numpy(), key[:a + i + 1], val[:a + i + 1], self.k, self.m, self.C, a + i, self.scale, bool(self.flags & ksa.KSA_FLAG_SUMMARY_TEXT_ONLY))
                     ref.check(out[row0 + i:row0 + i + 1], lse[row0 + i:row0 + i + 1], r, self.D)
             row0 += n
         assert (out[row0:] == 7.0).all() and (lse[row0:] == -1.0).all()      # rows behind the last sequence
@@ -215,22 +217,24 @@ SHAPES = [
 ]
 
 
+@pytest.mark.parametrize("kernel", [BY_RULE, MANY, FEW])
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("k,m,C,Hq,Hkv,D,ps,flags,spans,pad", SHAPES)
-def test_attention(ctx, fmt, k, m, C, Hq, Hkv, D, ps, flags, spans, pad):
-    s = Server(ctx, k, m, C, Hq, Hkv, D, ps, fmt, [max(1, a + n) for a, n in spans], flags, seed=11)
+def test_attention(ctx, kernel, fmt, k, m, C, Hq, Hkv, D, ps, flags, spans, pad):
+    s = Server(ctx, k, m, C, Hq, Hkv, D, ps, fmt, [max(1, a + n) for a, n in spans], flags | kernel, seed=11)
     s.fill(spans)
     out, lse = s.attn(spans, pad)
     s.check(out, lse, spans, sample=60)
 
 
+@pytest.mark.parametrize("kernel", [BY_RULE, MANY])
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("Hq,Hkv,D,n", [(8, 2, 128, 1), (8, 2, 128, 300), (4, 4, 64, 40)])
-def test_long_context_with_released_pages(ctx, fmt, Hq, Hkv, D, n):
+def test_long_context_with_released_pages(ctx, kernel, fmt, Hq, Hkv, D, n):
     """Text that has left every window is given back (and its pages poisoned); rows behind the sequence are NaN."""
     k, m, C, ps = 8, 1, 9, 16
     a = 6007
-    s = Server(ctx, k, m, C, Hq, Hkv, D, ps, fmt, [a + n + 40, 33], seed=5)
+    s = Server(ctx, k, m, C, Hq, Hkv, D, ps, fmt, [a + n + 40, 33], seed=5, flags=kernel)
     spans = [(a, n), (20, 3)]
     s.fill(spans)
     first = max(0, a // 9 - C) * k // ps
@@ -245,39 +249,42 @@ def test_long_context_with_released_pages(ctx, fmt, Hq, Hkv, D, n):
     s.check(out, lse, spans, sample=25)
 
 
+@pytest.mark.parametrize("kernel", [BY_RULE, MANY])
 @pytest.mark.parametrize("fmt,k,m,D,ctx_rows,n", [
     ("bf16", 8, 0, 128, 4300, 40), ("e4m3", 8, 0, 64, 4300, 70), ("bf16", 8, 1, 64, 4200, 90),     # six CTAs a query tile
     ("bf16", 8, 0, 64, 2200, 600), ("e4m3", 8, 0, 128, 2200, 150),                                # four
     ("bf16", 8, 0, 64, 1200, 1000), ("e4m3", 8, 0, 64, 1200, 1000),                               # three
 ])
-def test_long_views_on_several_ctas(ctx, fmt, k, m, D, ctx_rows, n):
-    s = Server(ctx, k, m, 1 << 20, 8, 2, D, 64, fmt, [ctx_rows + n], seed=n)
+def test_long_views_on_several_ctas(ctx, kernel, fmt, k, m, D, ctx_rows, n):
+    s = Server(ctx, k, m, 1 << 20, 8, 2, D, 64, fmt, [ctx_rows + n], seed=n, flags=kernel)
     spans = [(ctx_rows, n)]
     s.fill(spans)
     out, lse = s.attn(spans)
     s.check(out, lse, spans, sample=40)
 
 
+@pytest.mark.parametrize("kernel", [BY_RULE, MANY])
 @pytest.mark.parametrize("fmt,B,most", [("bf16", 65, 1), ("e4m3", 65, 3), ("bf16", 1100, 1), ("e4m3", 1100, 2), ("bf16", 2049, 2),   # single tokens' kernel
                                         ("bf16", 33, 30), ("bf16", 800, 11), ("e4m3", 90, 40), ("bf16", 1537, 11)])                  # the other
-def test_many_sequences(ctx, fmt, B, most):
+def test_many_sequences(ctx, kernel, fmt, B, most):
     """Tens to thousands of sequences, some without rows, in whole groups too, of lengths from nothing to a few pages."""
     rng = np.random.default_rng(B + most)
     spans = [(int(a), int(n)) for a, n in zip(rng.integers(0, 60, B), rng.integers(0 if most > 1 else 1, most + 1, B))]
     for b in range(32, min(B, 64)):
         spans[b] = (spans[b][0], 0)
     spans[B - 1] = (37, most)
-    s = Server(ctx, 8, 1, 3, 4, 1, 64, 16, fmt, [max(1, a + n) for a, n in spans], seed=B)
+    s = Server(ctx, 8, 1, 3, 4, 1, 64, 16, fmt, [max(1, a + n) for a, n in spans], seed=B, flags=kernel)
     s.fill(spans)
     out, lse = s.attn(spans, pad=3)
     s.check(out, lse, spans, sample=2)
 
 
+@pytest.mark.parametrize("kernel", [BY_RULE, MANY])
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("n", [1, 150])
-def test_peaked_and_spread_scores(ctx, fmt, n):
+def test_peaked_and_spread_scores(ctx, kernel, fmt, n):
     """Scores up to hundreds: the running maximum moves often, and rows differ by orders of magnitude."""
-    s = Server(ctx, 8, 1, 40, 8, 2, 128, 32, fmt, [1000], seed=8, qkv_scale=4.0)
+    s = Server(ctx, 8, 1, 40, 8, 2, 128, 32, fmt, [1000], seed=8, qkv_scale=4.0, flags=kernel)
     for b in (s.key, s.val):
         b[0][::97] *= 16.0
         b[0][5::41] *= 2.0 ** -20
@@ -287,6 +294,7 @@ def test_peaked_and_spread_scores(ctx, fmt, n):
     s.check(out, lse, spans, sample=25)
 
 
+@pytest.mark.parametrize("kernel", [MANY])
 @pytest.mark.parametrize("k,m,C,Hq,Hkv,D,ps,flags,spans,pad", [
     (8, 1, 9, 16, 4, 128, 64, 0, [(2003, 700)], 0),
     (8, 1, 9, 8, 1, 64, 16, 0, [(77, 800), (0, 0), (1500, 300)], 3),
@@ -296,10 +304,10 @@ def test_peaked_and_spread_scores(ctx, fmt, n):
     (8, 1, 0, 32, 4, 128, 16, 0, [(9, 300)], 0),
     (8, 1, 5, 16, 2, 128, 32, 0, [(900, 1), (13, 1400), (0, 0), (300, 2), (44, 17)], 2),      # single tokens among them
 ])
-def test_long_runs_over_e4m3(ctx, k, m, C, Hq, Hkv, D, ps, flags, spans, pad):
+def test_long_runs_over_e4m3(ctx, kernel, k, m, C, Hq, Hkv, D, ps, flags, spans, pad):
     """With the workspace (the rows in view as bf16 pages) and without: each against the reference.  Pages before every window are
     given back, and whatever nobody sees is NaN; so is the workspace."""
-    s = Server(ctx, k, m, C, Hq, Hkv, D, ps, "e4m3", [a + n + 7 for a, n in spans], flags, seed=19)
+    s = Server(ctx, k, m, C, Hq, Hkv, D, ps, "e4m3", [a + n + 7 for a, n in spans], flags | kernel, seed=19)
     s.fill(spans)
     for b, (a, n) in enumerate(spans):
         s.text[b, :max(0, a // (k + m) - C) * k // ps] = -1
@@ -317,12 +325,13 @@ def test_long_runs_over_e4m3(ctx, k, m, C, Hq, Hkv, D, ps, flags, spans, pad):
         s.check(out, lse, spans, sample=24)
 
 
+@pytest.mark.parametrize("kernel", [BY_RULE, MANY])
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("n", [1, 150, 700])
 @pytest.mark.parametrize("what", ["all V", "some V", "all K", "tiny V", "huge V"])
-def test_rows_of_zeros_and_of_extreme_size(ctx, fmt, n, what):
+def test_rows_of_zeros_and_of_extreme_size(ctx, kernel, fmt, n, what):
     """Rows of zeros have the least scale: their keys count in the sums all the same.  V of 1e-15 or 1e30 scales the output."""
-    s = Server(ctx, 8, 1, 100, 8, 2, 128, 32, fmt, [1100], seed=9)
+    s = Server(ctx, 8, 1, 100, 8, 2, 128, 32, fmt, [1100], seed=9, flags=kernel)
     rows = (s.val if "V" in what else s.key)[0]
     if what.startswith("all"):
         rows.zero_()
@@ -337,26 +346,28 @@ def test_rows_of_zeros_and_of_extreme_size(ctx, fmt, n, what):
     s.check(out, lse, spans, sample=12)
 
 
-def test_one_page_and_one_head_of_any_stride(ctx):
+@pytest.mark.parametrize("kernel", [BY_RULE, MANY])
+def test_one_page_and_one_head_of_any_stride(ctx, kernel):
     """Strides of a dimension of one are not looked at."""
     D = 64
     base = torch.empty(5 * 128 * D + 3 * D, dtype=torch.bfloat16, device=DEV)
     pools = lambda n: tuple(torch.as_strided(base, (1, 1, 128, D), (3, 5, D, 1), off) for off in (0, 128 * D + 2 * D))
     for n in (1, 90):
-        s = Server(ctx, 8, 0, 100, 4, 1, D, 128, "bf16", [100], seed=2, spare=0, pools=pools)
+        s = Server(ctx, 8, 0, 100, 4, 1, D, 128, "bf16", [100], seed=2, spare=0, pools=pools, flags=kernel)
         spans = [(100 - n, n)]
         s.fill(spans)
         out, lse = s.attn(spans)
         s.check(out, lse, spans, sample=20)
 
 
-def test_strided_pools_and_rows(ctx):
+@pytest.mark.parametrize("kernel", [BY_RULE, MANY])
+def test_strided_pools_and_rows(ctx, kernel):
     """Pages as [page, row, head, d] and padded heads; q a slice of a fused projection; out a slice of a wider tensor."""
     k, m, C, Hq, Hkv, D, ps = 8, 1, 3, 8, 2, 128, 32
     pools = lambda n: tuple(torch.empty((n, ps, Hkv + 1, D), dtype=torch.bfloat16, device=DEV)[:, :, :Hkv].transpose(1, 2) for _ in range(2))
     for n in (1, 200):
         spans = [(150, n), (31, 2)]
-        s = Server(ctx, k, m, C, Hq, Hkv, D, ps, "bf16", [a + c for a, c in spans], pools=pools, seed=4)
+        s = Server(ctx, k, m, C, Hq, Hkv, D, ps, "bf16", [a + c for a, c in spans], pools=pools, seed=4, flags=kernel)
         total = n + 2
         fused = torch.zeros((a_ := sum(a + c for a, c in spans), Hkv * 2 + 1, D), dtype=torch.bfloat16, device=DEV)
         full = [(0, a + c) for a, c in spans]
@@ -474,13 +485,14 @@ def test_pieces_equal_the_forward_pass_and_go_on_in_the_contiguous_cache(ctx):
     s.check(step_out, step_lse.t().contiguous(), [(L, 1)])
 
 
+@pytest.mark.parametrize("kernel", [BY_RULE, MANY])
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 128), (16, 1, 64), (16, 2, 64), (20, 1, 128)])
-def test_tokens_and_prompts_in_one_call(ctx, fmt, Hq, Hkv, D):
+def test_tokens_and_prompts_in_one_call(ctx, kernel, fmt, Hq, Hkv, D):
     """Sequences of one row to hundreds in a call, more than 32 of them, in and out of order: every row by the kernel it falls to.  Many
     calls after another, each appending what the next attends to."""
     lens = [700, 40, 300, 33, 1, 9, 150] + [20 + 7 * i for i in range(30)]
-    s = Server(ctx, 8, 1, 4, Hq, Hkv, D, 16, fmt, lens, seed=23)
+    s = Server(ctx, 8, 1, 4, Hq, Hkv, D, 16, fmt, lens, seed=23, flags=kernel)
     at = [n // 2 for n in lens]
     s.append([(0, n) for n in at])
     for step in range(3):
@@ -491,11 +503,12 @@ def test_tokens_and_prompts_in_one_call(ctx, fmt, Hq, Hkv, D):
         at = [a + n for a, n in spans]
 
 
+@pytest.mark.parametrize("kernel", [BY_RULE, MANY])
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("n", [1, 40])
-def test_captured_calls_follow_lengths_and_tables(ctx, fmt, n):
+def test_captured_calls_follow_lengths_and_tables(ctx, kernel, fmt, n):
     """append + attn in a graph, replayed with other lengths, tables and rows; two graphs of the same cache; on a side stream."""
-    s = Server(ctx, 8, 1, 5, 8, 2, 128, 16, fmt, [600, 600], seed=31)
+    s = Server(ctx, 8, 1, 5, 8, 2, 128, 16, fmt, [600, 600], seed=31, flags=kernel)
     rows = 2 * n
     batch = s.batch([(0, n), (0, n)])
     q = torch.zeros((rows, 8, 128), dtype=torch.bfloat16, device=DEV)
@@ -535,11 +548,12 @@ def test_captured_calls_follow_lengths_and_tables(ctx, fmt, n):
     assert ctx.device_status() == 0
 
 
+@pytest.mark.parametrize("kernel", [BY_RULE, MANY])
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
-def test_many_calls_in_a_row_in_a_graph(ctx, fmt):
+def test_many_calls_in_a_row_in_a_graph(ctx, kernel, fmt):
     """Eight steps of append and attn, one after another without a pause, kernels beside one another: as each step alone, twice."""
     lens = [500, 60, 340, 90, 340, 700]
-    s = Server(ctx, 8, 1, 5, 16, 2, 128, 16, fmt, lens, seed=41)
+    s = Server(ctx, 8, 1, 5, 16, 2, 128, 16, fmt, lens, seed=41, flags=kernel)
     start = [n // 2 for n in lens]
     steps = [[(start[b] + (i if b % 2 else 20 * i), 1 if b % 2 else 20) for b in range(len(lens))] for i in range(8)]
     s.append([(0, n) for n in start])
@@ -573,10 +587,11 @@ def test_many_calls_in_a_row_in_a_graph(ctx, fmt):
     assert ctx.device_status() == 0
 
 
-def test_two_streams_and_repeated_calls_agree(ctx):
+@pytest.mark.parametrize("kernel", [BY_RULE, MANY])
+def test_two_streams_and_repeated_calls_agree(ctx, kernel):
     """The same calls on two streams at once, and again: bit for bit the same (sums are in a fixed order)."""
     for n in (1, 5, 200):
-        s = Server(ctx, 8, 1, 20, 32, 4, 128, 64, "e4m3", [900, 700, 300], seed=17)
+        s = Server(ctx, 8, 1, 20, 32, 4, 128, 64, "e4m3", [900, 700, 300], seed=17, flags=kernel)
         spans = [(700, n), (500, n), (100, n)]
         s.fill(spans)
         want = s.attn(spans)
@@ -652,8 +667,9 @@ def test_written_rows_have_places_of_their_own(ctx):
             s.cache.attn(s.batch(spans), q, bad, torch.empty((4, 20), device=DEV))
 
 
+@pytest.mark.parametrize("kernel", [BY_RULE, MANY])
 @pytest.mark.parametrize("fmt,n", [("bf16", 1), ("bf16", 90), ("e4m3", 1), ("e4m3", 90), ("e4m3", 700)])
-def test_pools_past_32_bits(ctx, fmt, n):
+def test_pools_past_32_bits(ctx, kernel, fmt, n):
     """Pages 2^28 elements apart, the last of them past 2^32 elements."""
     D, ps, far = 64, 128, 1 << 28
     base = []
@@ -662,7 +678,7 @@ def test_pools_past_32_bits(ctx, fmt, n):
         base.append(torch.empty((pages - 1) * far + 4 * ps * D, dtype=torch.bfloat16 if fmt == "bf16" else torch.float8_e4m3fn, device=DEV))
         return tuple(torch.as_strided(base[0], (pages, 2, ps, D), (far, ps * D, D, 1), off) for off in (0, 2 * ps * D))
 
-    s = Server(ctx, 8, 1, 4, 8, 2, D, ps, fmt, [1000, 900], seed=n, pools=pools)
+    s = Server(ctx, 8, 1, 4, 8, 2, D, ps, fmt, [1000, 900], seed=n, pools=pools, flags=kernel)
     assert s.cache.spec.num_pages > 16
     spans = [(1000 - n, n), (900 - n // 3, n // 3)]
     s.fill(spans)
@@ -674,10 +690,11 @@ def test_pools_past_32_bits(ctx, fmt, n):
         assert (g.double().cpu().numpy() == s.cached_values(rows[0])).all()
 
 
-def test_two_captured_calls_with_workspaces_run_at_once(ctx):
+@pytest.mark.parametrize("kernel", [BY_RULE, MANY])
+def test_two_captured_calls_with_workspaces_run_at_once(ctx, kernel):
     """Long runs over e4m3 pages (which the calls copy to workspaces of their own), captured twice and replayed on two streams."""
     k, n = 8, 700
-    s = Server(ctx, k, 1, 12, 16, 2, 128, 32, "e4m3", [1500, 1200], seed=3)
+    s = Server(ctx, k, 1, 12, 16, 2, 128, 32, "e4m3", [1500, 1200], seed=3, flags=kernel)
     calls = []
     for spans in ([(800, n), (500, n)], [(400, n), (450, n)]):
         s.fill(spans)

@@ -220,7 +220,7 @@ BAD, UNSUP = ksa.KSA_ERR_INVALID_ARG, ksa.KSA_ERR_UNSUPPORTED
 @pytest.mark.parametrize("change,want", [
     (dict(struct_size=8), BAD), (dict(batch=0), BAD), (dict(num_rows=-1), BAD), (dict(chunk_len=0), BAD), (dict(summaries_per_chunk=-1), BAD),
     (dict(window_chunks=-1), BAD), (dict(num_q_heads=7), BAD), (dict(num_kv_heads=0), BAD), (dict(head_dim=96), UNSUP),
-    (dict(softmax_scale=0.0), BAD), (dict(softmax_scale=float("nan")), BAD), (dict(flags=2), BAD), (dict(kv_format=2), BAD),
+    (dict(softmax_scale=0.0), BAD), (dict(softmax_scale=float("nan")), BAD), (dict(flags=2), BAD), (dict(flags=0x60), BAD), (dict(kv_format=2), BAD),
     (dict(page_rows=48), UNSUP), (dict(page_rows=256), UNSUP), (dict(page_rows=8), UNSUP), (dict(num_pages=0), BAD), (dict(text_cols=0), BAD),
     (dict(summ_cols=0), BAD), (dict(page_stride=-16), BAD), (dict(page_stride=0), BAD), (dict(head_stride=0), BAD), (dict(row_stride=1 << 38), UNSUP), (dict(row_stride=120), BAD), (dict(row_stride=64), BAD), (dict(head_stride=8), BAD),
     (dict(num_q_heads=130), UNSUP), (dict(num_rows=1 << 25), UNSUP), (dict(batch=70000), UNSUP), (dict(chunk_len=2**31 - 1), UNSUP),
