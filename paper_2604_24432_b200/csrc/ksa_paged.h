@@ -20,7 +20,7 @@ struct PagedArgs {
     PagedDiv by_chunk, by_k, by_m, by_tile;                          // divisors k + m, k, m, tokens_per_tile
     PagedDiv by_heads, by_group, by_split;                           // ... of a CTA's number and of a tile's row, see the kernels
     int32_t page_shift, num_pages, text_cols, summ_cols;             // page_rows = 1 << page_shift
-    int32_t tokens_per_tile, head_blocks, nsplit, box_rows;                    // attention: see the kernels
+    int32_t tokens_per_tile, head_blocks, nsplit, box_rows;        // attention: see the kernels
     int32_t rows_min, rows_max;                                      // ... of sequences with as many rows in the call
     int32_t beside;                                                  // 1: the kernel behind runs beside this one; 2: this one is it
     uint32_t flags;
@@ -40,7 +40,7 @@ cudaError_t setup_paged_attn();
 cudaError_t launch_paged_tc(const PagedArgs& a, bool e4m3, int num_sms, PagedEncode encode, cudaStream_t stream);
 cudaError_t setup_paged_tc();
 // What the call will take by the one and the other, in us and roughly, from the lengths that the host knows: every sequence as long
-// as its table, rows spread evenly.  Fitted to 115 calls (80 drawn at random over all sizes): taking the smaller estimate costs
+// as its table, rows spread evenly.  Fitted to 115 calls (94 drawn at random over all sizes): taking the smaller estimate costs
 // 1.4 % over the better kernel each time on average, borders on the query rows alone cost 8.7 %.
 float paged_attn_us(const PagedArgs& a, bool e4m3, int query_rows, int num_sms);
 float paged_tc_us(const PagedArgs& a, bool e4m3, int num_sms);
