@@ -131,6 +131,16 @@ def _kv_rows(shape, gen):
     return x
 
 
+_CONTEXT = []
+
+
+def _context(ksa):
+    """The library's handle on the device: one a process, as a server opens it, however many caches it has."""
+    if not _CONTEXT:
+        _CONTEXT.append(ksa.Context(0))
+    return _CONTEXT[0]
+
+
 def prepare(case, seed):
     gen = torch.Generator(device=DEV).manual_seed(seed)
     k, m, C = LAYOUTS[case["layout"]]
@@ -187,7 +197,7 @@ def prepare(case, seed):
     if own:
         from paper_2604_24432_b200 import binding as ksa
         spec = ksa.PagedSpec(k, m, C, hq, hkv, d, float(np.float32(d ** -0.5)), ps, num_pages, case["fmt"])
-        st["cache"] = ksa.PagedCache(ksa.Context(0), spec, st["kp"], st["vp"], st["ke"] if case["fmt"] == "e4m3" else None, st["ve"] if case["fmt"] == "e4m3" else None)
+        st["cache"] = ksa.PagedCache(_context(ksa), spec, st["kp"], st["vp"], st["ke"] if case["fmt"] == "e4m3" else None, st["ve"] if case["fmt"] == "e4m3" else None)
         st["batch"] = ksa.PagedBatch(st["cached"], st["cu"], st["text"], st["summ"])
     return st
 
