@@ -16,8 +16,11 @@
 // values (sm_100 has no mma.sync for e4m3: it is made of conversions to f16 and two f16 products).  So Q becomes f16 too, its
 // row scaled by a power of two, and the scale of a key multiplies its scores.  The scale of a value row goes into the
 // exponent, u = 2^(score + e - 127 - reference) with the reference maximum taken over these sums: u is at most 2^8 and what f16
-// rounds off or loses is relative to the largest that the row has met, whatever the scales are; the softmax's sum takes
-// u 2^(127 - e).  A key's 16 bytes hold four values for each of four lanes; which of the 16 columns a product calls its k-th
+// rounds off or loses is relative to the largest that the row has met, whatever the scales are.  The softmax's sum has a
+// reference of its own, over the scores: from u it would be u 2^(127 - e), and since the scales span 2^-110 .. 2^120, either
+// may be beyond fp32 where the other is about one.  (An exponential and a
+// maximum more a score, some constants fewer: 32 tokens over 147,451 rows each 110.9 and 110.1 us, timed in turn.)
+// A key's 16 bytes hold four values for each of four lanes; which of the 16 columns a product calls its k-th
 // does not matter as long as Q agrees, so lane t takes columns 4 t .. 4 t + 3 as they stand.  Of V, ldmatrix.trans hands a lane
 // two neighbouring columns of two keys, which become rows r and r + 8 of a product.
 //
@@ -59,10 +62,11 @@ struct PgCfg {
     // log2 units.  The reference maximum moves when a score outgrows it by this
     static constexpr float kRescale = 8.0f;
     static constexpr int kLd = D + 4;                           // floats from one row of partial results to the next
-    static constexpr int kMergeB = kWarps * kRows * (kLd + 2) * 4;      // the warps' results, over the ring
+    static constexpr int kMl = E4M3 ? 4 : 2;                    // floats of a row beside O: maximum, sum; e4m3: the sum's own maximum
+    static constexpr int kMergeB = kWarps * kRows * (kLd + kMl) * 4;    // the warps' results, over the ring
     // what the cluster's other CTAs push: memory of its own, this CTA may still be at work
     static constexpr int kPushOff = kWarps * kRingB > kMergeB ? kWarps * kRingB : kMergeB;
-    static constexpr int kPushO = (kRows * (D / 4) + kPgMaxSplit) * 16, kPushMl = kPgMaxSplit * kRows * 8;
+    static constexpr int kPushO = (kRows * (D / 4) + kPgMaxSplit) * 16, kPushMl = kPgMaxSplit * kRows * kMl * 4;
     static constexpr int kScaleOff = kPushOff + kPushO + kPushMl;       // [warps][stages]
     static constexpr int kBarOff = kScaleOff + kWarps * kStages * kScaleB;
     static constexpr int kSmemBytes = kBarOff + 8 * kWarps * kStages + 16 + 1024;       // + slack for 1024-byte alignment
@@ -244,10 +248,10 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
         }
     }
     float o[D / 16][N][4];
-    float m[N][2], l[N][2];                                    // of query rows 8 n + c2, + 1
+    float m[N][2], l[N][2], ml[N][2];                          // of query rows 8 n + c2, + 1; e4m3: ml is the reference of the sum
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        m[n][0] = m[n][1] = -INFINITY; l[n][0] = l[n][1] = 0.f;
+        m[n][0] = m[n][1] = ml[n][0] = ml[n][1] = -INFINITY; l[n][0] = l[n][1] = 0.f;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) { o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f; }
     }
@@ -286,7 +290,7 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
             __syncwarp();
         }
         // S^T (16 keys x 8 N query rows, run by run) = K Q^T, in log2 units
-        float s[kSubs][N][4], back[kSubs][2], tiny[kSubs][2];  // e4m3: with the value rows' exponents, 2^(127 - 20 - e) of these, see below
+        float s[kSubs][N][4], r[kSubs][N][4];                  // e4m3: with the value rows' exponents, and without
 #pragma unroll
         for (int u = 0; u < kSubs; ++u) {
 #pragma unroll
@@ -310,16 +314,14 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
                 for (int h = 0; h < 2; ++h) {                  // keys l4, l4 + 8
                     const float fk = a.scale_log2 * e8m0_factor(pg_ld_u8(se + 8 * h));
                     const uint32_t e = pg_ld_u8(se + 16 + 8 * h);
-                    // Exponents below -64 count as -64 (a row of zeros has -110, and its share of the sum must not underflow), and
-                    // what is left of such a row's values goes into its probability.
-                    const uint32_t ec = max(e, 63u);
-                    tiny[u][h] = e < 63u ? __uint_as_float((e + 64u) << 23) : 1.f;
-                    const float ef = e == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(0x4b000000u | ec) - (8388608.f + 127.f);
-                    back[u][h] = __uint_as_float((uint32_t)max((int)(234u - ec) << 23, 0x00400000));      // (2^-20: sums stay far below 2^128)
+                    const float ef = e == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(0x4b000000u | e) - (8388608.f + 127.f);
 #pragma unroll
                     for (int n = 0; n < N; ++n)
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) s[u][n][2 * h + c] = fmaf(s[u][n][2 * h + c] * qf[n][c], fk, ef);
+                        for (int c = 0; c < 2; ++c) {
+                            r[u][n][2 * h + c] = s[u][n][2 * h + c] * qf[n][c] * fk;
+                            s[u][n][2 * h + c] = r[u][n][2 * h + c] + ef;
+                        }
                 }
             } else {
 #pragma unroll
@@ -345,11 +347,14 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
                     for (int u = 0; u < kSubs; ++u)
 #pragma unroll
                         for (int h = 0; h < 2; ++h)
-                            if (16 * u + 8 * h < rlo || 16 * u + 8 * h >= rhi) s[u][n][2 * h + c] = -INFINITY;
+                            if (16 * u + 8 * h < rlo || 16 * u + 8 * h >= rhi) {
+                                s[u][n][2 * h + c] = -INFINITY;
+                                if constexpr (E4M3) r[u][n][2 * h + c] = -INFINITY;
+                            }
                 }
         }
         // the reference maximum moves, and O with it, only when some row outgrew its own (eight lanes share a row)
-        float mx[N][2];
+        float mx[N][2], rx[N][2];
         bool grown = false;
 #pragma unroll
         for (int n = 0; n < N; ++n)
@@ -359,6 +364,12 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
 #pragma unroll
                 for (int u = 1; u < kSubs; ++u) mx[n][c] = ptx::fmax3(mx[n][c], s[u][n][c], s[u][n][2 + c]);
                 grown |= mx[n][c] > m[n][c] + Cfg::kRescale;
+                if constexpr (E4M3) {
+                    rx[n][c] = fmaxf(r[0][n][c], r[0][n][2 + c]);
+#pragma unroll
+                    for (int u = 1; u < kSubs; ++u) rx[n][c] = ptx::fmax3(rx[n][c], r[u][n][c], r[u][n][2 + c]);
+                    grown |= rx[n][c] > ml[n][c] + Cfg::kRescale;
+                }
             }
         if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
@@ -370,7 +381,16 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
                     for (int b = 4; b < 32; b <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, b));
                     const float mn = fmaxf(m[n][c], x), al = (mn == -INFINITY) ? 1.f : ptx::ex2_approx(m[n][c] - mn);
                     m[n][c] = mn;
-                    l[n][c] *= al;
+                    if constexpr (E4M3) {
+                        x = rx[n][c];
+#pragma unroll
+                        for (int b = 4; b < 32; b <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, b));
+                        const float rn = fmaxf(ml[n][c], x);
+                        l[n][c] *= (rn == -INFINITY) ? 1.f : ptx::ex2_approx(ml[n][c] - rn);
+                        ml[n][c] = rn;
+                    } else {
+                        l[n][c] *= al;
+                    }
 #pragma unroll
                     for (int i = 0; i < D / 16; ++i) { o[i][n][c] *= al; o[i][n][2 + c] *= al; }
                 }
@@ -385,9 +405,9 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
                 for (int h = 0; h < 2; ++h) {
                     const float p0 = ptx::ex2_approx(s[u][n][2 * h] - sub0), p1 = ptx::ex2_approx(s[u][n][2 * h + 1] - sub1);
                     if constexpr (E4M3) {
-                        l[n][0] = fmaf(p0, back[u][h], l[n][0]);
-                        l[n][1] = fmaf(p1, back[u][h], l[n][1]);
-                        pb[n][h] = pg_transpose(pack_f16x2(p0 * tiny[u][h], p1 * tiny[u][h]));
+                        l[n][0] += ptx::ex2_approx(r[u][n][2 * h] - ((ml[n][0] == -INFINITY) ? 0.f : ml[n][0]));
+                        l[n][1] += ptx::ex2_approx(r[u][n][2 * h + 1] - ((ml[n][1] == -INFINITY) ? 0.f : ml[n][1]));
+                        pb[n][h] = pg_transpose(pack_f16x2(p0, p1));
                     } else {
                         l[n][0] += p0;
                         l[n][1] += p1;
@@ -428,11 +448,11 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
 #pragma unroll
             for (int b = 4; b < 32; b <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], b);
     if constexpr (E4M3) asm volatile("cp.async.wait_all;" ::: "memory");
-    // the warps' results: rows of (maximum, sum) and of O each
+    // the warps' results: rows of (maximum, sum; e4m3: the sum's maximum) and of O each
     __syncthreads();
-    constexpr int kRows = Cfg::kRows, kLd = Cfg::kLd;
+    constexpr int kRows = Cfg::kRows, kLd = Cfg::kLd, kMl = Cfg::kMl;
     float* sm_o = reinterpret_cast<float*>(pgsm);                      // [warps][rows][kLd]
-    float* sm_ml = sm_o + kWarps * kRows * kLd;                        // [warps][rows][2]
+    float* sm_ml = sm_o + kWarps * kRows * kLd;                        // [warps][rows][kMl]
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -443,48 +463,56 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
                 if constexpr (E4M3) *reinterpret_cast<float2*>(r + i * 16 + 2 * l4) = make_float2(o[i][n][e], o[i][n][2 + e]);
                 else { r[i * 16 + l4] = o[i][n][e]; r[i * 16 + 8 + l4] = o[i][n][2 + e]; }
             }
-            if (l4 == 0) *reinterpret_cast<float2*>(sm_ml + (warp * kRows + n * 8 + c2 + e) * 2) = make_float2(m[n][e], l[n][e]);
+            if (l4 == 0) {
+                float* to = sm_ml + (warp * kRows + n * 8 + c2 + e) * kMl;
+                *reinterpret_cast<float2*>(to) = make_float2(m[n][e], l[n][e]);
+                if constexpr (E4M3) to[2] = ml[n][e];
+            }
         }
     __syncthreads();
-    constexpr float kUnit = E4M3 ? 20.f : 0.f, kInv = E4M3 ? 1.f / (1 << 20) : 1.f;      // of the sums, see `back`
-    auto write = [&](int g, int d, const float4& acc, float M, float L) {
-        const float inv = kInv / L;
+    // A row's O relative to 2^M, its sum relative to 2^ML (bf16: M and ML are one), of all warps (CTAs) so far: the next ones' added
+    struct Row { float M, ML, L; float4 acc; };
+    auto reference = [&](const float* x, Row& w) { w.M = fmaxf(w.M, x[0]); if constexpr (E4M3) w.ML = fmaxf(w.ML, x[2]); };
+    auto add = [&](const float* x, const float4& v, Row& w) {
+        const float f = (x[0] == -INFINITY) ? 0.f : ptx::ex2_approx(x[0] - w.M);
+        if constexpr (E4M3) w.L += (x[2] == -INFINITY) ? 0.f : x[1] * ptx::ex2_approx(x[2] - w.ML); else w.L += x[1] * f;
+        w.acc.x += v.x * f; w.acc.y += v.y * f; w.acc.z += v.z * f; w.acc.w += v.w * f;
+    };
+    auto write = [&](int g, int d, const Row& w) {
+        // (2^(M - ML) in two halves: it may be past 2^127 where what it multiplies is small)
+        const float half = E4M3 ? ptx::ex2_approx(0.5f * (w.M - w.ML)) : 1.f, inv = half / w.L;
+        const float4& acc = w.acc;
         const int64_t row = paged_row(a, t, t.x0 + g / heads);
         const int h = head0 + g % heads;
         if (!ksa_in_bounds(row >= 0 && row < a.rows && h < a.Hq, a.status)) return;
         *reinterpret_cast<uint2*>(a.out + row * a.o_st + h * a.o_sh + d) =
-            make_uint2(ptx::pack_bf16x2(acc.x * inv, acc.y * inv), ptx::pack_bf16x2(acc.z * inv, acc.w * inv));
-        if (d == 0) a.lse[(int64_t)h * a.rows + row] = (M + kUnit + log2f(L)) * 0.6931471805599453f;
+            make_uint2(ptx::pack_bf16x2(acc.x * inv * half, acc.y * inv * half), ptx::pack_bf16x2(acc.z * inv * half, acc.w * inv * half));
+        if (d == 0) a.lse[(int64_t)h * a.rows + row] = ((E4M3 ? w.ML : w.M) + log2f(w.L)) * 0.6931471805599453f;
     };
     // Each CTA of the cluster sums up a share of the output's elements (4 columns of a row each), `share` of them: the others
     // write what they have of these into its memory, where the one barrier finds everything.
     const int total = nrow * (D / 4), share = (total + parts - 1) / parts;
-    const uint32_t push_o = sbase + Cfg::kPushOff, push_ml = push_o + Cfg::kPushO;       // [parts][share] of 16 bytes, [parts][rows] of 8
+    const uint32_t push_o = sbase + Cfg::kPushOff, push_ml = push_o + Cfg::kPushO;       // [parts][share] of 16 bytes, [parts][rows][kMl] floats
     if (parts > 1) ptx::cluster_wait();                        // they have all started
     for (int idx = threadIdx.x; idx < total; idx += kThreads) {
         const int g = idx / (D / 4), d = (idx - g * (D / 4)) * 4;
-        float2 ml[kWarps];
-        float M = -INFINITY;
+        Row w{-INFINITY, -INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) { ml[w] = *reinterpret_cast<const float2*>(sm_ml + (w * kRows + g) * 2); M = fmaxf(M, ml[w].x); }
-        float L = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i = 0; i < kWarps; ++i) reference(sm_ml + (i * kRows + g) * kMl, w);
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const float f = (ml[w].x == -INFINITY) ? 0.f : ptx::ex2_approx(ml[w].x - M);
-            const float4 v = *reinterpret_cast<const float4*>(sm_o + (w * kRows + g) * kLd + d);
-            L += ml[w].y * f;
-            acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
-        }
+        for (int i = 0; i < kWarps; ++i) add(sm_ml + (i * kRows + g) * kMl, *reinterpret_cast<const float4*>(sm_o + (i * kRows + g) * kLd + d), w);
         if (parts == 1) {
-            write(g, d, acc, M, L);
+            write(g, d, w);
         } else {
             const int to = idx / share;
             asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};"
-                         ::"r"(ptx::mapa_shared(push_o + (split * share + idx - to * share) * 16, to)), "f"(acc.x), "f"(acc.y), "f"(acc.z), "f"(acc.w) : "memory");
+                         ::"r"(ptx::mapa_shared(push_o + (split * share + idx - to * share) * 16, to)), "f"(w.acc.x), "f"(w.acc.y), "f"(w.acc.z), "f"(w.acc.w) : "memory");
             if (d == 0)
-                for (int p = 0; p < parts; ++p)
-                    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(ptx::mapa_shared(push_ml + (split * kRows + g) * 8, p)), "f"(M), "f"(L) : "memory");
+                for (int p = 0; p < parts; ++p) {
+                    const uint32_t at = ptx::mapa_shared(push_ml + (split * kRows + g) * kMl * 4, p);
+                    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(w.M), "f"(w.L) : "memory");
+                    if constexpr (E4M3) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 8), "f"(w.ML) : "memory");
+                }
         }
     }
     if (parts > 1) {
@@ -492,21 +520,14 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
         ptx::cluster_arrive();
         ptx::cluster_wait();
         const float4* po = reinterpret_cast<const float4*>(pgsm + Cfg::kPushOff);
-        const float2* pm = reinterpret_cast<const float2*>(pgsm + Cfg::kPushOff + Cfg::kPushO);
+        const float* pm = reinterpret_cast<const float*>(pgsm + Cfg::kPushOff + Cfg::kPushO);
         for (int e = threadIdx.x; e < share && split * share + e < total; e += kThreads) {
             const int idx = split * share + e, g = idx / (D / 4), d = (idx - g * (D / 4)) * 4;
-            float M = -INFINITY, L = 0.f;
-            for (int p = 0; p < parts; ++p) M = fmaxf(M, pm[p * kRows + g].x);
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            Row w{-INFINITY, -INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+            for (int p = 0; p < parts; ++p) reference(pm + (p * kRows + g) * kMl, w);
 #pragma unroll 4
-            for (int p = 0; p < parts; ++p) {
-                const float2 ml = pm[p * kRows + g];
-                const float4 v = po[p * share + e];
-                const float f = (ml.x == -INFINITY) ? 0.f : ptx::ex2_approx(ml.x - M);
-                L += ml.y * f;
-                acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
-            }
-            write(g, d, acc, M, L);
+            for (int p = 0; p < parts; ++p) add(pm + (p * kRows + g) * kMl, po[p * share + e], w);
+            write(g, d, w);
         }
     }
 }

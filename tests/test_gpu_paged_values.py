@@ -1,0 +1,44 @@
+"""Paged attention of values at the ends of their range, against the definitions in 64 bits, by each of the two kernels: value rows
+from zeros to the largest scale, beside one another and out of one another's sight, queries of zeros, one key that outweighs
+thousands.  The bounds are those of paged_ref.check."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_24432_b200 import binding as ksa
+from tests.paged_check import Strict
+from tests.test_gpu_paged import DEV, FEW, MANY, _i32, ctx  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def _no_workspace(s, spans):
+    """The call over the e4m3 pages themselves."""
+    return s.attn(spans, workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
+
+
+def _size(rows, byte, seed=0):
+    """Rows whose e4m3 scale byte is `byte`: largest value 237 times the scale."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.rand(rows, generator=g, dtype=torch.float64) * 2 - 1
+    x[..., 0] = 1.0
+    return (x * 237.0 * 2.0 ** (byte - 127)).bfloat16()
+
+
+# ---- value rows of any size ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kernel,before,n", [(FEW, 300, 1), (FEW, 300, 5), (FEW, 2500, 5)])
+@pytest.mark.parametrize("byte", [30, 186, 234, 235, 240, 247])
+@pytest.mark.parametrize("where", ["alone", "beside", "zeros beside"])
+def test_value_rows_of_any_scale(ctx, kernel, before, n, byte, where):
+    s = Strict(ctx, 8, 1, 1 << 10, 8, 2, 128, 32, "e4m3", [before + n], seed=byte, flags=kernel)
+    v = s.val[0]
+    if where == "zeros beside":
+        v.zero_()
+    pick = slice(None) if where == "alone" else slice(None, None, 7)
+    v[pick] = _size(v[pick].shape, byte)
+    spans = [(before, n)]
+    s.fill(spans)
+    out, lse = _no_workspace(s, spans)
+    s.check(out, lse, spans, sample=6)
