@@ -678,17 +678,19 @@ class PagedCache:
             raise KsaError(status, name)
 
     def _workspace(self, p: bytes, stream):
-        """The workspace that makes the call faster, from torch's allocator (which keeps it until the work before its next use
-        on the stream is done, in a captured call as long as the graph lives), or None."""
+        """The workspace that makes the call faster, from torch's allocator, or None.  The block is asked for on the call's own stream:
+        the allocator gives what was freed on a stream to that stream's next request, in the order of its work (what was freed on
+        another stream may still be in use there), and keeps it in a captured call as long as the graph lives."""
         import torch
         n = ctypes.c_size_t()
         _check(lib().ksa_paged_workspace_bytes(p, ctypes.byref(n)), "ksa_paged_workspace_bytes")
         if n.value == 0:
             return None
-        ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
-        if stream is not None and stream != _current_stream(self.device):
-            ws.record_stream(torch.cuda.ExternalStream(stream, device=self.device))
-        return ws
+        if stream is None or stream == _current_stream(self.device):
+            return torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        on = torch.cuda.ExternalStream(stream, device=self.device) if stream else torch.cuda.default_stream(self.device)
+        with torch.cuda.stream(on):
+            return torch.empty(n.value, dtype=torch.uint8, device=self.device)
 
     def append(self, batch: PagedBatch, k, v, stream: Optional[int] = None):
         """ksa_paged_append: k, v [num_rows, Hkv, D] of the batch's new rows into their pages (quantised on the way)."""
