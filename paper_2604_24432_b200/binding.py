@@ -678,7 +678,8 @@ class PagedCache:
             raise KsaError(status, name)
 
     def _workspace(self, p: bytes, stream):
-        """The workspace that makes the call faster, from torch's allocator, or None.  The block is asked for on the call's own stream:
+        """The workspace that makes the call faster, from torch's allocator, or None (also where there is no memory for it: the call
+        works without).  The block is asked for on the call's own stream:
         the allocator gives what was freed on a stream to that stream's next request, in the order of its work (what was freed on
         another stream may still be in use there), and keeps it in a captured call as long as the graph lives."""
         import torch
@@ -686,11 +687,14 @@ class PagedCache:
         _check(lib().ksa_paged_workspace_bytes(p, ctypes.byref(n)), "ksa_paged_workspace_bytes")
         if n.value == 0:
             return None
-        if stream is None or stream == _current_stream(self.device):
-            return torch.empty(n.value, dtype=torch.uint8, device=self.device)
-        on = torch.cuda.ExternalStream(stream, device=self.device) if stream else torch.cuda.default_stream(self.device)
-        with torch.cuda.stream(on):
-            return torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        try:
+            if stream is None or stream == _current_stream(self.device):
+                return torch.empty(n.value, dtype=torch.uint8, device=self.device)
+            on = torch.cuda.ExternalStream(stream, device=self.device) if stream else torch.cuda.default_stream(self.device)
+            with torch.cuda.stream(on):
+                return torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        except torch.OutOfMemoryError:
+            return None
 
     def append(self, batch: PagedBatch, k, v, stream: Optional[int] = None):
         """ksa_paged_append: k, v [num_rows, Hkv, D] of the batch's new rows into their pages (quantised on the way)."""

@@ -36,8 +36,10 @@ class Allocator:
     @contextlib.contextmanager
     def stream(self, s):
         before, self.on = self.on, s
-        yield
-        self.on = before
+        try:
+            yield
+        finally:
+            self.on = before
 
     def empty(self, n, **kw):
         self.asked.append(self.on)
@@ -55,6 +57,16 @@ def test_block_is_asked_for_on_the_calls_stream(monkeypatch, current, stream, wa
     mem = Allocator(monkeypatch, current)
     assert _cache()._workspace(_params(), stream) is not None
     assert mem.asked == [want] and mem.on == current
+
+
+@pytest.mark.parametrize("stream", [None, 9])
+def test_no_memory_means_no_workspace(monkeypatch, stream):
+    mem = Allocator(monkeypatch, 7)
+
+    def full(n, **kw):
+        raise torch.OutOfMemoryError("no room")
+    monkeypatch.setattr(torch, "empty", full)
+    assert _cache()._workspace(_params(), stream) is None and mem.on == 7
 
 
 @pytest.mark.gpu
