@@ -292,7 +292,7 @@ static UnpackLayout unpack_layout(const ksa_paged_params* p)
     const int64_t G = p->num_q_heads / p->num_kv_heads;
     // From 1,024 query rows (four tiles of 256) a sequence on: the tcgen05 kernel converts a key tile once for each of them.  256 rows over
     // 36,864, 32/8 heads: 65 us without the copy, 59 with it; 128 rows: 43 and 46; 1,152: 122 and 89.
-    if (p->kv_format != KSA_KV_E4M3 || p->num_rows * G < 1024 * (int64_t)p->batch) return l;
+    if (p->kv_format != KSA_KV_E4M3 || p->num_rows * G < 1024 * (int64_t)p->batch || (p->flags & KSA_FLAG_PAGED_MMA_SYNC)) return l;
     const int64_t text = (int64_t)p->text_cols * p->page_rows, summ = p->summaries_per_chunk > 0 ? (int64_t)p->summ_cols * p->page_rows : 0;
     l.text_cols = (text + 127) / 128; l.summ_cols = (summ + 127) / 128;
     const int64_t seen = ((int64_t)p->window_chunks + 2) * p->chunk_len + p->num_rows;        // text tokens in view, at most

@@ -22,6 +22,16 @@ def _params(**change):
     return bytes(ksa.ksa_paged_params(**{**good, **change}))
 
 
+def _need(**change):
+    n = ctypes.c_size_t()
+    assert ksa.lib().ksa_paged_workspace_bytes(_params(**change), ctypes.byref(n)) == 0
+    return n.value
+
+
+def test_a_call_held_to_mma_sync_wants_none():
+    assert _need() > 0 and _need(flags=ksa.KSA_FLAG_PAGED_TCGEN05) == _need() and _need(flags=ksa.KSA_FLAG_PAGED_MMA_SYNC) == 0
+
+
 class Allocator:
     """torch.empty and the streams, recorded: `asked` is the stream of each request."""
 
