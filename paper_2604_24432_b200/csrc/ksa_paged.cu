@@ -351,6 +351,11 @@ static int validate_shape(const ksa_paged_params* p)
     if (p->page_rows != 16 && p->page_rows != 32 && p->page_rows != 64 && p->page_rows != 128) return KSA_ERR_UNSUPPORTED;
     if (p->num_q_heads / p->num_kv_heads > 64 || p->num_q_heads > 1024 || p->batch > 65535 || p->num_rows > (1 << 24)) return KSA_ERR_UNSUPPORTED;
     if ((int64_t)p->chunk_len + p->summaries_per_chunk > (1 << 30)) return KSA_ERR_UNSUPPORTED;
+    return KSA_OK;
+}
+
+static int validate_pool_strides(const ksa_paged_params* p)
+{
     const int64_t unit = p->kv_format == KSA_KV_BF16 ? 8 : 16;              // 16 bytes
     auto stride_of = [&](int64_t st) { return st <= 0 || st % unit != 0 ? KSA_ERR_INVALID_ARG : st >= (1ll << 38) ? KSA_ERR_UNSUPPORTED : KSA_OK; };
     int rc = p->row_stride < p->head_dim ? KSA_ERR_INVALID_ARG : stride_of(p->row_stride);
@@ -361,7 +366,8 @@ static int validate_shape(const ksa_paged_params* p)
 
 static int validate_paged(const ksa_paged_params* p, const ksa_paged_kv* kv)
 {
-    const int rc = validate_shape(p);
+    int rc = validate_shape(p);
+    if (rc == KSA_OK) rc = validate_pool_strides(p);
     if (rc != KSA_OK) return rc;
     if (!kv) return KSA_ERR_INVALID_ARG;
     auto misaligned = [](const void* q) { return ((uintptr_t)q & 15) != 0; };

@@ -32,6 +32,10 @@ def test_a_call_held_to_mma_sync_wants_none():
     assert _need() > 0 and _need(flags=ksa.KSA_FLAG_PAGED_TCGEN05) == _need() and _need(flags=ksa.KSA_FLAG_PAGED_MMA_SYNC) == 0
 
 
+def test_strides_do_not_matter_to_its_size():
+    assert _need(page_stride=0, head_stride=0, row_stride=0) == _need(page_stride=-8, head_stride=3, row_stride=1) == _need()
+
+
 class Allocator:
     """torch.empty and the streams, recorded: `asked` is the stream of each request."""
 
