@@ -473,7 +473,9 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
         }
         if (u < nh) {
             const PagedView see = paged_view(a, is_summ, x);
-            const float scale_log2 = E4M3 ? a.scale_log2 * q_back : a.scale_log2;
+            // (a normal number: a query of zeros over small keys would make it 0, and what is masked is -inf before it is scaled; scores
+            // that it multiplies stay next to 0, or far apart, all the same)
+            const float scale_log2 = E4M3 ? fminf(fmaxf(a.scale_log2 * q_back, 0x1p-126f), 0x1.fffffep127f) : a.scale_log2;
             uint32_t sf_phase = 0, pv_phase = 0;
             int rel_k = 0, rel_v = 0;                        // the stages handed back next, by the last query tile's first thread
             const bool releaser = (tid & 127) == 0 && u == nh - 1;

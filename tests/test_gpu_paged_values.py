@@ -42,3 +42,19 @@ def test_value_rows_of_any_scale(ctx, kernel, before, n, byte, where):
     s.fill(spans)
     out, lse = _no_workspace(s, spans)
     s.check(out, lse, spans, sample=6)
+
+
+# ---- queries of zeros -----------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kernel,before,n", [(FEW, 300, 5), (MANY, 300, 40), (MANY, 2500, 40)])
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("keys", [0.0, 1e-3, 1.0])
+@pytest.mark.parametrize("q", [0.0, 1e-30])
+def test_small_queries_and_keys(ctx, kernel, before, n, fmt, keys, q):
+    """Every second query of zeros or next to nothing, over keys of zeros, small and ordinary ones."""
+    s = Strict(ctx, 8, 1, 1 << 10, 8, 2, 128, 32, fmt, [before + n], seed=2, flags=kernel)
+    s.q[0][::2] = (s.q[0][::2].double() * q).bfloat16()
+    s.key[0] = (s.key[0].double() * keys).bfloat16()
+    spans = [(before, n)]
+    s.fill(spans)
+    out, lse = _no_workspace(s, spans)
+    s.check(out, lse, spans, sample=10)
