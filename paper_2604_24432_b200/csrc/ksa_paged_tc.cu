@@ -20,7 +20,8 @@
 // times the instructions, and the converting warps set the pace: 1.6 ms for the last 4,608 of 147,456 rows, 32/4 heads).  A row's
 // scale is taken relative to the largest among the rows in view, which is found first: values are at most 448 * 2^7, and what
 // underflows is below 2^-39 of the largest.  An e4m3 value has four significant bits, so rows whose scale is up to 2^28 smaller than
-// the largest keep theirs.  Q becomes f16 by a power of two for each row; P as f16 is rounded eight times finer than as bf16.
+// the largest keep theirs.  Q becomes f16 by a power of two for each row; P as f16 is rounded eight times finer than as bf16, down to
+// 2^-25 of the row's largest (see PtScale).
 //
 // Rows of a page that nothing in the tile sees may hold anything.  Scores of such keys are replaced by -inf; their V rows
 // are overwritten with zeros in shared memory (0 * NaN would reach the accumulators): by warp 10 in the tiles that hold an end
@@ -46,8 +47,12 @@ namespace ksa {
 using namespace ptx;
 
 constexpr int kPtTile = 128;
-// log2 units: P stays below 2^12 (see ksa_text_tc.cu)
-constexpr float kPtRescale = 12.0f;
+// log2 units: by how much a score may outgrow the reference maximum before that moves, and what P stands above 2^(score - reference).
+// bf16: P stays below 2^12 (see ksa_text_tc.cu).  f16 ends with 65,504 and loses bits below 2^-14, so P stays below 2^15 there, and as
+// close to it as can be: it keeps 11 bits down to 2^-25 of the largest, and is 0 below 2^-36 of it.  (From 1 downwards, keys 18
+// natural-log units below a single one in the same CTA's share came out as nothing.  900 rows over 36,864, 4/4 heads of 64:
+// 32.7 and 32.9 us; 200 rows, 32/8 of 128: 65.2 and 66.3.)
+template <bool E4M3> struct PtScale { static constexpr float kRescale = E4M3 ? 4.0f : 12.0f, kLift = E4M3 ? 11.0f : 0.0f; };
 
 template <int D, bool E4M3>
 struct PtCfg {
@@ -530,7 +535,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                 mx1 = fmax3(mx1, __uint_as_float(s[126]), __uint_as_float(s[127]));
                 const float mx_sc = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * scale_log2;
                 // lazy rescale: the reference max only moves when some row of the warp outgrew it
-                const bool need_any = __any_sync(0xffffffffu, mx_sc > m_used + kPtRescale);
+                const bool need_any = __any_sync(0xffffffffu, mx_sc > m_used + PtScale<E4M3>::kRescale);
                 float alpha = 1.f;
                 if (need_any) {
                     const float m_new = fmaxf(m_used, mx_sc);
@@ -538,7 +543,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                     m_used = m_new;
                     l_run *= alpha;
                 }
-                const float neg_m = (m_used == -INFINITY) ? 0.f : -m_used;
+                const float neg_m = (m_used == -INFINITY) ? 0.f : PtScale<E4M3>::kLift - m_used;
                 const float2 sc2 = make_float2(scale_log2, scale_log2);
                 const float2 nm2 = make_float2(neg_m, neg_m);
                 bool pv_ok = false;                           // the product before is known to be done
@@ -619,7 +624,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                         if (at >= 0) *reinterpret_cast<uint4*>(a.out + at + c * 32 + (lane & 3) * 8) = pk[e];
                     }
                 }
-                if (store) a.lse[(int64_t)head * a.rows + prow] = (m_used + log2f(l_run)) * 0.6931471805599453f;
+                if (store) a.lse[(int64_t)head * a.rows + prow] = (m_used - PtScale<E4M3>::kLift + log2f(l_run)) * 0.6931471805599453f;
                 tc_fence_before();
             }
         } else {
@@ -698,7 +703,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                     if (off < 0) continue;
                     const float inv = 1.f / L[r];
                     *reinterpret_cast<uint2*>(a.out + off + c4 * 4) = make_uint2(pack_bf16x2(acc[r].x * inv, acc[r].y * inv), pack_bf16x2(acc[r].z * inv, acc[r].w * inv));
-                    if (c4 == 0) a.lse[lse] = (M[r] + log2f(L[r])) * 0.6931471805599453f;
+                    if (c4 == 0) a.lse[lse] = (M[r] - PtScale<E4M3>::kLift + log2f(L[r])) * 0.6931471805599453f;
                 }
             }
             __syncwarp();

@@ -58,3 +58,23 @@ def test_small_queries_and_keys(ctx, kernel, before, n, fmt, keys, q):
     s.fill(spans)
     out, lse = _no_workspace(s, spans)
     s.check(out, lse, spans, sample=10)
+
+
+# ---- one key that outweighs thousands --------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kernel,n,ws", [(FEW, 1, False), (FEW, 4, False), (MANY, 70, False), (MANY, 70, True)])
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("gap,sink", [(8, 0.0), (16, 0.0), (16, 2.0 ** -6), (18, 0.0), (18, 2.0 ** -6)])
+def test_one_key_that_outweighs_the_others(ctx, kernel, n, ws, fmt, gap, sink):
+    """An attention sink: a first key whose score stands `gap` above those of 3,000 others, with a value row of zeros or a small one.
+    ws: with the workspace, where the call takes one."""
+    before = 3000
+    s = Strict(ctx, 8, 0, 1 << 20, 16, 1, 128, 64, fmt, [before + n], seed=7, flags=kernel)
+    s.q[0].fill_(1.0)
+    s.key[0].zero_()
+    s.key[0][0] = gap / math.sqrt(128.0)
+    s.val[0].abs_()
+    s.val[0][0] *= sink
+    spans = [(before, n)]
+    s.fill(spans)
+    out, lse = s.attn(spans) if ws else _no_workspace(s, spans)
+    s.check(out, lse, spans, sample=3)
