@@ -631,6 +631,14 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
             // ---- partial results into shared memory, summed up over the cluster, a share of the rows by each CTA ----
             pt_named_barrier(1, 256);                         // both query tiles' products have read their K, V and Q
             const uint32_t part_o = smem_base, part_ml = smem_base + Cfg::kPartMl, part_to = part_ml + 256 * 8;
+            // e4m3: O / sum / 8, and the sum in the maximum's place, as log2: times V's scale O itself may be beyond fp32 (whose
+            // largest is 1.4 times that of the format's values), and so may a sum of several CTAs' O / sum
+            float part_m = m_used, part_l = l_run, part_f = 1.f;
+            if constexpr (E4M3) {
+                part_f = (l_run == 0.f) ? 0.f : v_back * (0.125f / l_run);
+                part_m = (l_run == 0.f) ? -INFINITY : m_used + log2f(l_run);
+                part_l = (l_run == 0.f) ? 0.f : 1.f;
+            }
             if (tokens > 0) {
                 const uint32_t d = part_o + (uint32_t)((u * 128 + row) * D * 4);
 #pragma unroll
@@ -640,7 +648,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                         tmem_ld32(tO + c * 32, o);
                         tc_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) if (E4M3) o[e] = __float_as_uint(__uint_as_float(o[e]) * v_back);
+                        for (int e = 0; e < 32; ++e) if (E4M3) o[e] = __float_as_uint(__uint_as_float(o[e]) * part_f);
                     } else {
 #pragma unroll
                         for (int e = 0; e < 32; ++e) o[e] = 0u;
@@ -649,7 +657,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                     for (int e = 0; e < 8; ++e)               // (neighbouring rows on different banks)
                         pt_st_shared4(d + (uint32_t)((c * 8 + (e ^ (row & 7))) * 16), o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
                 }
-                asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(part_ml + (u * 128 + row) * 8), "f"(m_used), "f"(l_run) : "memory");
+                asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(part_ml + (u * 128 + row) * 8), "f"(part_m), "f"(part_l) : "memory");
                 const bool store = valid && ksa_in_bounds(prow >= 0 && prow < a.rows && head < a.Hq, a.status);
                 const uint64_t off = store ? (uint64_t)(prow * a.o_st + (int64_t)head * a.o_sh) : ~0ull, lse = (uint64_t)((int64_t)head * a.rows + prow);
                 pt_st_shared4(part_to + (u * 128 + row) * 16, (uint32_t)off, (uint32_t)(off >> 32), (uint32_t)lse, (uint32_t)(lse >> 32));
@@ -701,7 +709,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                     const uint4 to = pt_ld_shared4(part_to + pr[r] * 16);             // where the row's output and LSE go
                     const int64_t off = (int64_t)((uint64_t)to.y << 32 | to.x), lse = (int64_t)((uint64_t)to.w << 32 | to.z);
                     if (off < 0) continue;
-                    const float inv = 1.f / L[r];
+                    const float inv = (E4M3 ? 8.f : 1.f) / L[r];
                     *reinterpret_cast<uint2*>(a.out + off + c4 * 4) = make_uint2(pack_bf16x2(acc[r].x * inv, acc[r].y * inv), pack_bf16x2(acc[r].z * inv, acc[r].w * inv));
                     if (c4 == 0) a.lse[lse] = (M[r] - PtScale<E4M3>::kLift + log2f(L[r])) * 0.6931471805599453f;
                 }

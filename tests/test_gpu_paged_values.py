@@ -28,7 +28,7 @@ def _size(rows, byte, seed=0):
 
 
 # ---- value rows of any size ------------------------------------------------------------------------------------------------
-@pytest.mark.parametrize("kernel,before,n", [(FEW, 300, 1), (FEW, 300, 5), (FEW, 2500, 5)])
+@pytest.mark.parametrize("kernel,before,n", [(FEW, 300, 1), (FEW, 300, 5), (FEW, 2500, 5), (MANY, 300, 40), (MANY, 2500, 40)])
 @pytest.mark.parametrize("byte", [30, 186, 234, 235, 240, 247])
 @pytest.mark.parametrize("where", ["alone", "beside", "zeros beside"])
 def test_value_rows_of_any_scale(ctx, kernel, before, n, byte, where):
