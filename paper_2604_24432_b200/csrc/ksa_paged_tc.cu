@@ -16,12 +16,13 @@
 // TMEM: one score slot S [0,128) that the two query tiles take in turns, the bf16 probabilities P0 [128,192), P1 [192,256),
 // O0 [256,256+D), O1 [384,384+D).  The pipeline over the key tiles is that of the text-row kernel (ksa_text_tc.cu).
 //
-// e4m3 pages: all products are of f16 (one conversion for two values, one multiplication for their scale; as bf16 it took three
-// times the instructions, and the converting warps set the pace: 1.6 ms for the last 4,608 of 147,456 rows, 32/4 heads).  A row's
-// scale is taken relative to the largest among the rows in view, which is found first: values are at most 448 * 2^7, and what
-// underflows is below 2^-39 of the largest.  An e4m3 value has four significant bits, so rows whose scale is up to 2^28 smaller than
-// the largest keep theirs.  Q becomes f16 by a power of two for each row; P as f16 is rounded eight times finer than as bf16, down to
-// 2^-25 of the row's largest (see PtScale).
+// e4m3 pages: the products are of f16 (one conversion for two values, one multiplication for their scale; as bf16 it takes three
+// times the instructions, and the converting warps set the pace).  A row's scale is taken relative to the largest among the rows in
+// view, which is found first: values are at most 448 * 2^7, and what underflows is below 2^-39 of the largest.  An e4m3 value has
+// four significant bits, so rows whose scale is up to 2^28 smaller than the largest keep theirs.  Q becomes f16 by a power of two for
+// each row; P as f16 is rounded eight times finer than as bf16, down to 2^-25 of the row's largest (see PtScale).  Where the scales in
+// a CTA's view are further apart than that leaves room for (see PtTops), the same products are of bf16, which has the range: 200 rows
+// over 36,864, 32/8 heads of 128: 65.7 and 79.6 us.
 //
 // Rows of a page that nothing in the tile sees may hold anything.  Scores of such keys are replaced by -inf; their V rows
 // are overwritten with zeros in shared memory (0 * NaN would reach the accumulators): by warp 10 in the tiles that hold an end
@@ -36,6 +37,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "ksa_launch.h"
 #include "ksa_paged.h"
@@ -109,6 +111,22 @@ __device__ __forceinline__ float2 pt_ld_cluster2(uint32_t addr)
     return v;
 }
 
+// e4m3: the largest scale bytes of K and of V among the rows in view, and whether the products are of bf16.  f16 has room for keys whose
+// scale is up to 2^28 smaller than the largest (which other rows of the query tile may be the only ones to see).  A value row's share
+// of the output is its probability times its scale, and P keeps bits down to 2^-25, so there it is 2^10, rows of zeros counted
+// as the smallest (an attention sink of zeros leaves the output to probabilities of any size).
+struct PtTops { uint32_t k, v; bool wide; };
+__device__ __forceinline__ PtTops pt_tops(uint32_t at)
+{
+    uint32_t top[2] = {0u, 0u}, low[2] = {255u, 255u};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {                              // by converting warp: K, V; largest, smallest
+        const uint32_t w = ld_shared_u32(at + 4 * i);
+        top[i & 1] = max(top[i & 1], w & 255u); low[i & 1] = min(low[i & 1], w >> 8);
+    }
+    return PtTops{top[0], top[1], (int)top[0] - (int)low[0] > 28 || (int)top[1] - (int)low[1] > 10};
+}
+
 template <int D, bool E4M3>
 __global__ void __launch_bounds__(PtCfg<D, E4M3>::kThreads, 1)
 ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedMaps maps)
@@ -120,7 +138,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
     const uint32_t bars = smem_base + Cfg::kBarOff;
     const uint32_t tmem_slot = bars + 8 * Cfg::kNumBars;
     const uint32_t abort_addr = tmem_slot + 4;                 // (two words)
-    const uint32_t tops = tmem_slot + 16;                       // e4m3: the largest scale bytes of K and of V, by converting warp
+    const uint32_t tops = tmem_slot + 16;                       // e4m3: the largest and smallest scale bytes of K and of V, by converting warp
     auto bar = [&](int i) -> uint32_t { return bars + 8u * (uint32_t)i; };
 
     const int tid = threadIdx.x;
@@ -174,8 +192,9 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
             bool alive = true;
             int k_stage = 0, v_stage = 0, raw = 0;
             uint32_t k_phase = 0, v_phase = 0, raw_phase = 0;
-            // the largest scales of K and of V among the rows in view: 16 rows at a time
-            uint32_t top_k = 0, top_v = 0;
+            // the largest and the smallest scales of K and of V among the rows in view (rows of NaN and, of K, of zeros aside: the latter's
+            // scores are 0 in any form): 16 rows at a time
+            uint32_t top_k = 0, top_v = 0, low_k = ~0u, low_v = ~0u;
             for (int i = row; i < T * (kPtTile / 16); i += 128) {
                 const auto tile = w.at(w.j0 + i / (kPtTile / 16));
                 const int x = tile.x0 + i % (kPtTile / 16) * 16;
@@ -185,28 +204,30 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                 const int64_t at = (((int64_t)page * a.Hkv + hk) << a.page_shift) + (x & ((1 << a.page_shift) - 1));
                 const uint4 k = __ldcg(reinterpret_cast<const uint4*>(a.ke + at)), v = __ldcg(reinterpret_cast<const uint4*>(a.ve + at));
                 const uint32_t kw[4] = {k.x, k.y, k.z, k.w}, vw[4] = {v.x, v.y, v.z, v.w};
-                uint32_t mk = 0, mv = 0;
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     uint32_t in = 0u;                          // rows in view
 #pragma unroll
                     for (int e = 0; e < 4; ++e) in |= tile.sees(x + 4 * c + e) ? 0xffu << (8 * e) : 0u;
-                    mk = __vmaxu4(mk, kw[c] & in & ~__vcmpeq4(kw[c], 0xffffffffu));       // (255: a row of NaN)
-                    mv = __vmaxu4(mv, vw[c] & in & ~__vcmpeq4(vw[c], 0xffffffffu));
+                    const uint32_t ik = in & ~__vcmpeq4(kw[c], 0xffffffffu), iv = in & ~__vcmpeq4(vw[c], 0xffffffffu);
+                    top_k = __vmaxu4(top_k, kw[c] & ik); top_v = __vmaxu4(top_v, vw[c] & iv);
+                    low_k = __vminu4(low_k, kw[c] | ~ik | __vcmpleu4(kw[c], 0x11111111u)); low_v = __vminu4(low_v, vw[c] | ~iv);
                 }
-                mk = __vmaxu2(mk >> 8 & 0x00ff00ffu, mk & 0x00ff00ffu); mv = __vmaxu2(mv >> 8 & 0x00ff00ffu, mv & 0x00ff00ffu);
-                top_k = max(top_k, max(mk >> 16, mk & 0xffffu)); top_v = max(top_v, max(mv >> 16, mv & 0xffffu));
             }
-            top_k = __reduce_max_sync(0xffffffffu, top_k);
-            top_v = __reduce_max_sync(0xffffffffu, top_v);
-            if (lane == 0) { st_shared_u32(tops + 8 * (warp - 12), top_k); st_shared_u32(tops + 8 * (warp - 12) + 4, top_v); }
-            pt_named_barrier(2, 384);                          // with the softmax warps, who need them too
-            top_k = top_v = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { top_k = max(top_k, ld_shared_u32(tops + 8 * i)); top_v = max(top_v, ld_shared_u32(tops + 8 * i + 4)); }
-            // 2^(e - top + 7) as f16, twice; 255: NaN
-            auto factor = [](uint32_t e, uint32_t top) {
-                const int p = (int)e - (int)top + 7;
+            auto publish = [&](uint32_t top, uint32_t low, uint32_t to) {
+                top = __vmaxu2(top >> 8 & 0x00ff00ffu, top & 0x00ff00ffu); low = __vminu2(low >> 8 & 0x00ff00ffu, low & 0x00ff00ffu);
+                top = __reduce_max_sync(0xffffffffu, max(top >> 16, top & 0xffffu));
+                low = __reduce_min_sync(0xffffffffu, min(low >> 16, low & 0xffffu));
+                if (lane == 0) st_shared_u32(to, top | low << 8);
+            };
+            publish(top_k, low_k, tops + 8 * (warp - 12));
+            publish(top_v, low_v, tops + 8 * (warp - 12) + 4);
+            pt_named_barrier(2, 448);                          // with the softmax and the MMA warps, who need them too
+            const PtTops top = pt_tops(tops);
+            // 2^(e - top + 7), as f16 twice or (for bf16) as fp32; 255: NaN
+            auto factor = [&](uint32_t e, uint32_t largest) {
+                const int p = (int)e - (int)largest + 7;
+                if (top.wide) return e == 255u ? 0x7fc00000u : p >= -126 ? (uint32_t)(p + 127) << 23 : 0u;
                 const uint32_t h = e == 255u ? 0x7e00u : p >= -14 ? (uint32_t)(p + 15) << 10 : p >= -24 ? 1u << (p + 24) : 0u;
                 return h | h << 16;
             };
@@ -220,8 +241,8 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                 const int page = paged_page(a, t.b, tile.summ, x);
                 if (page < 0) return;
                 const int64_t at = (((int64_t)page * a.Hkv + hk) << a.page_shift) + (x & ((1 << a.page_shift) - 1));
-                fk = factor(__ldcg(a.ke + at), top_k);
-                fv = factor(__ldcg(a.ve + at), top_v);
+                fk = factor(__ldcg(a.ke + at), top.k);
+                fv = factor(__ldcg(a.ve + at), top.v);
             };
             auto convert = [&](uint32_t full, uint32_t empty, uint32_t empty_parity, uint32_t dst, uint32_t f) {
                 if (alive) alive = __all_sync(0xffffffffu, bounded_wait(bar(Cfg::kRawFull + raw), raw_phase, abort_addr, a.status, kStatusWaitKvFull));
@@ -236,6 +257,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                 const int half = D == 128 ? (lane >> 3 & 1) ^ (lane >> 2 & 1) : 0, c = lane & 3;
                 const uint32_t at = src + r0 * D + half * 64 + c * 16, to = dst + half * 16384 + ((row & 96) + r0) * 128;
                 const bool all = __all_sync(0xffffffffu, f != 0xffffffffu);
+                auto rows = [&](auto wide) {
 #pragma unroll
                 for (int i = 0; i < 32 / kStep; ++i) {
                     const uint4 y = pt_ld_shared4(at + i * kStep * D);
@@ -244,8 +266,14 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                     uint32_t z[8];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        e4m3x4_to_f16(yw[e], z[2 * e], z[2 * e + 1]);
-                        z[2 * e] = mul_f16x2(z[2 * e], g); z[2 * e + 1] = mul_f16x2(z[2 * e + 1], g);
+                        if constexpr (wide) {
+                            const float2 p = e4m3x2_to_f32(yw[e] & 0xffffu), q = e4m3x2_to_f32(yw[e] >> 16);
+                            const float f32 = __uint_as_float(g);
+                            z[2 * e] = pack_bf16x2(p.x * f32, p.y * f32); z[2 * e + 1] = pack_bf16x2(q.x * f32, q.y * f32);
+                        } else {
+                            e4m3x4_to_f16(yw[e], z[2 * e], z[2 * e + 1]);
+                            z[2 * e] = mul_f16x2(z[2 * e], g); z[2 * e + 1] = mul_f16x2(z[2 * e + 1], g);
+                        }
                     }
                     if (!all && g == 0xffffffffu) {                 // nobody sees the row: it may hold anything
 #pragma unroll
@@ -255,6 +283,8 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                     pt_st_shared4(to + i * kStep * 128 + (((c * 2) ^ x) << 4), z[0], z[1], z[2], z[3]);
                     pt_st_shared4(to + i * kStep * 128 + (((c * 2 + 1) ^ x) << 4), z[4], z[5], z[6], z[7]);
                 }
+                };
+                if (top.wide) rows(std::true_type{}); else rows(std::false_type{});
                 fence_proxy_async();
                 __syncwarp();
                 if (lane == 0) { mbar_arrive(full); mbar_arrive(bar(Cfg::kRawEmpty + raw)); }
@@ -342,13 +372,15 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
             constexpr uint32_t hi = smem_desc_hi_sw128(1024);
             const uint32_t leader = elect_one();
             const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+            bool bf16 = !E4M3;
+            if constexpr (E4M3) { pt_named_barrier(2, 448); bf16 = __all_sync(0xffffffffu, pt_tops(tops).wide); }
             bool alive = true;
             auto wait = [&](uint32_t b, uint32_t parity, int code) {
                 if (alive) alive = __all_sync(0xffffffffu, bounded_wait(b, parity, abort_addr, a.status, code));
             };
             uint32_t stage = 0, ring_phase = 0, phase0 = 0, phase1 = 0;
             if (warp == 9) {
-                constexpr uint32_t idesc = E4M3 ? make_idesc_f16(128, 128, false) : make_idesc_bf16(128, 128, false);
+                const uint32_t idesc = bf16 ? make_idesc_bf16(128, 128, false) : make_idesc_f16(128, 128, false);
                 const uint32_t q_lo = smem_desc_lo(sQ, 16), k_lo = smem_desc_lo(sK, 16);
                 int before = -1;                            // query tile whose scores stand in the slot
                 for (int j = 0; j < T && alive; ++j) {
@@ -374,7 +406,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                     if (++stage == (uint32_t)Cfg::kStagesK) { stage = 0; ring_phase ^= 1u; }
                 }
             } else {
-                constexpr uint32_t idesc = E4M3 ? make_idesc_f16(128, D, true) : make_idesc_bf16(128, D, true);
+                const uint32_t idesc = bf16 ? make_idesc_bf16(128, D, true) : make_idesc_f16(128, D, true);
                 const uint32_t v_lo = smem_desc_lo(sV, 16384);   // MN-major: 64-column panels 16 KB apart, groups of 8 keys 1 KB
                 for (int j = 0; j < T && alive; ++j) {
                     wait(bar(Cfg::kVFull) + 8u * stage, ring_phase, kStatusWaitKvFull);
@@ -433,48 +465,52 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
         const bool valid = row < nrow;
         bool alive = true;
         float q_back = 1.f, v_back = 1.f;                                      // e4m3: what the scores and O are to be multiplied with
+        // ---- Q: a warp's 32 rows, K-major with 128-byte swizzle; D / 8 lanes bring a row (a row per thread took 4.4 us of a
+        // CTA's 11.7 with one key tile) ----
+        constexpr int kLanesQ = D / 8, kRowsPassQ = 32 / kLanesQ;
+        const int qc = lane % kLanesQ, qr0 = lane / kLanesQ;
+        uint4 y[kLanesQ];
         if (u < nh) {
-            // ---- Q: a warp's 32 rows, K-major with 128-byte swizzle; D / 8 lanes bring a row (a row per thread took 4.4 us of a
-            // CTA's 11.7 with one key tile) ----
-            {
-                constexpr int kLanes = D / 8, kRowsPass = 32 / kLanes;
-                const int64_t off = prow * a.q_st + head * a.q_sh;
-                const int c = lane % kLanes, r0 = lane / kLanes;
-                uint4 y[kLanes];
+            const int64_t off = prow * a.q_st + head * a.q_sh;
 #pragma unroll
-                for (int i = 0; i < kLanes; ++i)
-                    y[i] = __ldcg(reinterpret_cast<const uint4*>(a.q + __shfl_sync(0xffffffffu, off, i * kRowsPass + r0) + c * 8));
-                if constexpr (E4M3) {                        // as f16, the row's largest value taken to 2^8 or more (below 2^9)
-#pragma unroll
-                    for (int i = 0; i < kLanes; ++i) {
-                        uint32_t top = __vmaxu2(__vmaxu2(y[i].x & 0x7fff7fffu, y[i].y & 0x7fff7fffu), __vmaxu2(y[i].z & 0x7fff7fffu, y[i].w & 0x7fff7fffu));
-#pragma unroll
-                        for (int o = kLanes / 2; o > 0; o >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
-                        const int e = min(max((int)(max(top >> 16, top & 0xffffu) >> 7) - 8, 1), 253);
-                        const float f = __uint_as_float((uint32_t)(254 - e) << 23);
-                        auto two = [&](uint32_t& z) { z = pack_f16x2(__uint_as_float(z << 16) * f, __uint_as_float(z & 0xffff0000u) * f); };
-                        two(y[i].x); two(y[i].y); two(y[i].z); two(y[i].w);
-                        const int mine = __shfl_sync(0xffffffffu, e, lane % kRowsPass * kLanes);
-                        if (lane / kRowsPass == i) q_back = __uint_as_float((uint32_t)mine << 23);      // (of this thread's own row)
-                    }
-                }
-                const uint32_t d = sQ + u * Cfg::kTileBytes + (c >> 3) * 16384 + (row & 96) * 128;
-#pragma unroll
-                for (int i = 0; i < kLanes; ++i) {
-                    const int r = i * kRowsPass + r0;
-                    pt_st_shared4(d + r * 128 + (((c ^ r) & 7) << 4), y[i].x, y[i].y, y[i].z, y[i].w);
-                }
-                fence_proxy_async();
-                mbar_arrive(bar(Cfg::kQFull + u));
-            }
+            for (int i = 0; i < kLanesQ; ++i)
+                y[i] = __ldcg(reinterpret_cast<const uint4*>(a.q + __shfl_sync(0xffffffffu, off, i * kRowsPassQ + qr0) + qc * 8));
         }
+        bool wide = false;                                   // e4m3: the products are of bf16
         if constexpr (E4M3) {
-            pt_named_barrier(2, 384);                        // the largest scales are known
-            uint32_t top_k = 0, top_v = 0;
+            pt_named_barrier(2, 448);                        // the largest scales are known
+            const PtTops top = pt_tops(tops);
+            wide = __all_sync(0xffffffffu, top.wide);
+            q_back = e8m0_factor(top.k) * 0.0078125f;        // (K and V stand 2^7 times larger)
+            v_back = e8m0_factor(top.v) * 0.0078125f;
+        }
+        if (u < nh) {
+            if constexpr (E4M3) {                            // the row's largest value taken to 2^8 or more (below 2^9)
+                const float back = q_back;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { top_k = max(top_k, ld_shared_u32(tops + 8 * i)); top_v = max(top_v, ld_shared_u32(tops + 8 * i + 4)); }
-            q_back *= e8m0_factor(top_k) * 0.0078125f;       // (K and V stand 2^7 times larger)
-            v_back = e8m0_factor(top_v) * 0.0078125f;
+                for (int i = 0; i < kLanesQ; ++i) {
+                    uint32_t top = __vmaxu2(__vmaxu2(y[i].x & 0x7fff7fffu, y[i].y & 0x7fff7fffu), __vmaxu2(y[i].z & 0x7fff7fffu, y[i].w & 0x7fff7fffu));
+#pragma unroll
+                    for (int o = kLanesQ / 2; o > 0; o >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
+                    const int e = min(max((int)(max(top >> 16, top & 0xffffu) >> 7) - 8, 1), 253);
+                    const float f = __uint_as_float((uint32_t)(254 - e) << 23);
+                    auto two = [&](uint32_t& z) {
+                        const float lo = __uint_as_float(z << 16) * f, hi = __uint_as_float(z & 0xffff0000u) * f;
+                        z = wide ? pack_bf16x2(lo, hi) : pack_f16x2(lo, hi);
+                    };
+                    two(y[i].x); two(y[i].y); two(y[i].z); two(y[i].w);
+                    const int mine = __shfl_sync(0xffffffffu, e, lane % kRowsPassQ * kLanesQ);
+                    if (lane / kRowsPassQ == i) q_back = __uint_as_float((uint32_t)mine << 23) * back;      // (of this thread's own row)
+                }
+            }
+            const uint32_t d = sQ + u * Cfg::kTileBytes + (qc >> 3) * 16384 + (row & 96) * 128;
+#pragma unroll
+            for (int i = 0; i < kLanesQ; ++i) {
+                const int r = i * kRowsPassQ + qr0;
+                pt_st_shared4(d + r * 128 + (((qc ^ r) & 7) << 4), y[i].x, y[i].y, y[i].z, y[i].w);
+            }
+            fence_proxy_async();
+            mbar_arrive(bar(Cfg::kQFull + u));
         }
         if (u < nh) {
             const PagedView see = paged_view(a, is_summ, x);
@@ -548,6 +584,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                 const float2 nm2 = make_float2(neg_m, neg_m);
                 bool pv_ok = false;                           // the product before is known to be done
                 float2 la = make_float2(0.f, 0.f), lb = make_float2(0.f, 0.f);
+                auto exponentials = [&](auto half) {           // (half: whether as f16)
 #pragma unroll
                 for (int q = 0; q < 64; ++q) {
                     const float2 z = ffma2(make_float2(__uint_as_float(s[2 * q]), __uint_as_float(s[2 * q + 1])), sc2, nm2);
@@ -555,7 +592,13 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                     pr.x = ex2_approx(z.x); pr.y = ex2_approx(z.y);
                     if (q & 1) lb = fadd2(lb, pr); else la = fadd2(la, pr);
                     if (q == 48 && j > 0) pv_ok = mbar_test_wait(bar(Cfg::kPvDone + u), pv_phase);
-                    s[q] = E4M3 ? pack_f16x2(pr.x, pr.y) : pack_bf16x2(pr.x, pr.y);
+                    s[q] = half ? pack_f16x2(pr.x, pr.y) : pack_bf16x2(pr.x, pr.y);
+                }
+                };
+                if constexpr (E4M3) {
+                    if (wide) exponentials(std::false_type{}); else exponentials(std::true_type{});
+                } else {
+                    exponentials(std::false_type{});
                 }
                 l_run += (la.x + la.y) + (lb.x + lb.y);
                 if (j > 0) {

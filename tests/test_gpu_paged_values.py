@@ -44,6 +44,25 @@ def test_value_rows_of_any_scale(ctx, kernel, before, n, byte, where):
     s.check(out, lse, spans, sample=6)
 
 
+# ---- rows out of one another's sight -----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kernel,before,n", [(FEW, 300, 5), (FEW, 2500, 5), (MANY, 300, 40), (MANY, 2500, 40)])
+@pytest.mark.parametrize("what", ["key", "val"])
+@pytest.mark.parametrize("byte", [155, 186, 247])
+def test_rows_beside_large_ones_that_they_do_not_see(ctx, kernel, before, n, what, byte):
+    """The later half of the new rows is large; the earlier half comes before them, in the same query tile."""
+    s = Strict(ctx, 8, 1, 1 << 10, 8, 2, 128, 32, "e4m3", [before + n], seed=byte, flags=kernel)
+    rows = (s.key if what == "key" else s.val)[0]
+    rows[before + n // 2:] = _size(rows[before + n // 2:].shape, byte)
+    spans = [(before, n)]
+    s.fill(spans)
+    out, lse = _no_workspace(s, spans)
+    half = n // 2
+    if what == "key":                                      # (scores of the others are beyond fp32 at the largest scale)
+        spans = [(before, half)]
+        out, lse = out[:half], lse[:, :half]
+    s.check(out, lse, spans, sample=10)
+
+
 # ---- queries of zeros -----------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("kernel,before,n", [(FEW, 300, 5), (MANY, 300, 40), (MANY, 2500, 40)])
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
@@ -63,7 +82,7 @@ def test_small_queries_and_keys(ctx, kernel, before, n, fmt, keys, q):
 # ---- one key that outweighs thousands --------------------------------------------------------------------------------------
 @pytest.mark.parametrize("kernel,n,ws", [(FEW, 1, False), (FEW, 4, False), (MANY, 70, False), (MANY, 70, True)])
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
-@pytest.mark.parametrize("gap,sink", [(8, 0.0), (16, 0.0), (16, 2.0 ** -6), (18, 0.0), (18, 2.0 ** -6)])
+@pytest.mark.parametrize("gap,sink", [(8, 0.0), (16, 0.0), (16, 2.0 ** -6), (18, 0.0), (18, 2.0 ** -6), (24, 0.0), (40, 0.0)])
 def test_one_key_that_outweighs_the_others(ctx, kernel, n, ws, fmt, gap, sink):
     """An attention sink: a first key whose score stands `gap` above those of 3,000 others, with a value row of zeros or a small one.
     ws: with the workspace, where the call takes one."""
