@@ -58,7 +58,7 @@ __device__ __forceinline__ bool paged_find(const PagedArgs& a, const PagedSeqs& 
         first = __ldcg(a.cached + lo);
     }
     int n;
-    if (i >= a.rows || !paged_seq(a, row0, r1, first, n) || i < row0 || i >= r1) return false;
+    if (i >= a.rows || !paged_seq(a, lo, row0, r1, first, n) || i < row0 || i >= r1) return false;
     bool summ;
     const int x = paged_place(a, first + (i - row0), summ);
     page = paged_page(a, lo, summ, x);
@@ -72,7 +72,7 @@ __device__ __forceinline__ void paged_check_all(const PagedArgs& a)
     if (blockIdx.x + blockIdx.y != 0) return;
     for (int b = threadIdx.x; b < a.B; b += kRowThreads) {
         int n;
-        paged_seq(a, __ldcg(a.cu + b), __ldcg(a.cu + b + 1), __ldcg(a.cached + b), n);
+        paged_seq(a, b, __ldcg(a.cu + b), __ldcg(a.cu + b + 1), __ldcg(a.cached + b), n);
     }
 }
 
@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(kUnpackThreads) ksa_paged_unpack_kernel(PagedA
     const int b = blockIdx.z, h = blockIdx.y, slot = blockIdx.x;
     int n;
     const int first = __ldcg(a.cached + b);
-    if (!paged_seq(a, __ldcg(a.cu + b), __ldcg(a.cu + b + 1), first, n) || n < a.rows_min || n > a.rows_max) return;
+    if (!paged_seq(a, b, __ldcg(a.cu + b), __ldcg(a.cu + b + 1), first, n) || n < a.rows_min || n > a.rows_max) return;
     const bool summ = slot >= u.text_pages;
     const PagedRange see = paged_range(a, first, n, summ);
     const int tile = summ ? slot - u.text_pages : see.lo / 128 + slot, x0 = tile * 128;

@@ -58,11 +58,11 @@ inline int64_t paged_most_tiles(const PagedArgs& a)
 // ---- rows and pages -------------------------------------------------------------------------------------------------
 // (Lengths, tables and rows are read past L1: a kernel here may start while the one before the one in front of it still reads,
 // after which L1 may keep a line that the one in front rewrites.)
-// A sequence's lengths, checked: false for what are no lengths (nothing of such a sequence is touched).
-__device__ __forceinline__ bool paged_seq(const PagedArgs& a, int row0, int r1, int first, int& n)
+// Sequence b's lengths, checked: false for what are no lengths (nothing of such a sequence is touched).
+__device__ __forceinline__ bool paged_seq(const PagedArgs& a, int b, int row0, int r1, int first, int& n)
 {
     n = r1 - row0;
-    if (!paged_lengths_ok(a, row0, r1, first)) {
+    if (!paged_lengths_ok(a, row0, r1, first) || (b == 0 && row0 != 0)) {
         atomicCAS(a.status, 0, KSA_PAGED_STATUS_BAD_ROWS);
         n = 0;
         return false;
@@ -83,10 +83,10 @@ __device__ __forceinline__ int paged_page(const PagedArgs& a, int b, bool summ, 
 // kMix: a run that fits into a tile is one, text tokens and summaries together.
 struct PagedRun { int n, t0, nt, tt, ts; };
 template <bool kMix>
-__device__ __forceinline__ PagedRun paged_run(const PagedArgs& a, int row0, int r1, int first)
+__device__ __forceinline__ PagedRun paged_run(const PagedArgs& a, int b, int row0, int r1, int first)
 {
     PagedRun r{};
-    paged_seq(a, row0, r1, first, r.n);
+    paged_seq(a, b, row0, r1, first, r.n);
     if (r.n < a.rows_min || r.n > a.rows_max) r.n = 0;
     if (r.n > 0) {
         r.t0 = paged_texts(a, first);
@@ -125,7 +125,7 @@ __device__ __forceinline__ PagedTile paged_tile(const PagedArgs& a, int item, Pa
             for (int u = 0; u < kAhead; ++u) {
                 int tiles = 0;
                 if (at + u * kThreads < a.B) {
-                    const PagedRun r = paged_run<kMix>(a, rows0[u], rows1[u], firsts[u]);
+                    const PagedRun r = paged_run<kMix>(a, at + u * kThreads + (int)threadIdx.x, rows0[u], rows1[u], firsts[u]);
                     tiles = (int)__reduce_add_sync(0xffffffffu, (unsigned)(r.tt + r.ts));
                 }
                 if (lane == 0) found.keys[u * kWarps + warp] = tiles;
@@ -156,7 +156,7 @@ __device__ __forceinline__ PagedTile paged_tile(const PagedArgs& a, int item, Pa
             if (base + lane < a.B) {
                 row0 = __ldcg(a.cu + base + lane);
                 first = __ldcg(a.cached + base + lane);
-                r = paged_run<kMix>(a, row0, __ldcg(a.cu + base + lane + 1), first);
+                r = paged_run<kMix>(a, base + lane, row0, __ldcg(a.cu + base + lane + 1), first);
             }
             int n = r.n, t0 = r.t0, nt = r.nt, tt = r.tt, ts = r.ts;
             int seq = base + lane;

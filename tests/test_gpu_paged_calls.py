@@ -1,0 +1,35 @@
+"""What the paged calls promise of their arguments on the device: lengths, padding rows, pools without scales."""
+import pytest
+import torch
+
+from paper_2604_24432_b200 import binding as ksa
+from tests.paged_check import Strict
+from tests.test_gpu_paged import BY_RULE, DEV, FEW, MANY, _i32, ctx  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("kernel", [BY_RULE, MANY, FEW])
+@pytest.mark.parametrize("n", [1, 130, 700])
+@pytest.mark.parametrize("others", [1, 70])                    # (more than 64 sequences are looked for in another way)
+def test_packed_rows_start_at_0(ctx, kernel, n, others):
+    """cu_rows[0] other than 0: reported, and of the first sequence nothing is written."""
+    s = Strict(ctx, 8, 1, 4, 16, 2, 64, 16, "e4m3", [900, 900] + [20] * (others - 1), seed=6, flags=kernel)
+    spans = [(60, n), (60, n)] + [(10, 1)] * (others - 1)
+    s.fill(spans)
+    b = s.batch(spans)
+    cu = b.cu_rows.clone()
+    cu[0] = 1
+    b = ksa.PagedBatch(b.cached, cu, b.text_table, b.summ_table)
+    q = s.rows(s.q, spans)
+    out, lse = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV), torch.full((16, q.shape[0]), -1.0, device=DEV)
+    back = [torch.full((q.shape[0], 2, 64), 7.0, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    rows = [s.rows(x, spans) for x in (s.key, s.val)]
+    for call in (lambda: s.cache.attn(b, q, out, lse), lambda: s.cache.gather(b, *back), lambda: s.cache.append(b, *rows)):
+        ctx.clear_device_status()
+        call()
+        torch.cuda.synchronize()
+        assert ctx.device_status() == ksa.KSA_PAGED_STATUS_BAD_ROWS
+    ctx.clear_device_status()
+    assert (out[:n] == 7.0).all() and (lse[:, :n] == -1.0).all() and all((t[:n] == 7.0).all() for t in back)
+    s.check(out[n:], lse[:, n:], [(0, 0)] + spans[1:], sample=2)
