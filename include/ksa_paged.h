@@ -24,7 +24,8 @@
  * Calls.  A call takes `batch` sequences; sequence b has `cached[b]` rows before the call and the packed rows
  * [cu_rows[b], cu_rows[b + 1]) of the call's tensors, its rows cached[b], cached[b] + 1, ...  Lengths and tables are read on
  * the device: a call recorded into a CUDA graph follows what stands there at each replay.  num_rows is the rows of the
- * tensors; rows from cu_rows[batch] on are not read, and left as they were.  A sequence may have no rows.
+ * tensors, all of them in memory; what stands in rows from cu_rows[batch] on does not matter (ksa_paged_append may load it), and
+ * they are left as they were.  A sequence may have no rows.
  *
  * Tensors (DEVICE; bf16 unless said otherwise; 16-byte aligned; strides in elements, multiples of 8 for bf16 and of 16 for
  * e4m3, of pages and of what is written not 0; head_dim contiguous):

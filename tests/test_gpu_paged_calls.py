@@ -1,4 +1,4 @@
-"""What the paged calls promise of their arguments on the device: lengths, padding rows, pools without scales."""
+"""What the paged calls promise of their arguments on the device: lengths, padding rows."""
 import pytest
 import torch
 
@@ -33,3 +33,19 @@ def test_packed_rows_start_at_0(ctx, kernel, n, others):
     ctx.clear_device_status()
     assert (out[:n] == 7.0).all() and (lse[:, :n] == -1.0).all() and all((t[:n] == 7.0).all() for t in back)
     s.check(out[n:], lse[:, n:], [(0, 0)] + spans[1:], sample=2)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("seqs", [2, 40])
+def test_what_stands_in_padding_rows_does_not_matter(ctx, fmt, seqs):
+    """Rows behind the last sequence may be read, as memory of the tensors, and are used for nothing."""
+    s = Strict(ctx, 8, 1, 4, 8, 8, 128, 16, fmt, [40] * seqs, seed=6)
+    spans, have = [(3, 30)] * seqs, 30 * seqs
+    pools = []
+    for fill in (0.0, float("nan")):
+        s.poison()
+        kk, vv = (torch.full((have + 50, 8, 128), fill, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        kk[:have], vv[:have] = s.rows(s.key, spans), s.rows(s.val, spans)
+        s.cache.append(s.batch(spans), kk, vv)
+        pools.append([t.view(torch.uint8).clone() for t in (s.cache.kpages, s.cache.vpages, s.cache.kscale, s.cache.vscale) if t is not None])
+    assert all(torch.equal(x, y) for x, y in zip(*pools))
