@@ -608,7 +608,8 @@ class PagedCache:
     """The page pools of a paged KV cache plus the calls on it (argument marshalling only).
 
     kpages, vpages [num_pages, Hkv, page_rows, D] (any strides, head_dim contiguous; bf16, or float8_e4m3fn with the scale
-    bytes kscale, vscale uint8 [num_pages, Hkv, page_rows]) are allocated here unless they are given."""
+    bytes kscale, vscale uint8 [num_pages, Hkv, page_rows]) are allocated here unless they are given.  e4m3 pools that are given
+    without their scales hold nothing yet: every row reads as NaN until it is appended."""
 
     def __init__(self, ctx: "Context", spec: PagedSpec, kpages=None, vpages=None, kscale=None, vscale=None):
         import torch
@@ -619,10 +620,10 @@ class PagedCache:
         dtype = torch.float8_e4m3fn if quantised else torch.bfloat16
         shape = (spec.num_pages, spec.Hkv, spec.page_rows, spec.D)
         _expect((kpages is None) == (vpages is None) and (kscale is None) == (vscale is None), "K and V pools come together")
+        if quantised and kscale is None:
+            kscale, vscale = (torch.full(shape[:3], 0 if kpages is None else 255, dtype=torch.uint8, device=self.device) for _ in range(2))
         if kpages is None:
             kpages, vpages = (torch.zeros(shape, dtype=dtype, device=self.device) for _ in range(2))
-        if quantised and kscale is None:
-            kscale, vscale = (torch.zeros(shape[:3], dtype=torch.uint8, device=self.device) for _ in range(2))
         _expect(quantised or kscale is None, "a bf16 cache has no scales")
         for t in (kpages, vpages):
             _expect(tuple(t.shape) == shape and t.dtype == dtype and t.device == self.device, "pools must be %s %s on %s" % (shape, dtype, self.device))

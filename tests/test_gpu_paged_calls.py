@@ -1,4 +1,4 @@
-"""What the paged calls promise of their arguments on the device: lengths, padding rows."""
+"""What the paged calls promise of their arguments on the device: lengths, padding rows, pools without scales."""
 import pytest
 import torch
 
@@ -49,3 +49,18 @@ def test_what_stands_in_padding_rows_does_not_matter(ctx, fmt, seqs):
         s.cache.append(s.batch(spans), kk, vv)
         pools.append([t.view(torch.uint8).clone() for t in (s.cache.kpages, s.cache.vpages, s.cache.kscale, s.cache.vscale) if t is not None])
     assert all(torch.equal(x, y) for x, y in zip(*pools))
+
+
+def test_pools_without_their_scales_hold_nothing(ctx):
+    """Scales of zeros would read them as 2^-127 times what they hold."""
+    s = Strict(ctx, 8, 0, 100, 4, 2, 64, 16, "e4m3", [40], seed=6)
+    s.append([(0, 40)])
+    again = ksa.PagedCache(ctx, s.cache.spec, s.cache.kpages, s.cache.vpages)
+    got = [torch.zeros((40, 2, 64), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    again.gather(s.batch([(0, 40)]), *got)
+    assert all(torch.isnan(g).all() for g in got)
+    b = s.batch([(0, 40)])
+    again.append(b, s.rows(s.key, [(0, 40)]), s.rows(s.val, [(0, 40)]))
+    again.gather(b, *got)
+    for g, x in zip(got, (s.key, s.val)):
+        assert (g.double().cpu().numpy() == s.cached_values(x[0])).all()
