@@ -90,6 +90,35 @@ static void upload_stream_give(int device)
     if (--u.users == 0) { cudaStreamDestroy(u.stream); u.stream = nullptr; }
 }
 
+// What the contexts of a device share while there are any: what was asked of the device, and that the paged attention kernels'
+// shared-memory opt-in, a per-device setting of twenty kernels, was done.  (A server may open a context for every thread.)
+namespace {
+struct DeviceShared { int contexts = 0, major = 0, num_sms = 0; bool paged_ready = false; };
+std::mutex g_device_mutex;
+DeviceShared g_device[64];                               // by device
+}  // namespace
+static cudaError_t device_take(int device, int* major, int* num_sms)
+{
+    if (device >= 64) return cudaErrorInvalidDevice;
+    std::lock_guard<std::mutex> lock(g_device_mutex);
+    DeviceShared& d = g_device[device];
+    if (d.contexts == 0) {
+        cudaDeviceProp prop;
+        const cudaError_t e = cudaGetDeviceProperties(&prop, device);
+        if (e != cudaSuccess) return e;
+        d.major = prop.major; d.num_sms = prop.multiProcessorCount;
+        d.paged_ready = false;
+    }
+    ++d.contexts;
+    *major = d.major; *num_sms = d.num_sms;
+    return cudaSuccess;
+}
+static void device_give(int device)
+{
+    std::lock_guard<std::mutex> lock(g_device_mutex);
+    --g_device[device].contexts;
+}
+
 static int cuda_fail(ksa_ctx* ctx, cudaError_t e)
 {
     if (ctx) ctx->last_cuda_error = (int)e;
@@ -101,7 +130,15 @@ int ksa_ctx_num_sms(const ksa_ctx* ctx) { return ctx->num_sms; }
 void ksa_ctx_add_launches(ksa_ctx* ctx, int n) { ctx->launches += n; }
 int ksa_ctx_cuda_fail(ksa_ctx* ctx, int cuda_error) { return cuda_fail(ctx, (cudaError_t)cuda_error); }
 bool* ksa_ctx_decode_ready(ksa_ctx* ctx) { return &ctx->decode_ready; }
-bool* ksa_ctx_paged_ready(ksa_ctx* ctx) { return &ctx->paged_ready; }
+int ksa_ctx_paged_setup(ksa_ctx* ctx, int (*setup)())
+{
+    if (ctx->paged_ready) return 0;
+    std::lock_guard<std::mutex> lock(g_device_mutex);
+    DeviceShared& d = g_device[ctx->device];
+    const int e = d.paged_ready ? 0 : setup();
+    if (e == 0) d.paged_ready = ctx->paged_ready = true;
+    return e;
+}
 int ksa_ctx_device(const ksa_ctx* ctx) { return ctx->device; }
 void* ksa_ctx_encode_tiled(const ksa_ctx* ctx) { return (void*)ctx->encode; }
 
@@ -486,13 +523,14 @@ extern "C" __attribute__((visibility("default"))) int ksa_create(ksa_ctx** out, 
     if (e != cudaSuccess) return KSA_ERR_CUDA;
     if (cuda_device < 0 || cuda_device >= count) return KSA_ERR_INVALID_ARG;
     if ((e = cudaSetDevice(cuda_device)) != cudaSuccess) return KSA_ERR_CUDA;
-    cudaDeviceProp prop;
-    if ((e = cudaGetDeviceProperties(&prop, cuda_device)) != cudaSuccess) return KSA_ERR_CUDA;
-    if (prop.major != 10) return KSA_ERR_UNSUPPORTED;     // kernels are built for sm_100a only
+    int major = 0, num_sms = 0;
+    if ((e = device_take(cuda_device, &major, &num_sms)) != cudaSuccess) return KSA_ERR_CUDA;
+    struct Give { int device; ~Give() { if (device >= 0) device_give(device); } } give{cuda_device};      // (on every way out but the last)
+    if (major != 10) return KSA_ERR_UNSUPPORTED;          // kernels are built for sm_100a only
     ksa_ctx* ctx = new (std::nothrow) ksa_ctx();
     if (!ctx) return KSA_ERR_NOMEM;
     ctx->device = cuda_device;
-    ctx->num_sms = prop.multiProcessorCount;
+    ctx->num_sms = num_sms;
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult qres;
     e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
@@ -502,6 +540,7 @@ extern "C" __attribute__((visibility("default"))) int ksa_create(ksa_ctx** out, 
     if ((e = cudaMemset(ctx->d_status, 0, sizeof(int32_t))) != cudaSuccess) { cudaFree(ctx->d_status); delete ctx; return KSA_ERR_CUDA; }
     cudaEventCreate(&ctx->ev0);
     cudaEventCreate(&ctx->ev1);
+    give.device = -1;
     *out = ctx;
     return KSA_OK;
 }
@@ -521,6 +560,7 @@ extern "C" __attribute__((visibility("default"))) int ksa_destroy(ksa_ctx* ctx)
     for (cudaEvent_t e : ctx->ev_done) cudaEventDestroy(e);
     if (ctx->s_in) cudaStreamDestroy(ctx->s_in);
     if (ctx->s_out) cudaStreamDestroy(ctx->s_out);
+    device_give(ctx->device);
     delete ctx;
     return KSA_OK;
 }

@@ -48,6 +48,6 @@ int ksa_ctx_num_sms(const ksa_ctx* ctx);
 void ksa_ctx_add_launches(ksa_ctx* ctx, int n);
 int ksa_ctx_cuda_fail(ksa_ctx* ctx, int cuda_error);        // records the error, returns KSA_ERR_CUDA
 bool* ksa_ctx_decode_ready(ksa_ctx* ctx);                   // the decode kernels' shared-memory opt-in was done on this context's device
-bool* ksa_ctx_paged_ready(ksa_ctx* ctx);                    // ... of the paged attention kernels
+int ksa_ctx_paged_setup(ksa_ctx* ctx, int (*setup)());      // ... of the paged attention kernels: once a device; a CUDA error
 int ksa_ctx_device(const ksa_ctx* ctx);
 void* ksa_ctx_encode_tiled(const ksa_ctx* ctx);              // cuTensorMapEncodeTiled

@@ -480,16 +480,13 @@ KSA_API int ksa_paged_attn(ksa_ctx* ctx, const ksa_paged_kv* kv, const void* q, 
     a.q = (const uint16_t*)q; a.out = (uint16_t*)out; a.lse = lse;
     bool e4m3 = p->kv_format == KSA_KV_E4M3;
     return paged_call(ctx, [&]() -> cudaError_t {
-        bool& ready = *ksa_ctx_paged_ready(ctx);                // shared-memory opt-in: a per-device setting
         const PagedEncode encode = (PagedEncode)ksa_ctx_encode_tiled(ctx);
         const cudaStream_t stream = (cudaStream_t)cuda_stream;
-        cudaError_t e = cudaSuccess;
-        if (!ready) {
-            e = setup_paged_attn();
-            if (e == cudaSuccess) e = setup_paged_tc();
-            if (e != cudaSuccess) return e;
-            ready = true;
-        }
+        cudaError_t e = (cudaError_t)ksa_ctx_paged_setup(ctx, [] {
+            const cudaError_t e = setup_paged_attn();
+            return (int)(e == cudaSuccess ? setup_paged_tc() : e);
+        });
+        if (e != cudaSuccess) return e;
         // Up to 16 query rows a sequence, on average (64 over e4m3 pages): the mma.sync kernel for all.  16 sequences of 3, 4, 5, 6, 8 rows
         // over 800 to 37,000, 32/8 heads (12 to 32 query rows), that one and the tcgen05 kernel: bf16 50, 50, 55, 86, 86 and 48, 51, 51,
         // 52, 55 us, e4m3 40, 41, 48, 57, 60 and 78, 81, 82, 84, 90 us.  More: the same where it is expected to be faster, since

@@ -545,10 +545,7 @@ template <int D, class F> static cudaError_t with_kernel(bool e4m3, int n, bool 
 }
 cudaError_t setup_paged_attn()
 {
-    auto set = [](auto kernel, int smem, int) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        return e != cudaSuccess ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    };
+    auto set = [](auto kernel, int smem, int) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem); };
     for (bool many : {false, true})
         for (int n : {1, 2})
             for (bool e4m3 : {false, true})
