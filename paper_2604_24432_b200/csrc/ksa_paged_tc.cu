@@ -363,10 +363,9 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                 page_before = page;
                 page = next;
             }
-            if (ld_shared_u32(abort_addr) != 0u) {           // leave no copy in flight behind
-                for (int st = 0; st < stages; ++st)
-                    if (armed_mask & (1u << st)) bounded_wait(full0 + 8u * st, (armed_parity >> st) & 1u, abort_addr + 4, a.status, kStatusWaitKvFull);
-            }
+            // leave no copy in flight behind, whoever gives up on it later on
+            for (int st = 0; st < stages; ++st)
+                if (armed_mask & (1u << st)) bounded_wait(full0 + 8u * st, (armed_parity >> st) & 1u, abort_addr + 4, a.status, kStatusWaitKvFull);
         } else if (warp != 11) {
             // =============================== MMA issuers =================================
             constexpr uint32_t hi = smem_desc_hi_sw128(1024);
