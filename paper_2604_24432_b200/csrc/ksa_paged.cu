@@ -66,6 +66,12 @@ __device__ __forceinline__ bool paged_find(const PagedArgs& a, const PagedSeqs& 
     return true;
 }
 
+// Whether a place is one of the pool (KSA_DEBUG builds: recorded, and the access skipped)
+__device__ __forceinline__ bool paged_place_ok(const PagedArgs& a, int page, int h, int slot)
+{
+    return ksa_in_bounds(page >= 0 && page < a.num_pages && h < a.Hkv && slot >= 0 && slot < (1 << a.page_shift), a.status);
+}
+
 // Every sequence's lengths, looked at by the first block: a row's search meets only those of the sequences that it lands in.
 __device__ __forceinline__ void paged_check_all(const PagedArgs& a)
 {
@@ -141,14 +147,14 @@ __global__ void __launch_bounds__(kRowThreads) ksa_paged_append_kernel(PagedArgs
         const int h = h0 + c;
         const int64_t at = page * a.page_st + h * a.head_st + slot * a.row_st;
         if constexpr (!E4M3) {
-            if (!put || h >= a.Hkv) continue;
+            if (!put || h >= a.Hkv || !paged_place_ok(a, page, h, slot)) continue;
             *reinterpret_cast<uint4*>(a.kp + at + lane * 16) = xk[c];
             *reinterpret_cast<uint4*>(a.vp + at + lane * 16) = xv[c];
         } else {
             uint32_t top = top8(xk[c]) | (top8(xv[c]) << 16);  // K's in the low half, V's in the high half
 #pragma unroll
             for (int o = kLanes / 2; o > 0; o >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
-            if (!put || h >= a.Hkv) continue;
+            if (!put || h >= a.Hkv || !paged_place_ok(a, page, h, slot)) continue;
             // the row's largest magnitude is (1 + mant / 128) 2^(e - 127): within 448 = 1.75 * 2^8 at 2^(e - 135), or at twice that
             auto scale_of = [](uint32_t t) { return t >= 0x7f80u ? 255 : max(17, (int)(t >> 7) - 8 + ((t & 0x7fu) > 0x60u)); };
             const int ek = scale_of(top & 0xffffu), ev = scale_of(top >> 16);
@@ -189,7 +195,7 @@ __global__ void __launch_bounds__(kRowThreads) ksa_paged_gather_kernel(PagedArgs
         yk[c] = yv[c] = Raw{};
         ek[c] = ev[c] = 0;
         const int h = h0 + c;
-        if (page >= 0 && h < a.Hkv) {
+        if (page >= 0 && h < a.Hkv && paged_place_ok(a, page, h, slot)) {
             const int64_t at = page * a.page_st + h * a.head_st + slot * a.row_st + lane * (int)sizeof(Raw);
             yk[c] = __ldcg(reinterpret_cast<const Raw*>(a.kp + at));
             yv[c] = __ldcg(reinterpret_cast<const Raw*>(a.vp + at));
@@ -202,7 +208,7 @@ __global__ void __launch_bounds__(kRowThreads) ksa_paged_gather_kernel(PagedArgs
 #pragma unroll
     for (int c = 0; c < kHeads; ++c) {
         const int h = h0 + c;
-        if (h >= a.Hkv) continue;
+        if (h >= a.Hkv || !ksa_in_bounds(i >= 0 && i < a.rows, a.status)) continue;
         uint4 xk, xv;
         if constexpr (E4M3) {
             const float fk = e8m0_scale(ek[c]), fv = e8m0_scale(ev[c]);
@@ -241,6 +247,7 @@ __global__ void __launch_bounds__(kUnpackThreads) ksa_paged_unpack_kernel(PagedA
     const int tile = summ ? slot - u.text_pages : see.lo / 128 + slot, x0 = tile * 128;
     if (x0 >= see.hi || x0 + 128 <= see.lo || tile >= (summ ? u.summ_cols : u.text_cols)) return;
     const int page = b * u.seq_pages + slot;
+    if (!ksa_in_bounds(tile >= 0 && slot < u.seq_pages && h < a.Hkv && b < a.B, a.status)) return;
     if (h == 0 && threadIdx.x == 0) (summ ? u.summ_table : u.text_table)[(int64_t)b * (summ ? u.summ_cols : u.text_cols) + tile] = page;
     // all of a thread's page lookups, then all of its loads, then its stores
     constexpr int kPasses = 128 / kRowsPass;
@@ -260,6 +267,7 @@ __global__ void __launch_bounds__(kUnpackThreads) ksa_paged_unpack_kernel(PagedA
             continue;
         }
         const int in = x0 + threadIdx.x / kLanes + i * kRowsPass & in_page;
+        if (!paged_place_ok(a, from[i], h, in)) { from[i] = -3; continue; }
         const int64_t at = from[i] * a.page_st + h * a.head_st + in * a.row_st + lane * 16, se = (((int64_t)from[i] * a.Hkv + h) << a.page_shift) + in;
         yk[i] = __ldcg(reinterpret_cast<const uint4*>(a.kp + at)); yv[i] = __ldcg(reinterpret_cast<const uint4*>(a.vp + at));
         ek[i] = __ldcg(a.ke + se); ev[i] = __ldcg(a.ve + se);
