@@ -27,7 +27,7 @@
  * tensors, all of them in memory; what stands in rows from cu_rows[batch] on does not matter (ksa_paged_append may load it), and
  * they are left as they were.  A sequence may have no rows.
  *
- * Tensors (DEVICE; bf16 unless said otherwise; 16-byte aligned; strides in elements, multiples of 8 for bf16 and of 16 for
+ * Tensors (DEVICE; bf16 unless said otherwise; 16-byte aligned, int32 and lse 4-byte; strides in elements, multiples of 8 for bf16 and of 16 for
  * e4m3, of pages and of what is written not 0; head_dim contiguous):
  *   q, out : [num_rows, num_q_heads, head_dim]     k, v : [num_rows, num_kv_heads, head_dim]
  *   lse    : fp32 [num_q_heads, num_rows], natural log of the softmax denominator

@@ -382,6 +382,8 @@ static int validate_paged(const ksa_paged_params* p, const ksa_paged_kv* kv)
     if (!kv->kpages || !kv->vpages || misaligned(kv->kpages) || misaligned(kv->vpages)) return KSA_ERR_INVALID_ARG;
     if (p->kv_format == KSA_KV_E4M3 && (!kv->kscale || !kv->vscale || misaligned(kv->kscale) || misaligned(kv->vscale))) return KSA_ERR_INVALID_ARG;
     if (!kv->text_table || (!kv->summ_table && p->summaries_per_chunk > 0) || !kv->cached || !kv->cu_rows) return KSA_ERR_INVALID_ARG;
+    for (const int32_t* t : {kv->text_table, kv->summ_table, kv->cached, kv->cu_rows})
+        if ((uintptr_t)t & 3) return KSA_ERR_INVALID_ARG;
     return KSA_OK;
 }
 

@@ -41,13 +41,13 @@ class Context:
         self.L, self.handle = L, ctypes.c_void_p()
         assert L.ksa_create(ctypes.byref(self.handle), device) == ksa.KSA_OK
 
-    def attn(self, rows=1):
+    def attn(self, rows=1, **other):
         D, Hkv, ps = 128, 2, 64
         p = ksa.ksa_paged_params(struct_size=ctypes.sizeof(ksa.ksa_paged_params), batch=1, num_rows=rows, chunk_len=8, summaries_per_chunk=1, window_chunks=4,
                                  num_q_heads=8, num_kv_heads=Hkv, head_dim=D, softmax_scale=0.1, flags=0, kv_format=ksa.KSA_KV_BF16, page_rows=ps,
                                  num_pages=7, text_cols=30, summ_cols=4, page_stride=Hkv * ps * D, head_stride=ps * D, row_stride=D,
                                  q_stride_tok=8 * D, q_stride_head=D, o_stride_tok=8 * D, o_stride_head=D)
-        kv = ksa.ksa_paged_kv(**{n: 0x10000 * (i + 1) for i, (n, _) in enumerate(ksa.ksa_paged_kv._fields_)})
+        kv = ksa.ksa_paged_kv(**{**{n: 0x10000 * (i + 1) for i, (n, _) in enumerate(ksa.ksa_paged_kv._fields_)}, **other})
         return self.L.ksa_paged_attn(self.handle, ctypes.addressof(kv), 0x900000, 0xA00000, 0xB00000, None, 0, ctypes.addressof(p), None)
 
     def close(self):
@@ -83,4 +83,13 @@ def test_a_setup_that_fails_is_tried_again(fake):
     fake.fake_fail_attribute(3)
     assert c.attn() == ksa.KSA_ERR_CUDA
     assert c.attn() == ksa.KSA_OK and _spent(fake, c.attn)["attributes"] == 0
+    c.close()
+
+
+@pytest.mark.parametrize("name", ["text_table", "summ_table", "cached", "cu_rows"])
+def test_integers_out_of_alignment_are_refused(fake, name):
+    c = Context(fake)
+    for off in (1, 2, 3):
+        assert c.attn(**{name: 0x40000 + off}) == ksa.KSA_ERR_INVALID_ARG
+    assert c.attn(**{name: 0x40004}) == ksa.KSA_OK
     c.close()
