@@ -61,6 +61,8 @@ struct PgCfg {
     static constexpr int kRingB = kStages * kStageB;            // of a warp
     // log2 units.  The reference maximum moves when a score outgrows it by this
     static constexpr float kRescale = 8.0f;
+    // bf16: what P stands below 2^(score - reference), so that O, a sum of P V, is within fp32 for V up to 2^128 and down to 2^-90
+    static constexpr float kLow = E4M3 ? 0.0f : 30.0f, kUnit = E4M3 ? 1.0f : 0x1p30f;
     static constexpr int kLd = D + 4;                           // floats from one row of partial results to the next
     static constexpr int kMl = E4M3 ? 4 : 2;                    // floats of a row beside O: maximum, sum; e4m3: the sum's own maximum
     static constexpr int kMergeB = kWarps * kRows * (kLd + kMl) * 4;    // the warps' results, over the ring
@@ -400,7 +402,7 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
             uint32_t pb[N][2];
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                const float sub0 = (m[n][0] == -INFINITY) ? 0.f : m[n][0], sub1 = (m[n][1] == -INFINITY) ? 0.f : m[n][1];
+                const float sub0 = (m[n][0] == -INFINITY) ? 0.f : m[n][0] + Cfg::kLow, sub1 = (m[n][1] == -INFINITY) ? 0.f : m[n][1] + Cfg::kLow;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float p0 = ptx::ex2_approx(s[u][n][2 * h] - sub0), p1 = ptx::ex2_approx(s[u][n][2 * h + 1] - sub1);
@@ -487,7 +489,7 @@ __global__ void __launch_bounds__(PgCfg<D, E4M3, N>::kThreads) ksa_paged_attn_ke
         if (!ksa_in_bounds(row >= 0 && row < a.rows && h < a.Hq, a.status)) return;
         *reinterpret_cast<uint2*>(a.out + row * a.o_st + h * a.o_sh + d) =
             make_uint2(ptx::pack_bf16x2(acc.x * inv * half, acc.y * inv * half), ptx::pack_bf16x2(acc.z * inv * half, acc.w * inv * half));
-        if (d == 0) a.lse[(int64_t)h * a.rows + row] = ((E4M3 ? w.ML : w.M) + log2f(w.L)) * 0.6931471805599453f;
+        if (d == 0) a.lse[(int64_t)h * a.rows + row] = ((E4M3 ? w.ML : w.M) + log2f(w.L * Cfg::kUnit)) * 0.6931471805599453f;
     };
     // Each CTA of the cluster sums up a share of the output's elements (4 columns of a row each), `share` of them: the others
     // write what they have of these into its memory, where the one barrier finds everything.

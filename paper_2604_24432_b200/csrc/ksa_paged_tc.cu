@@ -50,11 +50,12 @@ using namespace ptx;
 
 constexpr int kPtTile = 128;
 // log2 units: by how much a score may outgrow the reference maximum before that moves, and what P stands above 2^(score - reference).
-// bf16: P stays below 2^12 (see ksa_text_tc.cu).  f16 ends with 65,504 and loses bits below 2^-14, so P stays below 2^15 there, and as
+// bf16: P moves up to 2^12 past the first maximum (see ksa_text_tc.cu), and stands low, where bf16 keeps its bits: O is a sum of P V, which
+// has to be within fp32 for V up to 2^128 and thousands of keys, and for V down to 2^-90.  f16 ends with 65,504 and loses bits below 2^-14, so P stays below 2^15 there, and as
 // close to it as can be: it keeps 11 bits down to 2^-25 of the largest, and is 0 below 2^-36 of it.  (From 1 downwards, keys 18
 // natural-log units below a single one in the same CTA's share came out as nothing.  900 rows over 36,864, 4/4 heads of 64:
 // 32.7 and 32.9 us; 200 rows, 32/8 of 128: 65.2 and 66.3.)
-template <bool E4M3> struct PtScale { static constexpr float kRescale = E4M3 ? 4.0f : 12.0f, kLift = E4M3 ? 11.0f : 0.0f; };
+template <bool E4M3> struct PtScale { static constexpr float kRescale = E4M3 ? 4.0f : 12.0f, kLift = E4M3 ? 11.0f : -30.0f, kUnit = E4M3 ? 0x1p-11f : 0x1p30f; };
 
 template <int D, bool E4M3>
 struct PtCfg {
@@ -666,7 +667,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                         if (at >= 0) *reinterpret_cast<uint4*>(a.out + at + c * 32 + (lane & 3) * 8) = pk[e];
                     }
                 }
-                if (store) a.lse[(int64_t)head * a.rows + prow] = (m_used - PtScale<E4M3>::kLift + log2f(l_run)) * 0.6931471805599453f;
+                if (store) a.lse[(int64_t)head * a.rows + prow] = (m_used + log2f(l_run * PtScale<E4M3>::kUnit)) * 0.6931471805599453f;
                 tc_fence_before();
             }
         } else {
@@ -678,7 +679,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
             float part_m = m_used, part_l = l_run, part_f = 1.f;
             if constexpr (E4M3) {
                 part_f = (l_run == 0.f) ? 0.f : v_back * (0.125f / l_run);
-                part_m = (l_run == 0.f) ? -INFINITY : m_used + log2f(l_run);
+                part_m = (l_run == 0.f) ? -INFINITY : m_used + log2f(l_run * PtScale<E4M3>::kUnit);
                 part_l = (l_run == 0.f) ? 0.f : 1.f;
             }
             if (tokens > 0) {
@@ -753,7 +754,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
                     if (off < 0) continue;
                     const float inv = (E4M3 ? 8.f : 1.f) / L[r];
                     *reinterpret_cast<uint2*>(a.out + off + c4 * 4) = make_uint2(pack_bf16x2(acc[r].x * inv, acc[r].y * inv), pack_bf16x2(acc[r].z * inv, acc[r].w * inv));
-                    if (c4 == 0) a.lse[lse] = (M[r] - PtScale<E4M3>::kLift + log2f(L[r])) * 0.6931471805599453f;
+                    if (c4 == 0) a.lse[lse] = (M[r] + log2f(E4M3 ? L[r] : L[r] * PtScale<E4M3>::kUnit)) * 0.6931471805599453f;
                 }
             }
             __syncwarp();

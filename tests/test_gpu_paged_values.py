@@ -44,6 +44,22 @@ def test_value_rows_of_any_scale(ctx, kernel, before, n, byte, where):
     s.check(out, lse, spans, sample=6)
 
 
+@pytest.mark.parametrize("kernel,before,n", [(FEW, 300, 5), (FEW, 2500, 1), (MANY, 300, 40), (MANY, 2500, 40), (MANY, 2500, 300)])
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("byte", [45, 186, 220, 247])
+@pytest.mark.parametrize("where", ["alone", "beside", "unseen beside"])
+def test_value_rows_of_any_size_in_bf16(ctx, kernel, before, n, fmt, byte, where):
+    """The same values in bf16 pages, and in the bf16 copy of e4m3 pages (300 rows of 4 query heads)."""
+    s = Strict(ctx, 8, 1, 1 << 10, 8, 2, 128, 32, fmt, [before + n], seed=byte, flags=kernel)
+    v = s.val[0]
+    pick = slice(None) if where == "alone" else slice(None, None, 7) if where == "beside" else slice(before + n // 2, None)
+    v[pick] = _size(v[pick].shape, byte)
+    spans = [(before, n)]
+    s.fill(spans)
+    out, lse = s.attn(spans)
+    s.check(out, lse, spans, sample=6)
+
+
 # ---- rows out of one another's sight -----------------------------------------------------------------------------------------
 @pytest.mark.parametrize("kernel,before,n", [(FEW, 300, 5), (FEW, 2500, 5), (MANY, 300, 40), (MANY, 2500, 40)])
 @pytest.mark.parametrize("what", ["key", "val"])
