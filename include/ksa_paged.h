@@ -55,7 +55,7 @@ extern "C" {
 
 /* ksa_paged_attn takes what it expects to be faster for the call's sizes: the kernel for few query rows (mma.sync) for all
  * sequences, or the one for many (tcgen05), beside it the former for sequences of few rows where there are several.  These hold it
- * to the first or the second; results differ in the order of roundings only.  Not both. */
+ * to the first or the second; results differ by roundings (see ksa_paged_attn).  Not both. */
 #define KSA_FLAG_PAGED_MMA_SYNC  0x20u
 #define KSA_FLAG_PAGED_TCGEN05   0x40u
 
@@ -100,13 +100,18 @@ int ksa_paged_gather(ksa_ctx* ctx, const ksa_paged_kv* kv, void* k, void* v, con
  * sees are not looked up.  What stands in rows that no row of the call sees -- behind the sequence, before its windows --
  * does not matter; rows that one of the call's rows sees must be finite (or NaN reaches rows of the same sequence that do
  * not see them, and LSEs too).  e4m3 pages hold no NaN codes (0x7f, 0xff): a row of NaN is said by its scale byte.
+ *
+ * Roundings: scores, maxima, sums and outputs are fp32 until the output's one rounding to bf16.  A probability is rounded before its
+ * product with V, to bf16 (2^-8 of itself at most), or to f16 over e4m3 pages: the mma.sync kernel takes it times its value
+ * row's scale and keeps what is above 2^-25 of the largest such product among the keys of a warp, the tcgen05 kernel what is above
+ * 2^-36 of the largest probability (all of it where the scales of the value rows in view differ by more than 2^10).
  */
 int ksa_paged_attn(ksa_ctx* ctx, const ksa_paged_kv* kv, const void* q, void* out, float* lse, void* workspace, size_t workspace_bytes,
                    const ksa_paged_params* p, void* cuda_stream);
 /* Bytes of DEVICE workspace, 256-byte aligned, with which ksa_paged_attn is faster for p: 0 but for calls of many rows a sequence
  * over an e4m3 cache (then room for the rows in view as bf16; of p the strides do not matter).  The workspace is scratch
  * for the length of the call, and other work must not use it meanwhile; without one (NULL, or smaller) the call works all the
- * same, and its results differ in the order of roundings only. */
+ * same, and its results differ by roundings. */
 int ksa_paged_workspace_bytes(const ksa_paged_params* p, size_t* bytes);
 
 #define KSA_PAGED_STATUS_BAD_PAGE  103   /* a row that a call needs lies in no page of the pool */

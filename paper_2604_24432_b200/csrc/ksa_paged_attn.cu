@@ -13,7 +13,7 @@
 // first product's layout to the second's by movmatrix.  Running maximum and sum in fp32.
 //
 // bf16 rows: P rounded to bf16.  e4m3 rows become f16 in registers on their way into the products, one conversion for two
-// values (sm_100 has no mma.sync for e4m3: it is made of conversions to f16 and two f16 products).  So Q becomes f16 too, its
+// values (products of e4m3 take e4m3 on both sides, and Q and P would keep four bits of theirs).  So Q becomes f16 too, its
 // row scaled by a power of two, and the scale of a key multiplies its scores.  The scale of a value row goes into the
 // exponent, u = 2^(score + e - 127 - reference) with the reference maximum taken over these sums: u is at most 2^8 and what f16
 // rounds off or loses is relative to the largest that the row has met, whatever the scales are.  The softmax's sum has a

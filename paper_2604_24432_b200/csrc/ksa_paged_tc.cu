@@ -12,8 +12,8 @@
 //   warp  9     issues S = Q K^T (tcgen05.mma, smem x smem)
 //   warp 10     issues O += P V (P from TMEM)
 //   warp 11     TMA of the value tiles (bf16 pages)
-//   warps 12-15 (e4m3 pages) turn the tiles that warp 8 brings in 8 bits into f16 ones, a row per thread, its scale on the way
-// TMEM: one score slot S [0,128) that the two query tiles take in turns, the bf16 probabilities P0 [128,192), P1 [192,256),
+//   warps 12-15 (e4m3 pages) turn the tiles that warp 8 brings in 8 bits into f16 ones (or bf16, see below), a row's scale on the way
+// TMEM: one score slot S [0,128) that the two query tiles take in turns, the 16-bit probabilities P0 [128,192), P1 [192,256),
 // O0 [256,256+D), O1 [384,384+D).  The pipeline over the key tiles is that of the text-row kernel (ksa_text_tc.cu).
 //
 // e4m3 pages: the products are of f16 (one conversion for two values, one multiplication for their scale; as bf16 it takes three
@@ -29,7 +29,7 @@
 // of a range, or by the converting warps.
 //
 // Every mbarrier wait is bounded, as in the other kernels: on timeout all roles leave their loops, copies in flight are waited
-// for, the cluster's barriers are still passed, TMEM is freed.
+// for, the cluster's barriers are still passed, TMEM is freed.  (No test makes a wait of this kernel run out: the helper has one.)
 //
 // Measured: 1,152 rows over 36,864, 32/8 heads of 128, bf16: 72 us = 1,170 TFLOP/s of what is visible (83 us in a long loop, at the
 // power cap; 128 of the query tiles are full ones, on 148 SMs); 1,000 and 1,024 rows over 16,001 and 7,168, causal, 16/16 heads:
@@ -187,7 +187,7 @@ ksa_paged_tc_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__
 
     if (warp >= 12) {
         if constexpr (E4M3) {
-            // ============================ 8-bit tiles to bf16 ============================
+            // ============================ 8-bit tiles to 16 bits ==========================
             setmaxnreg_dec<Cfg::kRegsConvert>();
             const int row = tid & 127;
             bool alive = true;
