@@ -104,7 +104,8 @@ int ksa_paged_gather(ksa_ctx* ctx, const ksa_paged_kv* kv, void* k, void* v, con
  * Roundings: scores, maxima, sums and outputs are fp32 until the output's one rounding to bf16.  A probability is rounded before its
  * product with V, to bf16 (2^-8 of itself at most), or to f16 over e4m3 pages: the mma.sync kernel takes it times its value
  * row's scale and keeps what is above 2^-25 of the largest such product among the keys of a warp, the tcgen05 kernel what is above
- * 2^-36 of the largest probability (all of it where the scales of the value rows in view differ by more than 2^10).
+ * 2^-36 of the largest probability (all of it where the scales of the value rows in view differ by more than 2^10).  q over e4m3
+ * pages is f16 too, times a power of two for each row: exact down to 2^-22 of the row's largest value, off by 2^-33 of that at most below.
  */
 int ksa_paged_attn(ksa_ctx* ctx, const ksa_paged_kv* kv, const void* q, void* out, float* lse, void* workspace, size_t workspace_bytes,
                    const ksa_paged_params* p, void* cuda_stream);

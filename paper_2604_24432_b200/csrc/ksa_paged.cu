@@ -2,8 +2,8 @@
 //
 // Both passes are bound by HBM: an element is read and written once.  D / 8 lanes take one row of one head, 16 bytes of
 // bf16 each, K and V of it at once; the row's sequence, page and place in the page are worked out by every lane for itself.
-// Measured: 32,176 bf16 rows of 16 heads of 128 written in 84.6 us = 6,230 GB/s, 147,456 e4m3 rows of 4 heads read back in 75.6 us =
-// 6,010 GB/s (a copy: 6,465); 9,216 e4m3 rows of 8 heads written in 13.7 us, where launch and dependent loads count.
+// Measured: 32,176 bf16 rows of 16 heads of 128 written in 84.6 us = 6,230 GB/s, 147,456 e4m3 rows of 4 heads read back in 75.6 - 79 us =
+// 6,010 - 5,750 GB/s (a copy: 6,465); 9,216 e4m3 rows of 8 heads written in 13.6 us, where launch and dependent loads count.
 #include <cuda_bf16.h>
 
 #include <algorithm>

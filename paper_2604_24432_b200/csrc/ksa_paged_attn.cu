@@ -24,7 +24,7 @@
 // does not matter as long as Q agrees, so lane t takes columns 4 t .. 4 t + 3 as they stand.  Of V, ldmatrix.trans hands a lane
 // two neighbouring columns of two keys, which become rows r and r + 8 of a product.
 //
-// Measured: 32 tokens, each over 147,451 rows, 32/4 heads of 128: bf16 181 us = 6,270 GB/s (a copy: 6,465), e4m3 106 us = 5,400 GB/s,
+// Measured: 32 tokens, each over 147,451 rows, 32/4 heads of 128: bf16 180 us = 6,300 GB/s (a copy: 6,465), e4m3 110 us = 5,190 GB/s,
 // the conversions, the products and HBM about level; one token over 9,219 rows, 32/8 heads, bf16: 8.0 us.
 #include <cuda_bf16.h>
 
